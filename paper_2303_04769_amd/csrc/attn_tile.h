@@ -1,0 +1,295 @@
+// What the attention kernels share (attn.hip, attn_token.hip, attn_grad.hip): arguments, addresses, scores, tiles in LDS (gfx950).
+//
+// All products run on v_mfma_f32_16x16x4_f32: lane l = 16 g + m gives row m of the left operand (column m of the right one) at
+// reduction index g, and holds rows 4g .. 4g+3 of column m of the result. Reduction indices may be permuted as long as both
+// operands agree, and two permutations make every operand come straight from where it lies:
+//   - over channels, index g of step (c, e) is channel 16c + 4g + e: a lane's four steps are one 16-byte load;
+//   - over the tokens of a tile, index g of step (b, r) is token 16b + 4g + r: exactly the rows that a lane already holds of the product
+//     before. So scores are taken transposed (rows: keys, columns: queries), and their exponentials are the next product's right
+//     operand in the registers where they were computed; softmax statistics are per lane and column, joined over four lanes.
+// The left operand of that second product wants channels in lanes: channel 16 VD grp + VD m + v for result tile grp * VD + v, so
+// that a lane reads VD neighbouring channels of a token at once and ends up with 4 VD neighbouring ones of the result.
+#pragma once
+#include "small_internal.h"
+
+namespace small {
+
+struct TokenStrides { long long image, block, token; };      // floats
+
+struct AttnArgs {
+    const float *q, *k, *v;
+    float *o, *lse;
+    TokenStrides qs, ks, vs, os;
+    int N, Sq, Sk, heads, group, D, Cb;
+    float scale, cap;                                        // scale of the dot products; cap = 0: none
+    int causal, width, reach, buckets;
+    const int *lengths, *first, *prefix, *docs;
+    const float *slopes, *table;
+    const int *bucket;
+    // derived
+    int pack;                     // a workgroup's rows run over the query heads of one key head (few queries, shared heads)
+    int head_sets, rows;          // heads / group sets of group * Sq rows, or heads of Sq
+    int splits, bias_lds;         // bias_lds: heads whose expanded bias fits LDS (0: gathered from memory)
+    int row_tiles;
+    FastDiv by_Cb, by_Sq, by_width, by_tiles, by_sets, by_splits, by_group;
+    float *part_o;
+    float2 *part_ml;              // splits > 1: results before joining, and their (maximum, sum)
+    // gradient
+    const float *dout, *lse_in;
+    float *dq, *dk, *dv, *delta, *part_bias;                 // part_bias: null, or [N * heads * row_tiles][2 reach + 1]
+    TokenStrides dos, dqs, dks, dvs;
+    int key_tiles, bias_acc_lds;
+    FastDiv by_key_tiles, by_code, by_heads;                 // by_code: 2 width - 1
+};
+
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
+constexpr int kFar = 1 << 28;     // positions are taken into -kFar .. kFar: differences of their numbers fit an int
+constexpr float kInf = __builtin_huge_valf();
+
+__device__ __forceinline__ const float *token_at(const float *p, const TokenStrides &s, int n, long long t)
+{
+    return p + n * s.image + t * s.token;
+}
+// Offset of a channel from its token's place.
+__device__ __forceinline__ long long channel_at(const AttnArgs &a, const TokenStrides &s, int ch)
+{
+    const int b = a.by_Cb.div(ch);
+    return b * s.block + (ch - b * a.Cb);
+}
+
+// Channels d .. d + 3 of a head whose first channel is c0, zeros from channel D on. VEC: D, Cb and all strides are multiples of four
+// and the tensors 16-byte aligned, so that the four stand together.
+template <bool VEC>
+__device__ __forceinline__ floatx4 load_quad(const AttnArgs &a, const TokenStrides &s, const float *token, int c0, int d)
+{
+    if constexpr (VEC) {
+        if (d >= a.D) return floatx4{0.f, 0.f, 0.f, 0.f};
+        return *reinterpret_cast<const floatx4 *>(token + channel_at(a, s, c0 + d));
+    } else {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = d + i < a.D ? token[channel_at(a, s, c0 + d + i)] : 0.f;
+        return floatx4{x[0], x[1], x[2], x[3]};
+    }
+}
+template <bool VEC>
+__device__ __forceinline__ void store_quad(const AttnArgs &a, const TokenStrides &s, float *token, int c0, int d, floatx4 x)
+{
+    if constexpr (VEC) {
+        if (d < a.D) *reinterpret_cast<floatx4 *>(token + channel_at(a, s, c0 + d)) = x;
+    } else {
+        const float y[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (d + i < a.D) token[channel_at(a, s, c0 + d + i)] = y[i];
+    }
+}
+
+__device__ __forceinline__ floatx4 mfma(float a, float b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// VD of the second product's left operand.
+template <int DT> constexpr int kVD = DT % 4 == 0 ? 4 : DT % 2 == 0 ? 2 : 1;
+
+// Number of a position: differs by a number of its own for every offset of rows and columns of images `width` pixels wide.
+__device__ __forceinline__ int code_of(const AttnArgs &a, int p)
+{
+    const int w = a.width;
+    if (w == 1) return p;
+    const int row = p >= 0 ? a.by_width.div(p) : -a.by_width.div(w - 1 - p);
+    return row * (2 * w - 1) + (p - row * w);
+}
+
+// What masks an image's keys: length, prefix.
+struct ImageMask {
+    int len, prefix, first;
+    __device__ __forceinline__ ImageMask(const AttnArgs &a, int n)
+    {
+        len = a.lengths ? max(0, min(a.lengths[n], a.Sk)) : a.Sk;
+        prefix = a.prefix ? min(a.prefix[n], a.Sk) : 0;
+        first = a.first ? max(-kFar, min(a.first[n], kFar)) : a.Sk - a.Sq;
+    }
+    __device__ __forceinline__ int position(int i) const { return max(-kFar, min(first + i, kFar)); }
+};
+
+// What a query needs besides its channels. It sees the keys in front of `bound` -- of its document, if there are documents.
+struct RowState {
+    int p, code, bound, doc, head;
+    float slope;                  // times log2(e)
+    __device__ __forceinline__ RowState(const AttnArgs &a, const ImageMask &im, int n, int i, int h)
+    {
+        p = im.position(i);
+        code = a.table ? code_of(a, p) : 0;
+        bound = a.causal ? min(im.len, max(p + 1, im.prefix)) : im.len;
+        doc = a.docs && p >= 0 && p < a.Sk ? a.docs[(size_t)n * a.Sk + p] : -2;
+        if (doc < 0) doc = -2;
+        head = h;
+        slope = a.slopes ? a.slopes[h] * kLog2e : 0.f;
+    }
+    // (no branches: a choice among vector elements behind lane-dependent branches has been compiled wrongly here)
+    __device__ __forceinline__ bool sees(int j, int key_doc, bool docs) const { return (j < bound) & (!docs | (key_doc == doc)); }
+};
+__device__ __forceinline__ int key_document(const AttnArgs &a, int n, int j)       // -1: none (no query has that)
+{
+    return max(-1, a.docs[(size_t)n * a.Sk + min(j, a.Sk - 1)]);
+}
+
+// tanh as the seventh convergent of Lambert's continued fraction x / (1 + x^2 / (3 + x^2 / (5 + ...))), all of whose terms are positive:
+// within 2^-23 of its value up to |x| = 2; beyond, 1 - 2 / (exp(2x) + 1), where nothing cancels any more.
+__device__ __forceinline__ float tanh_of(float x)
+{
+    const float y = x * x;
+    const float n = fmaf(y, fmaf(y, y + 378.f, 17325.f), 135135.f), d = fmaf(y, fmaf(y, fmaf(y, 28.f, 3150.f), 62370.f), 135135.f);
+    float r = x * n * __builtin_amdgcn_rcpf(d);
+    if (fabsf(x) > 2.f) {
+        const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
+        r = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
+    }
+    return r;
+}
+
+// A bias in units of log2. One of about the type's lowest value hides its offsets as minus infinity does: a sum of weights of scores of that size
+// could not be written next to them in a row's lse, from which the gradient takes the weights.
+__device__ __forceinline__ float bias_log2(float b) { return b < -1e30f ? -kInf : b * kLog2e; }
+__device__ __forceinline__ float bias_gather(const AttnArgs &a, int head, int at)       // at: offset's place in 0 .. 2 reach
+{
+    const int b = max(0, min(a.bucket[at], a.buckets - 1));
+    return bias_log2(a.table[(size_t)head * a.buckets + b]);
+}
+__device__ __forceinline__ int offset_at(const AttnArgs &a, int key_code, int code) { return max(-a.reach, min(key_code - code, a.reach)) + a.reach; }
+
+// The scores of a lane's four neighbouring keys j0 .. j0 + 3 for its row, in units of log2, from their dot products. bias: the row's head's
+// expanded bias in LDS, or null. far: every offset of the tile is at one end of the reach, whose bias is far_bias.
+struct Scorer {
+    const AttnArgs &a;
+    float scale2, cap_in, cap2;
+    __device__ __forceinline__ Scorer(const AttnArgs &args) : a(args)
+    {
+        scale2 = a.scale * kLog2e;
+        cap_in = a.cap > 0.f ? a.scale / a.cap : 0.f;
+        cap2 = a.cap * kLog2e;
+    }
+    __device__ __forceinline__ float capped(float dot) const { return a.cap > 0.f ? cap2 * tanh_of(dot * cap_in) : dot * scale2; }
+    __device__ __forceinline__ float biased(float t, const RowState &row, int j, int key_code, const float *bias) const
+    {
+        if (a.slopes) t = fmaf(-row.slope, fabsf((float)(row.p - j)), t);
+        if (a.table) {
+            const int at = offset_at(a, key_code, row.code);
+            t += bias ? bias[at] : bias_gather(a, row.head, at);
+        }
+        return t;
+    }
+};
+
+// A tile of KT tokens in LDS: [channels / 16][token][16], chunks 16 floats further apart than they are long, so that the four chunks that a
+// wave reads of one token are in different banks.
+template <int DT, int KT>
+struct Tile {
+    static constexpr int kChunk = KT * 16 + 16, kFloats = DT * kChunk, kAll = KT * DT * 4, kQuads = (kAll + 255) / 256;
+    // Thread t's quads of the tile, tokens from j0 on; on(token) says which are read, others are zeros.
+    template <bool VEC, typename On>
+    static __device__ __forceinline__ void fetch(floatx4 (&x)[kQuads], const AttnArgs &a, const TokenStrides &s, const float *base, int n, int c0, int j0, On on)
+    {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) {
+            const int e = threadIdx.x + i * 256, q = e & 3, j = (e >> 2) % KT, c = (e >> 2) / KT;
+            x[i] = floatx4{0.f, 0.f, 0.f, 0.f};
+            if ((kAll % 256 == 0 || e < kAll) && on(j)) x[i] = load_quad<VEC>(a, s, token_at(base, s, n, j0 + j), c0, c * 16 + q * 4);
+        }
+    }
+    static __device__ __forceinline__ void put(float *lds, const floatx4 (&x)[kQuads])
+    {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) {
+            const int e = threadIdx.x + i * 256, q = e & 3, j = (e >> 2) % KT, c = (e >> 2) / KT;
+            if (kAll % 256 == 0 || e < kAll) *reinterpret_cast<floatx4 *>(lds + c * kChunk + j * 16 + q * 4) = x[i];
+        }
+    }
+    // Left operand with tokens in lanes: channels 16c + 4g .. +3 of token 16b + m.
+    static __device__ __forceinline__ floatx4 tokens(const float *lds, int b, int c, int m, int g)
+    {
+        return *reinterpret_cast<const floatx4 *>(lds + c * kChunk + (16 * b + m) * 16 + 4 * g);
+    }
+    // Left operand with channels in lanes: channels VD m .. of group grp of token j.
+    template <int VD>
+    static __device__ __forceinline__ void channels(float (&x)[VD], const float *lds, int j, int grp, int m)
+    {
+        const float *p = lds + (grp * VD + m * VD / 16) * kChunk + j * 16 + (m * VD & 15);
+        if constexpr (VD == 4) {
+            const floatx4 f = *reinterpret_cast<const floatx4 *>(p);
+            x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+        } else if constexpr (VD == 2) {
+            const float2 f = *reinterpret_cast<const float2 *>(p);
+            x[0] = f.x; x[1] = f.y;
+        } else {
+            x[0] = *p;
+        }
+    }
+};
+
+// The largest of a lane's value over the four lanes of its column, and the sum.
+__device__ __forceinline__ float column_max(float v)
+{
+    v = fmaxf(v, __shfl_xor(v, 16));
+    return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v)
+{
+    v += __shfl_xor(v, 16);
+    return v + __shfl_xor(v, 32);
+}
+
+// 4 VD neighbouring channels of a lane's column from result tiles grp * VD .. : quad x of them.
+template <int DT>
+__device__ __forceinline__ floatx4 result_quad(const floatx4 (&o)[DT], int grp, int x)
+{
+    constexpr int VD = kVD<DT>;
+    floatx4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int e = 4 * x + i;
+        r[i] = o[grp * VD + e % VD][e / VD];
+    }
+    return r;
+}
+
+// The keys of documents that a tile of rows belongs to: the smallest and one past the largest key whose document lies within lo .. hi
+// (whole workgroup; `words`: two ints of LDS, free afterwards for another call behind a barrier).
+__device__ __forceinline__ void document_hull(const int *docs, int from, int to, int lo, int hi, int *words, int *begin, int *end)
+{
+    if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; }
+    __syncthreads();
+    int first = 0x7fffffff, last = -1;
+    for (int j = from + threadIdx.x; j < to; j += blockDim.x) {
+        const int d = docs[j];
+        if (d >= 0 && d >= lo && d <= hi) { first = min(first, j); last = j; }
+    }
+    if (last >= 0) { atomicMin(&words[0], first); atomicMax(&words[1], last); }
+    __syncthreads();
+    *begin = words[0] == 0x7fffffff ? to : words[0];
+    *end = words[1] + 1;
+    if (*end < *begin) *end = *begin;
+}
+
+// Expanded biases and their gradients' sums go into LDS up to so many offsets.
+constexpr int kBiasLds = 8192;
+
+// A launch whose dynamic LDS may pass the 64 KB that a kernel has without asking (160 KB a compute unit).
+template <typename K>
+hipError_t launch_lds(K *kernel, unsigned grid, size_t lds, const AttnArgs &a, hipStream_t s)
+{
+    if (lds > 8192)
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
+    hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), lds, s, a);
+    return hipGetLastError();
+}
+
+// attn.hip, attn_token.hip, attn_grad.hip
+hipError_t launch_attn_rows(const AttnArgs &a, bool vec, size_t bias_bytes, hipStream_t s);
+hipError_t launch_attn_join(const AttnArgs &a, hipStream_t s);
+hipError_t launch_attn_grad_rows(const AttnArgs &a, bool vec, hipStream_t s);
+hipError_t launch_attn_grad_keys(const AttnArgs &a, bool vec, hipStream_t s);
+hipError_t launch_attn_grad_bias(const AttnArgs &a, float *sums, float *dtable, hipStream_t s);
+int attn_grad_tile(int D);                                   // tokens of a tile that the gradient kernels stream
+hipError_t launch_attn_token(const AttnArgs &a, bool vec, hipStream_t s);
+
+}  // namespace small

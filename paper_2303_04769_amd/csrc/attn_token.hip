@@ -1,0 +1,203 @@
+// Attention of few rows (at most 16: single tokens, and the query heads that share a key head) against a long cache, forward (gfx950).
+//
+// Bound by the cache's bytes: every key and value is read once, straight into the registers where the matrix instructions want it (no
+// LDS: nothing is shared between waves). A key head's rows are the 16 columns of a wave's products -- mostly empty for single tokens, which the
+// matrix pipe can afford: 256 bytes of cache are 32 of its cycles, 19 TB/s over the chip. The waves of a workgroup take the
+// tiles of its keys in turn and join through LDS; long caches are split over workgroups too and joined by attn_join.
+#include "attn_row.h"
+
+namespace small {
+
+namespace {
+
+extern __shared__ float token_lds[];
+
+template <int DT, int KT, int WAVES, bool VEC>
+__global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
+{
+    constexpr int VD = kVD<DT>, GR = DT / VD, NB = KT / 16, DP = DT * 16;
+    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int by_split = a.by_splits.div((int)id), split = (int)id - by_split * a.splits;
+    const int n = a.by_sets.div(by_split), set = by_split - n * a.head_sets;
+    const int r = min(m, a.rows - 1), hh = a.pack ? a.by_Sq.div(r) : 0, i = r - hh * a.Sq;
+    const int head = a.pack ? set * a.group + hh : set, key_head = a.pack ? set : a.by_group.div(set);
+    const ImageMask im(a, n);
+    const RowState row(a, im, n, i, head);
+    floatx4 q[DT];
+    {
+        const float *token = token_at(a.q, a.qs, n, i);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) q[c] = load_quad<VEC>(a, a.qs, token, head * a.D, 16 * c + 4 * g);
+    }
+    // keys up to the last one that a row can see, this workgroup's share of them in whole tiles
+    int hi = im.len;
+    if (a.causal) hi = max(0, min(hi, max(im.position(a.Sq - 1) + 1, im.prefix)));
+    const int per = ((hi + KT - 1) / KT + a.splits - 1) / a.splits * KT, begin = min(hi, split * per), end = min(hi, begin + per);
+
+    const float far_lo = a.table ? bias_gather(a, head, 0) : 0.f, far_hi = a.table ? bias_gather(a, head, 2 * a.reach) : 0.f;
+    const Scorer sc(a);
+    const float *kbase = token_at(a.k, a.ks, n, 0), *vbase = token_at(a.v, a.vs, n, 0);
+    floatx4 kx[NB][DT];
+    float vx[NB * 4][GR][VD];
+    const auto fetch_k = [&](int j0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const float *token = kbase + (long long)min(j0 + 16 * b + m, end - 1) * a.ks.token;    // (keys past the end: the last one, hidden below)
+#pragma unroll
+            for (int c = 0; c < DT; ++c) kx[b][c] = load_quad<VEC>(a, a.ks, token, key_head * a.D, 16 * c + 4 * g);
+        }
+    };
+    const auto fetch_v = [&](int j0) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float *token = vbase + (long long)min(j0 + 16 * b + 4 * g + e, end - 1) * a.vs.token;
+#pragma unroll
+                for (int grp = 0; grp < GR; ++grp) {
+                    const int d = (grp * 16 + m) * VD;
+                    float(&x)[VD] = vx[4 * b + e][grp];
+                    if constexpr (VEC && VD == 4) {
+                        const floatx4 f = load_quad<true>(a, a.vs, token, key_head * a.D, d);
+                        x[0] = f.x; x[1] = f.y; x[2] = f.z; x[3] = f.w;
+                    } else if constexpr (VEC && VD == 2) {
+                        const float2 f = d < a.D ? *reinterpret_cast<const float2 *>(token + channel_at(a, a.vs, key_head * a.D + d)) : float2{0.f, 0.f};
+                        x[0] = f.x; x[1] = f.y;
+                    } else {
+#pragma unroll
+                        for (int v = 0; v < VD; ++v) x[v] = d + v < a.D ? token[channel_at(a, a.vs, key_head * a.D + d + v)] : 0.f;
+                    }
+                }
+            }
+    };
+    floatx4 o[DT] = {};
+    float top = -kInf, sum = 0.f;
+    const int step = waves * KT;
+    int j0 = begin + wave * KT;
+    if (j0 < end) { fetch_k(j0); fetch_v(j0); }
+    for (; j0 < end; j0 += step) {
+        floatx4 s[NB] = {};
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b] = mfma(kx[b][c][e], q[c][e], s[b]);
+        if (j0 + step < end) fetch_k(j0 + step);
+        float mx = -kInf;
+        // the tile's keys all at one end of the bias's reach: most of a long cache
+        const int c0 = a.table ? code_of(a, j0) : 0, c1 = a.table ? code_of(a, j0 + KT - 1) : 0;
+        const bool all_lo = a.table && __all(c1 - row.code <= -a.reach), all_hi = a.table && __all(c0 - row.code >= a.reach);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = j0 + 16 * b + 4 * g + e;
+                float t = sc.capped(s[b][e]);
+                if (a.slopes) t = fmaf(-row.slope, fabsf((float)(row.p - j)), t);
+                if (all_lo || all_hi) t += all_lo ? far_lo : far_hi;
+                else if (a.table) t += bias_gather(a, head, offset_at(a, code_of(a, j), row.code));
+                const int doc = a.docs ? key_document(a, n, j) : row.doc;
+                t = (j < end) & row.sees(j, doc, true) ? t : -kInf;
+                s[b][e] = t;
+                mx = fmaxf(mx, t);
+            }
+        mx = fmaxf(top, column_max(mx));
+        if (__any(mx > top)) {
+            const float w = mx > top ? __builtin_amdgcn_exp2f(top - mx) : 1.f;
+            sum *= w;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= w;
+            top = mx;
+        }
+        const float at = top == -kInf ? 0.f : top;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[b][e] = __builtin_amdgcn_exp2f(s[b][e] - at);
+                sum += s[b][e];
+            }
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int grp = 0; grp < GR; ++grp)
+#pragma unroll
+                    for (int v = 0; v < VD; ++v) o[grp * VD + v] = mfma(vx[4 * b + e][grp][v], s[b][e], o[grp * VD + v]);
+        if (j0 + step < end) fetch_v(j0 + step);
+    }
+    sum = column_sum(sum);
+
+    // join the waves: [wave][row][DP] and [wave][row] (maximum, sum)
+    float *const lo_ = token_lds;
+    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * a.rows * DP);
+    int *const flags = reinterpret_cast<int *>(ml + waves * a.rows);
+    if (m < a.rows) {
+#pragma unroll
+        for (int grp = 0; grp < GR; ++grp)
+#pragma unroll
+            for (int x = 0; x < VD; ++x)
+                *reinterpret_cast<floatx4 *>(lo_ + (wave * a.rows + m) * DP + grp * 16 * VD + 4 * g * VD + 4 * x) = result_quad<DT>(o, grp, x);
+        if (g == 0) ml[wave * a.rows + m] = float2{top, sum};
+    }
+    if (threadIdx.x < 16) flags[threadIdx.x] = 0;
+    __syncthreads();
+    constexpr int QD = DP / 4;
+    for (int e = threadIdx.x; e < a.rows * QD; e += blockDim.x) {
+        const int rr = e / QD, d = (e - rr * QD) * 4;
+        float all = -kInf, total = 0.f;
+        for (int w = 0; w < waves; ++w) all = fmaxf(all, ml[w * a.rows + rr].x);
+        const float ref = all == -kInf ? 0.f : all;
+        floatx4 y = {};
+        for (int w = 0; w < waves; ++w) {
+            const float2 p = ml[w * a.rows + rr];
+            if (p.y == 0.f) continue;
+            const float f = __builtin_amdgcn_exp2f(p.x - ref);
+            total = fmaf(f, p.y, total);
+            const floatx4 z = *reinterpret_cast<const floatx4 *>(lo_ + (w * a.rows + rr) * DP + d);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) y[x] = fmaf(f, z[x], y[x]);
+        }
+        if (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w) flags[rr] = 1;
+        const int h2 = a.pack ? a.by_Sq.div(rr) : 0, i2 = rr - h2 * a.Sq, head2 = a.pack ? set * a.group + h2 : set;
+        const size_t part = (((size_t)n * a.head_sets + set) * a.rows + rr) * a.splits + split;
+        if (a.splits > 1) {
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                if (d + x < a.D) a.part_o[part * a.D + d + x] = y[x];
+            if (d == 0) a.part_ml[part] = float2{all, total};
+        } else {
+            store_quad<VEC>(a, a.os, const_cast<float *>(token_at(a.o, a.os, n, i2)), head2 * a.D, d, total == 0.f ? floatx4{} : y * (1.f / total));
+            if (a.lse && d == 0) a.lse[((size_t)n * a.heads + head2) * a.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
+        }
+    }
+    __syncthreads();
+    for (int rr = wave; rr < a.rows; rr += waves)
+        if (flags[rr]) attend_row_and_store(a, im, n, set, rr, split, begin, end);
+}
+
+}  // namespace
+
+hipError_t launch_attn_token(const AttnArgs &a, bool vec, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((long)a.N * a.head_sets * a.splits);
+    // waves of a workgroup: as many as have a tile to do each, as far as their results fit 64 KB of LDS together
+#define TOKEN(dt, kt, most) \
+    if (a.D <= 16 * dt) { \
+        const int need = ((a.Sk + kt - 1) / kt + a.splits - 1) / a.splits; \
+        int w = 1; \
+        while (w < most && w < need && 2 * w * a.rows * (16 * dt + 2) * 4 + 64 <= 65536) w *= 2; \
+        const size_t lds = (size_t)w * a.rows * (16 * dt + 2) * 4 + 64; \
+        if (vec) hipLaunchKernelGGL((attn_token<dt, kt, most, true>), dim3(grid), dim3(64 * w), lds, s, a); \
+        else hipLaunchKernelGGL((attn_token<dt, kt, most, false>), dim3(grid), dim3(64 * w), lds, s, a); \
+        return hipGetLastError(); \
+    }
+    TOKEN(1, 32, 16) TOKEN(2, 32, 16) TOKEN(3, 32, 8) TOKEN(4, 32, 8) TOKEN(5, 16, 8) TOKEN(6, 16, 8) TOKEN(8, 16, 8) TOKEN(16, 16, 4)
+#undef TOKEN
+    return hipErrorInvalidValue;
+}
+
+}  // namespace small

@@ -315,6 +315,12 @@ hipError_t launch_upsample(const float *in, float *out, int N, int C, int H, int
 hipError_t launch_group_conv(const float *in, const float *filt, float *out, const LayerGeom &g, int F_C, int S_C, int K,
                              int F_Cb, hipStream_t s);
 
+// Group normalization with an activation and its gradient (dy != null: y is din) on the blocked layout (groupnorm.hip).
+size_t groupnorm_workspace(int N, int C, int S, int Cb);
+hipError_t launch_groupnorm(const float *x, const float *gamma, const float *beta, const float *stats_in, const float *dy, float *y,
+                            float *stats, float *dgamma, float *dbeta, int N, int C, int S, int G, float eps, int act, int Cb,
+                            void *ws, hipStream_t s);
+
 // Quantized (uint8) layers (quant.hip). acc = sum over in-image taps of (x - zx)(w - zw) in int32;
 // y = clamp(zy + ((int64)acc * mult + 2^(shift-1)) >> shift, lo, hi) (no rounding term when shift == 0).
 // amax: host-derived clamp of the sum that makes the 32-bit requantization path exact (0 = not available).
