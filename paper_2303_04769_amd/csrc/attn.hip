@@ -9,7 +9,7 @@ namespace small {
 
 namespace {
 
-extern __shared__ float bias_lds_mem[];
+extern __shared__ __attribute__((aligned(16))) float bias_lds_mem[];
 
 template <int DT, int KT, bool VEC>
 __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
@@ -18,7 +18,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
     using T = Tile<DT, KT>;
     __shared__ float kt[T::kFloats], vt[T::kFloats];
     __shared__ alignas(16) int key_code[KT];
-    __shared__ alignas(16) int key_doc[KT];
+    __shared__ alignas(16) int key_doc[KT + 1];
     __shared__ int words[2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     // (image, set of heads, tile of rows, split), the rows with the most keys first; neighbours share an XCD's cache
@@ -59,6 +59,8 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
         __syncthreads();
         document_hull(a.docs + (size_t)n * a.Sk, 0, hi, d0, d1, words, &lo, &hi);
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
     int begin = lo, end = hi;
     if (a.splits > 1) {
         const int per = ((hi - lo + KT - 1) / KT + a.splits - 1) / a.splits * KT;
@@ -79,7 +81,6 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
         far_hi = bias_gather(a, head, 2 * a.reach);
     }
 
-    const Scorer sc(a);
     floatx4 o[DT] = {};
     float top = -kInf, sum = 0.f;
     floatx4 kx[T::kQuads], vx[T::kQuads];
@@ -93,11 +94,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
         __syncthreads();
         T::put(kt, kx);
         T::put(vt, vx);
-        if (threadIdx.x < KT) {
-            const int j = j0 + threadIdx.x;
-            if (a.table) key_code[threadIdx.x] = code_of(a, j);
-            if (a.docs) key_doc[threadIdx.x] = key_document(a, n, j);
-        }
+        stage_keys<KT>(a, n, j0, key_code, key_doc);
         __syncthreads();
         if (j0 + KT < end) fetch(j0 + KT);
 
@@ -111,62 +108,14 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
                 for (int e = 0; e < 4; ++e) s[b] = mfma(x[e], q[4 * c + e], s[b]);
             }
 
-        const bool edge = a.docs || !__all(j0 + KT <= row.bound);
-        const bool all_lo = a.table && __all(key_code[KT - 1] - row.code <= -a.reach), all_hi = a.table && __all(key_code[0] - row.code >= a.reach);
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[b][e] = sc.capped(s[b][e]);
-        if (a.slopes)
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] = fmaf(-row.slope, fabsf((float)(row.p - (j0 + 16 * b + 4 * g + e))), s[b][e]);
-        if (all_lo || all_hi) {
-            const float x = all_lo ? far_lo : far_hi;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] += x;
-        } else if (a.table) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                const int4 kc = *reinterpret_cast<const int4 *>(key_code + 16 * b + 4 * g);
-                const int codes[4] = {kc.x, kc.y, kc.z, kc.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = offset_at(a, codes[e], row.code);
-                    s[b][e] += bias ? bias[at] : bias_gather(a, head, at);
-                }
-            }
-        }
-        if (edge)
-#pragma unroll
-            for (int b = 0; b < NB; ++b) {
-                int docs[4] = {row.doc, row.doc, row.doc, row.doc};
-                if (a.docs) {
-                    const int4 kd = *reinterpret_cast<const int4 *>(key_doc + 16 * b + 4 * g);
-                    docs[0] = kd.x; docs[1] = kd.y; docs[2] = kd.z; docs[3] = kd.w;
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] = row.sees(j0 + 16 * b + 4 * g + e, docs[e], true) ? s[b][e] : -kInf;
-            }
+        finish_scores<7>(a, s, row, 0, reference_of(top), j0, key_code, key_doc, g, bias, far_lo, far_hi);
 
-        float mx = -kInf;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(s[b].x, s[b].y), fmaxf(s[b].z, s[b].w)));
-        mx = fmaxf(top, column_max(mx));
-        if (__any(mx > top)) {
-            const float w = mx > top ? __builtin_amdgcn_exp2f(top - mx) : 1.f;
-            sum *= w;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= w;
-            top = mx;
-        }
-        const float at = top == -kInf ? 0.f : top;
+        raise_top(s, top, sum, o);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f(s[b][e] - at);
+                s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
                 sum += s[b][e];
             }
 #pragma unroll

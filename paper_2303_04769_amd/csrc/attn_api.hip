@@ -1,7 +1,7 @@
 // C-ABI layer of the attention block (include/small_attn.h has the contract of every entry point): argument checks and sizes, host only.
 #include "../../include/small.h"
 #include "../include/small_attn.h"
-#include "attn_tile.h"
+#include "attn_parts.h"
 
 #include <initializer_list>
 
@@ -120,12 +120,14 @@ int attn_check(const small_attn &a)
     return SMALL_OK;
 }
 
-// What a call of these sizes runs: few rows against the cache, or tiles of 64 rows; and over how many workgroups a row's keys are split.
+// What a call of these sizes runs: few rows against the cache, or tiles of rows, these with fp32 products or with values in two parts; and over
+// how many workgroups a row's keys are split.
 struct AttnPlan {
-    bool token;
+    bool token, parts;
     int pack, head_sets, rows, row_tiles, splits;
-    size_t part_floats, ml_at, bytes;
+    size_t ml_at, k_at, v_at, exps_at, bytes;          // places in the workspace, in bytes
 };
+bool parts_work(const small_attn &a) { return (double)a.N * a.heads * a.Sq * a.Sk * a.D >= 1e8; }
 AttnPlan plan_attn(const small_attn &a)
 {
     AttnPlan p{};
@@ -135,17 +137,26 @@ AttnPlan plan_attn(const small_attn &a)
     p.pack = group > 1 && (p.token || a.Sq < 64);
     p.head_sets = p.pack ? a.kv_heads : a.heads;
     p.rows = (int)(p.pack ? packed : a.Sq);
+    p.parts = !p.token && !p.pack && a.D <= 128 && parts_work(a);
+    const long sets = (long)a.N * p.head_sets;
     p.row_tiles = p.token ? 1 : (p.rows + 63) / 64;
-    const long base = (long)a.N * p.head_sets * p.row_tiles;
+    const long base = sets * p.row_tiles;
     long most = p.token ? (a.Sk + 511) / 512 : (a.Sk + 255) / 256;       // keys of a part, at least
     const long want = base < 2 * cus ? (2 * cus + base - 1) / base : 1;
     p.splits = (int)(want < most ? want : most);
     if (p.splits < 1) p.splits = 1;
+    const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
     if (p.splits > 1) {
-        const size_t parts = (size_t)a.N * p.head_sets * p.rows * p.splits;
-        p.part_floats = parts * a.D;
-        p.ml_at = (p.part_floats + 63) / 64 * 64;
-        p.bytes = (p.ml_at + 2 * parts) * sizeof(float);
+        const size_t pieces = (size_t)sets * p.rows * p.splits;
+        p.ml_at = up(pieces * a.D * sizeof(float));
+        p.bytes = up(p.ml_at + pieces * sizeof(float2));
+    }
+    if (p.parts) {
+        const size_t tiles = (size_t)a.N * a.kv_heads * ((a.Sk + 63) / 64), image = tiles * parts_tile_bytes(parts_steps(a.D));
+        p.k_at = p.bytes;
+        p.v_at = p.k_at + image;
+        p.exps_at = p.v_at + image;
+        p.bytes = up(p.exps_at + 2 * tiles * sizeof(int));
     }
     return p;
 }
@@ -171,7 +182,21 @@ void place(AttnArgs &x, const AttnPlan &p, void *ws)
     x.pack = p.pack; x.head_sets = p.head_sets; x.rows = p.rows; x.row_tiles = p.row_tiles; x.splits = p.splits;
     x.by_tiles = make_fastdiv(p.row_tiles); x.by_sets = make_fastdiv(p.head_sets); x.by_splits = make_fastdiv(p.splits);
     x.part_o = (float *)ws;
-    x.part_ml = (float2 *)((float *)ws + p.ml_at);
+    x.part_ml = (float2 *)((char *)ws + p.ml_at);
+}
+
+// The images of keys and values in the workspace, and the launch that makes them.
+hipError_t make_parts(AttnArgs &x, const AttnPlan &p, const small_attn &a, void *ws, bool vec, hipStream_t s)
+{
+    const int tiles = (a.Sk + 63) / 64;
+    int *const exps = (int *)((char *)ws + p.exps_at);
+    PartsArgs args{};
+    args.count = 2;
+    args.t[0] = PartsTensor{x.k, x.ks, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.k_at, nullptr, exps, 0};
+    args.t[1] = PartsTensor{x.v, x.vs, a.kv_heads, a.Sk, tiles, 0, nullptr, (char *)ws + p.v_at, exps + (size_t)a.N * a.kv_heads * tiles, 0};
+    x.k_tok = args.t[0].by_token; x.k_exps = args.t[0].exps;
+    x.v_chan = args.t[1].by_channel; x.v_exps = args.t[1].exps;
+    return launch_make_parts(x, args, vec, s);
 }
 
 // Four channels of a head at a time: they stand together in every tensor.
@@ -193,25 +218,50 @@ size_t bias_bytes(const small_attn &a, const AttnPlan &p)
     return offsets <= kBiasLds ? (size_t)offsets * sizeof(float) : 0;
 }
 
-// The gradient's workspace: delta [N][heads][Sq], then, with a table, its sums by offset of every tile of rows and of every head.
+// Where values in two parts take a gradient call: as the forward call, and with a bias whose sums by offset fit LDS.
+bool grad_in_parts(const small_attn &a)
+{
+    return a.D <= 128 && parts_work(a) && (!a.table || a.reach < 2048);
+}
+
+// The gradient's workspace: delta [N][heads][Sq]; with a table its sums by offset, of every tile of rows and of every head; in parts the images of keys, values,
+// queries and dout, their powers of two, and dk's and dv's parts where a key tile's rows are shared out. Places in bytes.
 struct GradPlan {
-    int row_tiles, key_tiles;
-    size_t part_at, sums_at, bytes;
+    bool parts;
+    int row_tiles, key_tiles, splits, row_parts;
+    size_t part_at, sums_at, images[7], exps[4], dkv_at, bytes;
 };
 GradPlan plan_grad(const small_attn &a)
 {
     GradPlan p{};
     p.row_tiles = (a.Sq + 63) / 64;
     p.key_tiles = (a.Sk + 63) / 64;
-    const auto up = [](size_t floats) { return (floats + 63) / 64 * 64; };
-    p.part_at = p.sums_at = up((size_t)a.N * a.heads * a.Sq);
-    size_t end = p.part_at;
+    p.splits = p.row_parts = 1;
+    size_t end = 0;
+    const auto take = [&](size_t bytes) { const size_t at = end; end += (bytes + 255) / 256 * 256; return at; };
+    take((size_t)a.N * a.heads * a.Sq * sizeof(float));
     if (a.table) {
         const size_t size = 2 * (size_t)a.reach + 1;
-        p.sums_at = p.part_at + up((size_t)a.N * a.heads * p.row_tiles * size);
-        end = p.sums_at + up((size_t)a.heads * size);
+        p.part_at = take((size_t)a.N * a.heads * p.row_tiles * size * sizeof(float));
+        p.sums_at = take((size_t)a.heads * size * sizeof(float));
     }
-    p.bytes = end * sizeof(float);
+    p.parts = grad_in_parts(a);
+    if (p.parts) {
+        const size_t tile = parts_tile_bytes(parts_steps(a.D)), keys = (size_t)a.N * a.kv_heads * p.key_tiles, rows = (size_t)a.N * a.heads * p.row_tiles;
+        for (int x = 0; x < 7; ++x) p.images[x] = take((x < 3 ? keys : rows) * tile);      // k, k, v; q, q, dout, dout
+        for (int x = 0; x < 4; ++x) p.exps[x] = take((x < 2 ? keys : rows) * sizeof(int));
+        // six workgroups a compute unit: by heads that share a key head, then by rows of 256 at least
+        const long want = (6L * device_cus() + (long)keys - 1) / (long)keys;
+        const int group = a.heads / a.kv_heads;
+        int heads = 1;
+        while (heads < group && (heads < want || group % heads)) ++heads;
+        long rows_of = (want + heads - 1) / heads;
+        if (rows_of > (a.Sq + 255) / 256) rows_of = (a.Sq + 255) / 256;
+        p.row_parts = (int)(rows_of < 1 ? 1 : rows_of);
+        p.splits = heads * p.row_parts;
+        if (p.splits > 1) p.dkv_at = take((size_t)p.splits * a.N * a.kv_heads * a.Sk * 2 * a.D * sizeof(float));
+    }
+    p.bytes = end;
     return p;
 }
 bool grad_vec(const small_attn &a)
@@ -262,9 +312,13 @@ int small_attention(const small_attn *a, const float *q, const float *k, const f
     x.lse = lse;
     place(x, p, workspace);
     const bool vec = attn_vec(*a, {q, k, v, out});
+    x.vec = vec;
     const size_t bias = p.token ? 0 : bias_bytes(*a, p);
     x.bias_lds = bias != 0;
-    hipError_t e = p.token ? launch_attn_token(x, vec, (hipStream_t)stream) : launch_attn_rows(x, vec, bias, (hipStream_t)stream);
+    hipError_t e = p.parts ? make_parts(x, p, *a, workspace, vec, (hipStream_t)stream) : hipSuccess;
+    if (e == hipSuccess)
+        e = p.token ? launch_attn_token(x, vec, (hipStream_t)stream)
+            : p.parts ? launch_attn_rows_parts(x, bias, (hipStream_t)stream) : launch_attn_rows(x, vec, bias, (hipStream_t)stream);
     if (e == hipSuccess && p.splits > 1) e = launch_attn_join(x, (hipStream_t)stream);
     return from_hip(e);
 }
@@ -300,18 +354,42 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     AttnArgs x = attn_args(*a, q, k, v, out);
     x.lse_in = lse; x.dout = dout; x.dq = dq; x.dk = dk; x.dv = dv;
     x.dos = strides(a->dout); x.dqs = strides(a->dq); x.dks = strides(a->dk); x.dvs = strides(a->dv);
-    x.row_tiles = p.row_tiles; x.key_tiles = p.key_tiles;
+    x.row_tiles = p.row_tiles; x.key_tiles = p.key_tiles; x.splits = p.splits; x.row_parts = p.row_parts;
     x.by_tiles = make_fastdiv(p.row_tiles); x.by_key_tiles = make_fastdiv(p.key_tiles); x.by_heads = make_fastdiv(a->heads);
+    x.by_sets = make_fastdiv(a->kv_heads); x.by_splits = make_fastdiv(p.splits);
     x.by_code = make_fastdiv(2 * a->width - 1);
-    x.delta = (float *)workspace;
-    x.part_bias = dtable ? (float *)workspace + p.part_at : nullptr;
-    const bool vec = attn_vec(*a, {q, k, v, out, dout, dq, dk, dv}) && grad_vec(*a);
+    char *const at = (char *)workspace;
+    x.delta = (float *)at;
+    x.part_bias = dtable ? (float *)(at + p.part_at) : nullptr;
+    x.vec = attn_vec(*a, {q, k, v, out, dout, dq, dk, dv}) && grad_vec(*a);
     const double size = 2.0 * a->reach + 1;
     x.bias_lds = a->table && size <= kBiasLds;
     x.bias_acc_lds = dtable && size <= kBiasLds;
-    hipError_t e = launch_attn_grad_rows(x, vec, (hipStream_t)stream);
-    if (e == hipSuccess) e = launch_attn_grad_keys(x, vec, (hipStream_t)stream);
-    if (e == hipSuccess && dtable) e = launch_attn_grad_bias(x, (float *)workspace + p.sums_at, dtable, (hipStream_t)stream);
+    // sets of sums by offset, 16, 8 or 4: as many as leave two workgroups a compute unit
+    x.bias_copies = 16;
+    while (x.bias_copies > 4 && 3 * parts_tile_bytes(parts_steps(a->D)) + 4 * size * (x.bias_copies + 1) > 79000) x.bias_copies /= 2;
+    const hipStream_t s = (hipStream_t)stream;
+    hipError_t e;
+    if (p.parts) {
+        int *const exps[] = {(int *)(at + p.exps[0]), (int *)(at + p.exps[1]), (int *)(at + p.exps[2]), (int *)(at + p.exps[3])};
+        PartsArgs args{};
+        args.count = 4;
+        args.t[0] = PartsTensor{k, x.ks, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[0], at + p.images[1], exps[0], 0};
+        args.t[1] = PartsTensor{v, x.vs, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[2], nullptr, exps[1], 0};
+        args.t[2] = PartsTensor{q, x.qs, a->heads, a->Sq, p.row_tiles, 1, at + p.images[3], at + p.images[4], exps[2], 0};
+        args.t[3] = PartsTensor{dout, x.dos, a->heads, a->Sq, p.row_tiles, 1, at + p.images[5], at + p.images[6], exps[3], 0};
+        x.k_tok = at + p.images[0]; x.k_chan = at + p.images[1]; x.v_tok = at + p.images[2];
+        x.q_tok = at + p.images[3]; x.q_chan = at + p.images[4]; x.do_tok = at + p.images[5]; x.do_chan = at + p.images[6];
+        x.k_exps = exps[0]; x.v_exps = exps[1]; x.q_exps = exps[2]; x.do_exps = exps[3];
+        x.part_o = (float *)(at + p.dkv_at);
+        e = launch_make_parts(x, args, x.vec, s);
+        if (e == hipSuccess) e = launch_attn_grad_rows_parts(x, s);
+        if (e == hipSuccess) e = launch_attn_grad_keys_parts(x, s);
+    } else {
+        e = launch_attn_grad_rows(x, x.vec, s);
+        if (e == hipSuccess) e = launch_attn_grad_keys(x, x.vec, s);
+    }
+    if (e == hipSuccess && dtable) e = launch_attn_grad_bias(x, (float *)(at + p.sums_at), dtable, s);
     return from_hip(e);
 }
 

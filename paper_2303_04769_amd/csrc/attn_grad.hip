@@ -12,7 +12,7 @@ namespace small {
 
 namespace {
 
-extern __shared__ float grad_lds[];
+extern __shared__ __attribute__((aligned(16))) float grad_lds[];
 
 // A score's way to its probability: capped (returned as tanh, or as the dot product where there is no cap), biased.
 __device__ __forceinline__ float score_core(const AttnArgs &a, const Scorer &sc, float dot) { return a.cap > 0.f ? tanh_of(dot * sc.cap_in) : dot; }

@@ -1,0 +1,93 @@
+// Attention on the fp16 matrix instructions with values in two parts (attn_parts.hip, attn_parts_grad.hip).
+//
+// x = hi + lo with hi = fp16(x), lo = fp16(x - hi) keeps x to 2^-22 of its size, and the products hi hi, hi lo, lo hi, summed in fp32, keep a
+// product to some 2^-21.5: sums of D or more of them come out as near to 64 bits as those of fp32 instructions, whose every addition rounds (errors
+// of both are in the tests and in the measured cases). Three v_mfma_f32_16x16x32_f16 of 16 cycles do what eight
+// v_mfma_f32_16x16x4_f32 of 32 do: 5.3 times the rate.
+//
+// fp16 has little range, so values carry a power of two: one for each tile of 64 tokens of a head (its largest magnitude comes to lie in
+// [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-25 times the tile's largest still has 22 bits, and below that the error is
+// 2^-35 of the largest one. Magnitudes beyond fp32's own range apart, no input is out of reach; infinities and NaN become NaN.
+//
+// attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, lane l = 16 g + m with its eight values behind each other,
+// so a wave reads an operand as one linear kilobyte, and copies of tiles into LDS are linear too:
+//   tokens in lanes   [16 tokens][32 channels][part]: lane (m, g) holds channels 8g .. 8g+7 of token m
+//   channels in lanes [32 tokens][16 channels][part]: lane (m, g) holds tokens 4g .. 4g+3 and 16+4g .. 16+4g+3 of channel m -- the order in
+//                     which two results of 16 tokens each lie in a lane's registers, which are the other operand of that product.
+#pragma once
+#include "attn_row.h"
+
+namespace small {
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half4 __attribute__((ext_vector_type(4)));
+
+constexpr int kTop = 10;                       // exponent of a tile's or row's largest value
+constexpr int kLift = 8;                       // of weights: with kSlack below 2^15
+
+__device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+
+// c += a b for operands in two parts, the small products first.
+__device__ __forceinline__ floatx4 mfma_parts(half8 a_hi, half8 a_lo, half8 b_hi, half8 b_lo, floatx4 c)
+{
+    c = mfma16(a_lo, b_hi, c);
+    c = mfma16(a_hi, b_lo, c);
+    return mfma16(a_hi, b_hi, c);
+}
+
+typedef _Float16 half2v __attribute__((ext_vector_type(2)));
+typedef float float2v __attribute__((ext_vector_type(2)));
+typedef unsigned uintx4v __attribute__((ext_vector_type(4)));
+
+// Two values into half a register's worth of parts each.
+__device__ __forceinline__ void split_pair(float x, float y, unsigned &hi, unsigned &lo)
+{
+    const half2v h = __builtin_convertvector((float2v{x, y}), half2v), l = {(_Float16)fmaf((float)h.x, -1.f, x), (_Float16)fmaf((float)h.y, -1.f, y)};
+    hi = __builtin_bit_cast(unsigned, h);
+    lo = __builtin_bit_cast(unsigned, l);
+}
+// Results of 32 tokens (two of 16) of a lane's column as a right operand in two parts.
+__device__ __forceinline__ void split_results(const floatx4 &first, const floatx4 &second, half8 &hi, half8 &lo)
+{
+    uintx4v h, l;
+    unsigned x, y;
+    split_pair(first.x, first.y, x, y); h.x = x; l.x = y;
+    split_pair(first.z, first.w, x, y); h.y = x; l.y = y;
+    split_pair(second.x, second.y, x, y); h.z = x; l.z = y;
+    split_pair(second.z, second.w, x, y); h.w = x; l.w = y;
+    hi = __builtin_bit_cast(half8, h);
+    lo = __builtin_bit_cast(half8, l);
+}
+
+// Power of two e such that a magnitude `most` times 2^-e lies in [2^kTop, 2^(kTop + 1)); nothing but zeros: a small one.
+__device__ __forceinline__ int parts_exponent(float most)
+{
+    if (most == 0.f) return -100;
+    const int e = (int)(__float_as_uint(most) >> 23) - 127 - kTop;
+    return max(e, -100);
+}
+__device__ __forceinline__ float finite_magnitude(float x) { return fabsf(x) < kInf ? fabsf(x) : 0.f; }
+
+struct PartsTensor {
+    const float *p;
+    TokenStrides s;
+    int heads, tokens, tiles, rows;            // rows: not keys but queries (their masks: rows of lse = -inf are left out)
+    char *by_token, *by_channel;               // images, or null
+    int *exps;                                 // [N * heads][tiles]
+    unsigned first_block;
+};
+struct PartsArgs {
+    PartsTensor t[4];
+    int count;
+};
+
+constexpr size_t parts_tile_bytes(int steps) { return (size_t)64 * 32 * steps * 4; }
+constexpr int parts_steps(int D) { return (D + 31) / 32; }
+
+// attn_parts.hip
+hipError_t launch_make_parts(const AttnArgs &a, PartsArgs &args, bool vec, hipStream_t s);
+hipError_t launch_attn_grad_rows_parts(const AttnArgs &a, hipStream_t s);        // attn_parts_grad.hip
+hipError_t launch_attn_grad_keys_parts(const AttnArgs &a, hipStream_t s);
+hipError_t launch_attn_rows_parts(const AttnArgs &a, size_t bias_bytes, hipStream_t s);
+
+}  // namespace small

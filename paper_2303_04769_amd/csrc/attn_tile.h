@@ -30,20 +30,35 @@ struct AttnArgs {
     int pack;                     // a workgroup's rows run over the query heads of one key head (few queries, shared heads)
     int head_sets, rows;          // heads / group sets of group * Sq rows, or heads of Sq
     int splits, bias_lds;         // bias_lds: heads whose expanded bias fits LDS (0: gathered from memory)
-    int row_tiles;
+    int row_tiles, vec;           // vec: four channels of a head stand together and aligned in every tensor
     FastDiv by_Cb, by_Sq, by_width, by_tiles, by_sets, by_splits, by_group;
     float *part_o;
     float2 *part_ml;              // splits > 1: results before joining, and their (maximum, sum)
+    // values in two parts (attn_parts.h): images of keys and values, their powers of two
+    const char *k_tok, *k_chan, *v_tok, *v_chan, *q_tok, *q_chan, *do_tok, *do_chan;
+    const int *k_exps, *v_exps, *q_exps, *do_exps;
     // gradient
     const float *dout, *lse_in;
     float *dq, *dk, *dv, *delta, *part_bias;                 // part_bias: null, or [N * heads * row_tiles][2 reach + 1]
     TokenStrides dos, dqs, dks, dvs;
-    int key_tiles, bias_acc_lds;
+    int key_tiles, bias_acc_lds, bias_copies, row_parts;
     FastDiv by_key_tiles, by_code, by_heads;                 // by_code: 2 width - 1
 };
 
+// The kernel's arguments read anew from where they are passed: what only a kernel's end needs would otherwise be kept in scalar registers, and spilled from
+// them, all the way through its loop.
+__device__ __forceinline__ AttnArgs late_args()
+{
+    auto at = (const __attribute__((address_space(4))) unsigned *)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(at));
+    unsigned words[sizeof(AttnArgs) / 4];
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(AttnArgs) / 4; ++i) words[i] = at[i];
+    return __builtin_bit_cast(AttnArgs, words);
+}
+
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
-constexpr int kFar = 1 << 28;     // positions are taken into -kFar .. kFar: differences of their numbers fit an int
+constexpr int kFar = 1 << 28;     // first positions are taken into -kFar .. kFar: differences of positions' numbers fit an int
 constexpr float kInf = __builtin_huge_valf();
 
 __device__ __forceinline__ const float *token_at(const float *p, const TokenStrides &s, int n, long long t)
@@ -108,13 +123,14 @@ struct ImageMask {
         prefix = a.prefix ? min(a.prefix[n], a.Sk) : 0;
         first = a.first ? max(-kFar, min(a.first[n], kFar)) : a.Sk - a.Sq;
     }
-    __device__ __forceinline__ int position(int i) const { return max(-kFar, min(first + i, kFar)); }
+    __device__ __forceinline__ int position(int i) const { return first + i; }
 };
 
 // What a query needs besides its channels. It sees the keys in front of `bound` -- of its document, if there are documents.
 struct RowState {
     int p, code, bound, doc, head;
     float slope;                  // times log2(e)
+    RowState() = default;
     __device__ __forceinline__ RowState(const AttnArgs &a, const ImageMask &im, int n, int i, int h)
     {
         p = im.position(i);
@@ -139,12 +155,35 @@ __device__ __forceinline__ float tanh_of(float x)
 {
     const float y = x * x;
     const float n = fmaf(y, fmaf(y, y + 378.f, 17325.f), 135135.f), d = fmaf(y, fmaf(y, fmaf(y, 28.f, 3150.f), 62370.f), 135135.f);
-    float r = x * n * __builtin_amdgcn_rcpf(d);
-    if (fabsf(x) > 2.f) {
-        const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
-        r = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x);
-    }
+    const float e = __builtin_amdgcn_exp2f(fabsf(x) * (2.f * kLog2e));
+    const float r = fabsf(x) > 2.f ? copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x) : x * n * __builtin_amdgcn_rcpf(d);
     return r;
+}
+
+// The same for |x| <= 0.6, a polynomial fitted at Chebyshev points (relative error 2.5e-9 before rounding): capped scores are mostly small against
+// their cap, and this takes no reciprocal.
+__device__ __forceinline__ float tanh_small(float x)
+{
+    const float y = x * x;
+    return x * fmaf(y, fmaf(y, fmaf(y, fmaf(y, fmaf(y, -0.00585642783f, 0.0207574759f), -0.05376992f), 0.133317053f), -0.333332837f), 1.f);
+}
+template <int NB>
+__device__ __forceinline__ void tanh_all(floatx4 (&s)[NB])
+{
+    float most = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) most = fmaxf(most, fmaxf(fmaxf(fabsf(s[b].x), fabsf(s[b].y)), fmaxf(fabsf(s[b].z), fabsf(s[b].w))));
+    if (__any(most > 0.6f)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][e] = tanh_of(s[b][e]);
+    } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][e] = tanh_small(s[b][e]);
+    }
 }
 
 // A bias in units of log2. One of about the type's lowest value hides its offsets as minus infinity does: a sum of weights of scores of that size
@@ -154,6 +193,12 @@ __device__ __forceinline__ float bias_gather(const AttnArgs &a, int head, int at
 {
     const int b = max(0, min(a.bucket[at], a.buckets - 1));
     return bias_log2(a.table[(size_t)head * a.buckets + b]);
+}
+// A head's biases by offset into LDS, by the whole workgroup (of 256).
+__device__ __forceinline__ void expand_bias(const AttnArgs &a, int head, float *lds)
+{
+#pragma unroll 4
+    for (int x = threadIdx.x; x <= 2 * a.reach; x += 256) lds[x] = bias_gather(a, head, x);
 }
 __device__ __forceinline__ int offset_at(const AttnArgs &a, int key_code, int code) { return max(-a.reach, min(key_code - code, a.reach)) + a.reach; }
 
@@ -179,6 +224,97 @@ struct Scorer {
         return t;
     }
 };
+
+// A lane's scores from its dot products (which stand for 2^-dot_exp of what they are), in units of log2 and relative to `ref`, of the keys j0 + 16b + 4g + e
+// of a tile whose numbers and documents are in LDS (key_doc[16 NB]: the document of all of them, or -3); hidden keys get minus infinity. bias: the head's expanded
+// bias in LDS, or null; far_lo, far_hi: its ends. A score is one operation where there is neither cap nor bias, so `ref` costs nothing.
+// MODE: which of cap (1), distances (2) and table (4) there may be at all; what a kernel is compiled without costs it no registers.
+template <int MODE, int NB>
+__device__ __forceinline__ void finish_scores(const AttnArgs &a, floatx4 (&s)[NB], const RowState &row, int dot_exp, float ref, int j0, const int *key_code, const int *key_doc,
+                                              int g, const float *bias, float far_lo, float far_hi, floatx4 *core = nullptr)       // core: gets tanh, where there is a cap
+{
+    const bool capped = (MODE & 1) && a.cap > 0.f, slopes = (MODE & 2) && a.slopes, table = (MODE & 4) && a.table;
+    float in = ldexpf(capped ? a.scale / a.cap : a.scale * kLog2e, dot_exp), base = -ref;
+    if (capped) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] *= in;
+        tanh_all(s);
+        if (core)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) core[b] = s[b];
+        in = a.cap * kLog2e;
+    }
+    bool near = false;
+    if (table) {
+        const bool all_lo = __all(key_code[16 * NB - 1] - row.code <= -a.reach), all_hi = __all(key_code[0] - row.code >= a.reach);
+        near = !all_lo && !all_hi;
+        base += all_lo ? far_lo : all_hi ? far_hi : 0.f;
+    }
+    if (slopes) {
+        const float from = (float)(j0 + 4 * g - row.p);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, fmaf(-row.slope, fabsf(from + (float)(16 * b + e)), base));
+    } else {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, base);
+    }
+    if (near) {
+        if (bias) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int4 kc = *reinterpret_cast<const int4 *>(key_code + 16 * b + 4 * g);
+                s[b].x += bias[offset_at(a, kc.x, row.code)];
+                s[b].y += bias[offset_at(a, kc.y, row.code)];
+                s[b].z += bias[offset_at(a, kc.z, row.code)];
+                s[b].w += bias[offset_at(a, kc.w, row.code)];
+            }
+        } else {
+#pragma unroll 1
+            for (int x = 0; x < 4 * NB; ++x) {
+                const float y = bias_gather(a, row.head, offset_at(a, key_code[16 * (x >> 2) + 4 * g + (x & 3)], row.code));
+#pragma unroll
+                for (int b = 0; b < NB; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] += x == 4 * b + e ? y : 0.f;
+            }
+        }
+    }
+    if (!__all(j0 + 16 * NB <= row.bound)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[b][e] = j0 + 16 * b + 4 * g + e < row.bound ? s[b][e] : -kInf;
+    }
+    if (a.docs && !__all(key_doc[16 * NB] == row.doc)) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int4 kd = *reinterpret_cast<const int4 *>(key_doc + 16 * b + 4 * g);
+            s[b].x = kd.x == row.doc ? s[b].x : -kInf;
+            s[b].y = kd.y == row.doc ? s[b].y : -kInf;
+            s[b].z = kd.z == row.doc ? s[b].z : -kInf;
+            s[b].w = kd.w == row.doc ? s[b].w : -kInf;
+        }
+    }
+}
+
+// Numbers and documents of a tile's KT keys into LDS, by the first KT threads of the workgroup; key_doc[KT]: the document of all of them, or -3.
+template <int KT>
+__device__ __forceinline__ void stage_keys(const AttnArgs &a, int n, int j0, int *key_code, int *key_doc)
+{
+    if (threadIdx.x >= KT) return;
+    const int j = j0 + threadIdx.x;
+    if (a.table) key_code[threadIdx.x] = code_of(a, j);
+    if (a.docs) {
+        const int doc = key_document(a, n, j), first = __builtin_amdgcn_readfirstlane(doc);
+        key_doc[threadIdx.x] = doc;
+        if (threadIdx.x == 0) key_doc[KT] = -3;
+        if (__all(doc == first)) key_doc[KT] = first;
+    }
+}
 
 // A tile of KT tokens in LDS: [channels / 16][token][16], chunks 16 floats further apart than they are long, so that the four chunks that a
 // wave reads of one token are in different banks.
@@ -226,16 +362,39 @@ struct Tile {
     }
 };
 
-// The largest of a lane's value over the four lanes of its column, and the sum.
-__device__ __forceinline__ float column_max(float v)
+// The largest of a lane's value over the four lanes of its column, and the sum, by swaps of lanes (a shuffle is a trip through LDS).
+template <typename F>
+__device__ __forceinline__ float over_column(float v, F f)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
+    const auto h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    const unsigned w = __float_as_uint(f(__uint_as_float(h[0]), __uint_as_float(h[1])));
+    const auto r = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
-__device__ __forceinline__ float column_sum(float v)
+__device__ __forceinline__ float column_max(float v) { return over_column(v, [](float x, float y) { return fmaxf(x, y); }); }
+__device__ __forceinline__ float column_sum(float v) { return over_column(v, [](float x, float y) { return x + y; }); }
+
+// A row's reference, against which its weights are taken (the same in the four lanes of its column): a score that it had, or minus infinity so far. It is
+// taken anew only where a score passes it by more than kSlack: weights are then at most 2^kSlack, and most tiles need no exchange between lanes and rescale
+// nothing. Scores s come relative to `reference_of(top)` and leave relative to the new one.
+constexpr float kSlack = 6.f;
+__device__ __forceinline__ float reference_of(float top) { return top == -kInf ? 0.f : top; }
+template <int NB, int DT>
+__device__ __forceinline__ void raise_top(floatx4 (&s)[NB], float &top, float &sum, floatx4 (&o)[DT], float lift = 0.f)      // (s: `lift` more than that)
 {
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    float mx = -kInf;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(s[b].x, s[b].y), fmaxf(s[b].z, s[b].w)));
+    if (!__any(mx > (top == -kInf ? -kInf : kSlack + lift))) return;
+    mx = column_max(mx) - lift;
+    const float by = top == -kInf ? (mx == -kInf ? 0.f : mx) : fmaxf(mx, 0.f);       // (a lower reference is never taken)
+    const float w = top == -kInf ? 1.f : __builtin_amdgcn_exp2f(-by);                // (nothing was summed so far)
+    top = top == -kInf ? mx : top + by;
+    sum *= w;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) o[d] *= w;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) s[b] -= by;
 }
 
 // 4 VD neighbouring channels of a lane's column from result tiles grp * VD .. : quad x of them.
@@ -284,6 +443,7 @@ hipError_t launch_lds(K *kernel, unsigned grid, size_t lds, const AttnArgs &a, h
 }
 
 // attn.hip, attn_token.hip, attn_grad.hip
+inline int attn_mode(const AttnArgs &a) { return (a.cap > 0.f ? 1 : 0) | (a.slopes ? 2 : 0) | (a.table ? 4 : 0); }
 hipError_t launch_attn_rows(const AttnArgs &a, bool vec, size_t bias_bytes, hipStream_t s);
 hipError_t launch_attn_join(const AttnArgs &a, hipStream_t s);
 hipError_t launch_attn_grad_rows(const AttnArgs &a, bool vec, hipStream_t s);

@@ -10,7 +10,7 @@ namespace small {
 
 namespace {
 
-extern __shared__ float token_lds[];
+extern __shared__ __attribute__((aligned(16))) float token_lds[];
 
 template <int DT, int KT, int WAVES, bool VEC>
 __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
@@ -85,7 +85,6 @@ __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b] = mfma(kx[b][c][e], q[c][e], s[b]);
         if (j0 + step < end) fetch_k(j0 + step);
-        float mx = -kInf;
         // the tile's keys all at one end of the bias's reach: most of a long cache
         const int c0 = a.table ? code_of(a, j0) : 0, c1 = a.table ? code_of(a, j0 + KT - 1) : 0;
         const bool all_lo = a.table && __all(c1 - row.code <= -a.reach), all_hi = a.table && __all(c0 - row.code >= a.reach);
@@ -94,29 +93,20 @@ __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int j = j0 + 16 * b + 4 * g + e;
-                float t = sc.capped(s[b][e]);
+                float t = sc.capped(s[b][e]) - reference_of(top);
                 if (a.slopes) t = fmaf(-row.slope, fabsf((float)(row.p - j)), t);
                 if (all_lo || all_hi) t += all_lo ? far_lo : far_hi;
                 else if (a.table) t += bias_gather(a, head, offset_at(a, code_of(a, j), row.code));
                 const int doc = a.docs ? key_document(a, n, j) : row.doc;
-                t = (j < end) & row.sees(j, doc, true) ? t : -kInf;
+                t = ((j < end) & row.sees(j, doc, true)) ? t : -kInf;
                 s[b][e] = t;
-                mx = fmaxf(mx, t);
             }
-        mx = fmaxf(top, column_max(mx));
-        if (__any(mx > top)) {
-            const float w = mx > top ? __builtin_amdgcn_exp2f(top - mx) : 1.f;
-            sum *= w;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] *= w;
-            top = mx;
-        }
-        const float at = top == -kInf ? 0.f : top;
+        raise_top(s, top, sum, o);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f(s[b][e] - at);
+                s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
                 sum += s[b][e];
             }
 #pragma unroll

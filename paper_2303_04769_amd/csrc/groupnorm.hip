@@ -85,7 +85,7 @@ __device__ __forceinline__ void segment_sums(int n, int count, int lanes, F f, O
     }
 }
 
-extern __shared__ float norm_lds[];
+extern __shared__ __attribute__((aligned(16))) float norm_lds[];
 
 // One workgroup, one unit of U channels of one image; K rows of VEC channels in a thread's registers.
 // LDS: red[RP][U], then the groups' sums.

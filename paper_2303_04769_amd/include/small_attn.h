@@ -69,8 +69,8 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
  * A row that sees no key, or only keys of score -inf, gives out = 0 and lse = -inf. Keys at and beyond an image's length are never
  * read and may hold anything; neither does what a key hidden by another mask holds reach a row that does not see it.
  *
- * All of lengths, first, prefix, docs, slopes, table and bucket are DEVICE pointers. Limits: D <= 256; Sq, Sk <= 2^28, positions are taken
- * into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31. Tensors may be larger than 2^31 values.
+ * All of lengths, first, prefix, docs, slopes, table and bucket are DEVICE pointers. Limits: D <= 256; Sq, Sk <= 2^28, first positions are
+ * taken into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31. Tensors may be larger than 2^31 values.
  * lse may be NULL in the forward call. small_attention_workspace (host only): bytes for a forward call (grad = 0) or a gradient call (grad = 1),
  * 256-byte aligned (0 is possible: then it may be NULL).
  *

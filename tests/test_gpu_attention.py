@@ -341,6 +341,59 @@ def test_attention_and_its_gradient(name):
     Case(**CASES[name]).check()
 
 
+# Sizes that are computed with values in two parts (10^8 multiply-adds a product and more).
+LARGE = {
+    "plain": dict(Sq=640, heads=4, D=64), "odd": dict(Sq=651, heads=4, D=64, Cb=8), "rows and keys of unlike number": dict(Sq=130, Sk=3100, heads=4, D=64),
+    "causal, shared": dict(Sq=660, heads=8, kv=2, D=32, causal=True), "causal, distances": dict(Sq=700, heads=4, D=64, causal=True, slopes=True),
+    "prefix, capped, buckets": dict(N=2, Sq=460, heads=4, kv=2, D=64, causal=True, prefix=[100, 321], cap=4.0, bias="log"),
+    "lengths": dict(N=4, Sq=333, heads=4, D=64, lengths=[0, 1, 64, 333]), "documents": dict(N=2, Sq=500, heads=4, D=64, docs=_docs(2, 500, [[3, 60, 70, 300], [250, 250]])),
+    "documents out of order": dict(N=1, Sq=700, heads=4, D=64, docs=[[(7 * i) % 4 - (i % 9 == 0) for i in range(700)]]),
+    "positions of their own": dict(N=3, Sq=400, heads=4, D=64, causal=True, first=[-100, 50, 390], bias="log"),
+    "pixels": dict(N=1, Sq=660, heads=4, D=64, bias=(20, 33)), "pixels, wide rows": dict(N=1, Sq=640, heads=4, D=64, bias=(2, 320)), "buckets": dict(Sq=651, heads=4, D=64, bias="log"),
+    "buckets too many for LDS": dict(Sq=640, heads=4, D=64, bias="wide"), "heads of 16": dict(Sq=1300, heads=4, D=16, bias="log"), "heads of 8": dict(Sq=1300, heads=8, D=8),
+    "heads of 40": dict(Sq=800, heads=4, D=40, Cb=8, bias="log", causal=True), "heads of 37": dict(Sq=850, heads=4, D=37, Cb=37), "heads of 80": dict(Sq=600, heads=4, D=80),
+    "heads of 96": dict(Sq=540, heads=4, D=96, bias="log"), "heads of 128": dict(Sq=480, heads=4, D=128, causal=True, slopes=True, cap=9.0), "channels last": dict(Sq=640, heads=4, D=64, Cb=256),
+    "few rows": dict(Sq=70, Sk=12000, heads=2, D=64, bias="log"), "everything": dict(N=3, Sq=400, cap=10.0, bias="log", slopes=True, causal=True, prefix=[50, 0, 300],
+        lengths=[400, 64, 290], docs=_docs(3, 400, [[150, 235], [400], [10, 10, 370]]), heads=6, kv=3, D=48),
+}
+
+
+@pytest.mark.parametrize("name", LARGE)
+def test_attention_and_its_gradient_in_parts(name):
+    Case(**LARGE[name]).check()
+
+
+@pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** 30])
+def test_parts_carry_any_magnitude(size):
+    """Tensors far from one in size, and tokens of very different sizes beside each other: fp16 alone holds neither."""
+    c = Case(Sq=640, heads=4, D=64)
+    c.k, c.v, c.dout, c.scale = c.k * size, c.v * size, c.dout / size, c.scale / size
+    c.check()
+    c = Case(Sq=640, heads=4, D=64)
+    steps = 2.0 ** (torch.arange(640) // 40 - 8)
+    c.v, c.dout = c.v * steps, c.dout * steps.flip(0)
+    c.check()
+
+
+def test_parts_leave_what_masked_places_hold():
+    """As for small sizes: NaN and infinities past lengths, in other documents, behind a causal row."""
+    shape = dict(Sq=640, heads=4, D=64)
+    c = Case(lengths=[600], **shape)
+    want, lse = c.ref()
+    c.k[0, :, 600:], c.v[0, :, 600:] = float("nan"), float("inf")
+    o, l = c.forward()
+    assert_near(plain(o), want, 704, "out past the length")
+    assert_near(l, lse, 704, "lse past the length")
+    for masks in (dict(causal=True), dict(docs=_docs(1, 640, [[500, 140]]))):
+        want, lse = Case(**shape, **masks).ref()
+        c = Case(**shape, **masks)
+        c.v[0, 5, 510], c.k[0, :, 511] = float("inf"), float("nan")
+        o, l = c.forward()
+        assert_near(plain(o)[:, :, :500], want[:, :, :500], 704, "out in front")
+        assert_near(l[:, :, :500], lse[:, :, :500], 704, "lse in front")
+        assert not torch.isfinite(plain(o)[0, 5, 512:]).any()
+
+
 TOKENS = {
     "one stream": dict(Sk=777, heads=8, D=32), "one key": dict(N=2, Sk=1), "a tile and a key": dict(N=2, Sk=33, D=64),
     "long": dict(N=1, Sk=5000, heads=2, D=64, bias="log"), "long, shared heads": dict(N=2, Sk=3001, heads=16, kv=1, D=128),
