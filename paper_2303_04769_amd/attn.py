@@ -59,6 +59,19 @@ def load():
     return _lib
 
 
+_fastcall = None
+
+
+def _fast():
+    """The extension's calls (binding._fast), told once what an attention plan's record is."""
+    global _fastcall
+    if _fastcall is None:
+        fast = B._fast()
+        fast.bind_attention(small_attn)
+        _fastcall = fast
+    return _fastcall
+
+
 def _bytes(t):
     """Device pointer and size of a workspace tensor."""
     return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
@@ -71,12 +84,18 @@ def small_groupnorm_workspace(N, Cc, H, W, G, Cb):
 
 
 def small_groupnorm(inp, gamma, beta, out, stats, N, Cc, H, W, G, eps, act, Cb, workspace, stream=None):
+    rc = _fast().groupnorm(inp, gamma, beta, out, stats, N, Cc, H, W, G, eps, act, Cb, workspace, None) if stream is None else None
+    if rc is not None:
+        return B._check(rc, "small_groupnorm")
     ws, size = _bytes(workspace)
     B._check(load().small_groupnorm(B._ptr(inp), B._ptr(gamma), B._ptr(beta), B._ptr(out), B._ptr(stats), N, Cc, H, W, G, eps, act, Cb,
                                     ws, size, B._stream(stream)), "small_groupnorm")
 
 
 def small_groupnorm_grad(inp, gamma, beta, stats, dout, din, dgamma, dbeta, N, Cc, H, W, G, act, Cb, workspace, stream=None):
+    rc = _fast().groupnorm_grad(inp, gamma, beta, stats, dout, din, dgamma, dbeta, N, Cc, H, W, G, act, Cb, workspace, None) if stream is None else None
+    if rc is not None:
+        return B._check(rc, "small_groupnorm_grad")
     ws, size = _bytes(workspace)
     B._check(load().small_groupnorm_grad(B._ptr(inp), B._ptr(gamma), B._ptr(beta), B._ptr(stats), B._ptr(dout), B._ptr(din),
                                          B._ptr(dgamma), B._ptr(dbeta), N, Cc, H, W, G, act, Cb, ws, size, B._stream(stream)),
@@ -162,9 +181,14 @@ class Attention:
         r.table, r.bucket = _floats(table, (r.heads, r.buckets)), _ints(bucket, (2 * r.reach + 1,))
 
     def _space(self, grad):
+        """Workspace of the forward or the gradient call, enough for calls with a table and without."""
         if grad not in self._workspace:
-            n = small_attention_workspace(self.record, grad)
-            self._workspace[grad] = torch.empty(n, dtype=torch.uint8, device=self.device) if n else None
+            r = small_attn.from_buffer_copy(self.record)
+            sizes = []
+            for there in (None, 256)[:2 if r.buckets else 1]:         # (a table is only looked at for being there)
+                r.table = r.bucket = there
+                sizes.append(small_attention_workspace(r, grad))
+            self._workspace[grad] = torch.empty(max(sizes), dtype=torch.uint8, device=self.device) if max(sizes) else None
         return self._workspace[grad]
 
     def _blocks(self, t, heads, S):
@@ -176,6 +200,10 @@ class Attention:
 
     def run(self, q, k, v, out, lse=None, lengths=None, first=None, prefix=None, docs=None, slopes=None, table=None, bucket=None, stream=None):
         r = self.record
+        if stream is None:
+            rc = _fast().attention(r, q, k, v, out, lse, self._space(0), lengths, first, prefix, docs, slopes, table, bucket, None)
+            if rc is not None:
+                return B._check(rc, "small_attention")
         self._fill(lengths, first, prefix, docs, slopes, table, bucket)
         pq, r.q = self._blocks(q, r.heads, r.Sq)
         pk, r.k = self._blocks(k, r.kv_heads, r.Sk)
@@ -188,6 +216,11 @@ class Attention:
     def grad(self, q, k, v, out, lse, dout, dq, dk, dv, dtable=None, lengths=None, first=None, prefix=None, docs=None, slopes=None,
              table=None, bucket=None, stream=None):
         r = self.record
+        if stream is None:
+            rc = _fast().attention_grad(r, q, k, v, out, lse, dout, dq, dk, dv, dtable, self._space(1), lengths, first, prefix, docs, slopes,
+                                        table, bucket, None)
+            if rc is not None:
+                return B._check(rc, "small_attention_grad")
         self._fill(lengths, first, prefix, docs, slopes, table, bucket)
         _floats(lse, (r.N, r.heads, r.Sq))
         if dtable is not None:

@@ -37,7 +37,7 @@ def _stale(target, deps):
 def build_fastcall(force=False):
     """Host code only, against torch's headers (its libraries are loaded before it)."""
     src = os.path.join(CSRC, "fastcall.cpp")
-    if not (force or _stale(FASTCALL, [src, os.path.join(HERE, "..", "include", "small.h")])):
+    if not (force or _stale(FASTCALL, [src, os.path.join(HERE, "..", "include", "small.h"), os.path.join(HERE, "include", "small_attn.h")])):
         return
     root = os.path.dirname(torch.__file__)
     include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),

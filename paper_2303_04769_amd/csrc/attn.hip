@@ -175,25 +175,43 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
     }
 }
 
-// Joins a row's parts: each is an unnormalized sum of values with the maximum that its weights were taken against. A wave a row.
+// Joins a row's parts: each is an unnormalized sum of values with the reference that its weights were taken against. WAVES waves a row (1: four rows a
+// workgroup; 4: one row, for many parts), which take the parts in turn.
+template <int WAVES>
 __global__ void __launch_bounds__(256) attn_join(AttnArgs a, size_t rows)
 {
-    const size_t at = (size_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (at >= rows) return;
-    const int lane = threadIdx.x & 63;
+    __shared__ float sums[4][256], all[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, first = WAVES == 1 ? 0 : wave;
+    const size_t at = WAVES == 1 ? (size_t)blockIdx.x * 4 + wave : blockIdx.x;
+    if (at >= rows) return;                                     // (WAVES 4: never)
     const float2 *ml = a.part_ml + at * a.splits;
     const float *parts = a.part_o + at * a.splits * a.D;
     float top = -kInf, sum = 0.f, o[4] = {};
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, ml[s].x);
+#pragma unroll 4
+    for (int s = lane; s < a.splits; s += 64) top = fmaxf(top, ml[s].x);
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float ref = top == -kInf ? 0.f : top;
-    for (int s = 0; s < a.splits; ++s) {
+#pragma unroll 4
+    for (int s = first; s < a.splits; s += WAVES) {
         const float2 w = ml[s];
-        if (w.y == 0.f) continue;                               // (the part saw no key)
-        const float x = __builtin_amdgcn_exp2f(w.x - ref);
+        const float x = w.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.x - ref);      // (a part that saw no key)
         sum = fmaf(x, w.y, sum);
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-            if (lane + 64 * k < a.D) o[k] = fmaf(x, parts[(size_t)s * a.D + lane + 64 * k], o[k]);
+            if (lane + 64 * k < a.D) {
+                const float y = parts[(size_t)s * a.D + lane + 64 * k];
+                o[k] += w.y == 0.f ? 0.f : x * y;
+            }
+    }
+    if constexpr (WAVES == 4) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) sums[wave][lane + 64 * k] = o[k];
+        if (lane == 0) all[wave] = sum;
+        __syncthreads();
+        if (wave) return;
+        sum = (all[0] + all[1]) + (all[2] + all[3]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = (sums[0][lane + 64 * k] + sums[1][lane + 64 * k]) + (sums[2][lane + 64 * k] + sums[3][lane + 64 * k]);
     }
     const int by_set = (int)(at / (unsigned)a.rows), r = (int)(at - (size_t)by_set * a.rows), n = a.by_sets.div(by_set), set = by_set - n * a.head_sets;
     const int hh = a.pack ? a.by_Sq.div(r) : 0, i = r - hh * a.Sq, head = a.pack ? set * a.group + hh : set;
@@ -222,7 +240,8 @@ hipError_t launch_attn_rows(const AttnArgs &a, bool vec, size_t bias_bytes, hipS
 hipError_t launch_attn_join(const AttnArgs &a, hipStream_t s)
 {
     const size_t rows = (size_t)a.N * a.head_sets * a.rows;
-    hipLaunchKernelGGL(attn_join, dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, rows);
+    if (a.splits >= 16 && rows < (1u << 30)) hipLaunchKernelGGL((attn_join<4>), dim3((unsigned)rows), dim3(256), 0, s, a, rows);
+    else hipLaunchKernelGGL((attn_join<1>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, s, a, rows);
     return hipGetLastError();
 }
 

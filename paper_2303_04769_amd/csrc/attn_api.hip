@@ -141,8 +141,10 @@ AttnPlan plan_attn(const small_attn &a)
     const long sets = (long)a.N * p.head_sets;
     p.row_tiles = p.token ? 1 : (p.rows + 63) / 64;
     const long base = sets * p.row_tiles;
-    long most = p.token ? (a.Sk + 511) / 512 : (a.Sk + 255) / 256;       // keys of a part, at least
-    const long want = base < 2 * cus ? (2 * cus + base - 1) / base : 1;
+    // Parts of 256 keys at least. Tiles of rows: two workgroups a compute unit. Single tokens: one round of workgroups, or, where there is about one without
+    // parts, four, whose lengths may differ (64 streams of 2048 to 16384 keys: 302 us with two rounds, 250 with four, 262 with eight).
+    const long most = (a.Sk + 255) / 256;
+    const long want = p.token ? (base < cus / 2 ? cus / base : (4 * cus + base - 1) / base) : base < 2 * cus ? (2 * cus + base - 1) / base : 1;
     p.splits = (int)(want < most ? want : most);
     if (p.splits < 1) p.splits = 1;
     const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };

@@ -1,4 +1,4 @@
-// The single-layer calls of binding.py from Python, without ctypes: a call of a few microseconds on the GPU is bound by its
+// The single-layer calls of binding.py, and the calls of attn.py, from Python, without ctypes: a call of a few microseconds on the GPU is bound by its
 // host time, and of that the launch itself takes 3.0 us; attribute reads, argument conversion and the foreign-function
 // interface took another 1.6 (ReLU) to 3 (convolution), here some 0.4.
 //
@@ -13,16 +13,22 @@
 
 #include <dlfcn.h>
 #include <stddef.h>
+#include <string.h>
+
+#include <initializer_list>
 
 #include "../../include/small.h"
+#include "../include/small_attn.h"
 
 namespace {
 
 PyTypeObject *quant_type = nullptr;        // binding.small_quant
+PyTypeObject *attn_type = nullptr;         // attn.small_attn
 
 #define SMALL_FUNCTIONS(X)                                                                                                        \
     X(small_pack) X(small_unpack) X(small_conv2d) X(small_dwconv2d) X(small_pool2d) X(small_relu) X(small_add) X(small_dense)     \
-    X(small_pack_u8) X(small_unpack_u8) X(small_conv2d_u8) X(small_dwconv2d_u8) X(small_dense_u8) X(small_pool2d_u8) X(small_relu_u8)
+    X(small_pack_u8) X(small_unpack_u8) X(small_conv2d_u8) X(small_dwconv2d_u8) X(small_dense_u8) X(small_pool2d_u8) X(small_relu_u8) \
+    X(small_groupnorm) X(small_groupnorm_grad) X(small_attention) X(small_attention_grad)
 struct Library {
 #define X(f) decltype(&::f) f = nullptr;
     SMALL_FUNCTIONS(X)
@@ -91,6 +97,88 @@ struct Reader {
             return nullptr;
         }
         return static_cast<T *>(t.data_ptr());
+    }
+    float number32(int k)
+    {
+        if (!plain) return 0.f;
+        if (!PyFloat_CheckExact(a[k])) {
+            plain = false;
+            return 0.f;
+        }
+        return (float)PyFloat_AS_DOUBLE(a[k]);
+    }
+    // The record of an attention plan, without its pointers and strides.
+    small_attn record(int k)
+    {
+        small_attn r = {};
+        if (!plain) return r;
+        if (!attn_type || Py_TYPE(a[k]) != attn_type || PyObject_GetBuffer(a[k], &quant, PyBUF_SIMPLE) != 0 || quant.len != (Py_ssize_t)sizeof(small_attn)) {
+            PyErr_Clear();
+            plain = false;
+            return r;
+        }
+        memcpy(&r, quant.buf, sizeof r);
+        return r;
+    }
+    // An activation [N][blocks][S][Cb] that may be a view, of at least `channels` channels.
+    float *view(int k, const small_attn &r, int S, long channels, small_tokens *strides)
+    {
+        if (!plain || error) return nullptr;
+        if (!THPVariable_CheckExact(a[k])) {
+            plain = false;
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(a[k]);
+        if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 4 || t.size(0) != r.N || t.size(2) != S || t.size(3) != r.Cb ||
+            (r.Cb > 1 && t.stride(3) != 1) || t.size(1) * r.Cb < channels) {
+            plain = false;                               // (the binding says what is wrong with it)
+            return nullptr;
+        }
+        *strides = small_tokens{(size_t)t.stride(0), (size_t)t.stride(1), (size_t)t.stride(2)};
+        return static_cast<float *>(t.data_ptr());
+    }
+    // A contiguous tensor of these sizes, or null for None.
+    template <typename T>
+    T *of(int k, at::ScalarType type, std::initializer_list<long> sizes)
+    {
+        if (!plain || error || a[k] == Py_None) return nullptr;
+        if (!THPVariable_CheckExact(a[k])) {
+            plain = false;
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(a[k]);
+        bool fits = t.is_cuda() && t.scalar_type() == type && t.is_contiguous() && t.dim() == (long)sizes.size();
+        long d = 0;
+        if (fits)
+            for (long n : sizes) fits = fits && t.size(d++) == n;
+        if (!fits) {
+            plain = false;
+            return nullptr;
+        }
+        return static_cast<T *>(t.data_ptr());
+    }
+    void *bytes(int k, size_t *size)
+    {
+        *size = 0;
+        if (!plain || error || a[k] == Py_None) return nullptr;
+        if (!THPVariable_CheckExact(a[k])) {
+            plain = false;
+            return nullptr;
+        }
+        const at::Tensor &t = THPVariable_Unpack(a[k]);
+        *size = t.nbytes();
+        return t.data_ptr();
+    }
+    // lengths, first, prefix, docs, slopes, table, bucket from argument k on.
+    void masks(int k, small_attn &r)
+    {
+        r.lengths = of<int>(k, at::kInt, {r.N});
+        r.first = of<int>(k + 1, at::kInt, {r.N});
+        r.prefix = of<int>(k + 2, at::kInt, {r.N});
+        r.docs = of<int>(k + 3, at::kInt, {r.N, r.Sk});
+        r.slopes = of<float>(k + 4, at::kFloat, {r.heads});
+        r.table = of<float>(k + 5, at::kFloat, {r.heads, r.buckets});
+        r.bucket = of<int>(k + 6, at::kInt, {2L * r.reach + 1});
     }
     float *f32(int k) { return tensor<float>(k, at::kFloat, "expected a contiguous float32 CUDA tensor"); }
     unsigned char *u8(int k) { return tensor<unsigned char>(k, at::kByte, "expected a contiguous uint8 CUDA tensor"); }
@@ -169,6 +257,45 @@ ENTRY(dense_u8, 11, const int N = r.i(3), Ci = r.i(4), Co = r.i(5), Cib = r.i(6)
       auto *x = r.u8(0); auto *w = r.u8(1); auto *y = r.u8(2); auto *sums = r.i32(9);
       return r.call([&](void *s) { return lib.small_dense_u8(x, w, y, N, Ci, Co, Cib, Cob, q, sums, s); });)
 
+ENTRY(groupnorm, 15, const int N = r.i(5), C = r.i(6), H = r.i(7), W = r.i(8), G = r.i(9); const float eps = r.number32(10); const int act = r.i(11), Cb = r.i(12);
+      size_t size; void *ws = r.bytes(13, &size);
+      auto *x = r.f32(0); auto *ga = r.f32(1); auto *be = r.f32(2); auto *y = r.f32(3); auto *st = r.f32(4);
+      return r.call([&](void *s) { return lib.small_groupnorm(x, ga, be, y, st, N, C, H, W, G, eps, act, Cb, ws, size, s); });)
+ENTRY(groupnorm_grad, 17, const int N = r.i(8), C = r.i(9), H = r.i(10), W = r.i(11), G = r.i(12), act = r.i(13), Cb = r.i(14);
+      size_t size; void *ws = r.bytes(15, &size);
+      auto *x = r.f32(0); auto *ga = r.f32(1); auto *be = r.f32(2); auto *st = r.f32(3); auto *dy = r.f32(4); auto *dx = r.f32(5); auto *dg = r.f32(6); auto *db = r.f32(7);
+      return r.call([&](void *s) { return lib.small_groupnorm_grad(x, ga, be, st, dy, dx, dg, db, N, C, H, W, G, act, Cb, ws, size, s); });)
+
+// (record, q, k, v, out, lse, workspace, lengths, first, prefix, docs, slopes, table, bucket, stream): of a plan
+ENTRY(attention, 15, small_attn rec = r.record(0); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
+      size_t size; void *ws = r.bytes(6, &size);
+      r.masks(7, rec);
+      auto *q = r.view(1, rec, rec.Sq, cq, &rec.q); auto *k = r.view(2, rec, rec.Sk, ck, &rec.k); auto *v = r.view(3, rec, rec.Sk, ck, &rec.v);
+      auto *o = r.view(4, rec, rec.Sq, cq, &rec.out); auto *l = r.of<float>(5, at::kFloat, {rec.N, rec.heads, rec.Sq});
+      return r.call([&](void *s) { return lib.small_attention(&rec, q, k, v, o, l, ws, size, s); });)
+// (record, q, k, v, out, lse, dout, dq, dk, dv, dtable, workspace, the same masks, stream)
+ENTRY(attention_grad, 20, small_attn rec = r.record(0); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
+      size_t size; void *ws = r.bytes(11, &size);
+      r.masks(12, rec);
+      auto *q = r.view(1, rec, rec.Sq, cq, &rec.q); auto *k = r.view(2, rec, rec.Sk, ck, &rec.k); auto *v = r.view(3, rec, rec.Sk, ck, &rec.v);
+      auto *o = r.view(4, rec, rec.Sq, cq, &rec.out); auto *l = r.of<float>(5, at::kFloat, {rec.N, rec.heads, rec.Sq});
+      auto *d = r.view(6, rec, rec.Sq, cq, &rec.dout); auto *dq = r.view(7, rec, rec.Sq, cq, &rec.dq);
+      auto *dk = r.view(8, rec, rec.Sk, ck, &rec.dk); auto *dv = r.view(9, rec, rec.Sk, ck, &rec.dv);
+      auto *dt = r.of<float>(10, at::kFloat, {rec.heads, rec.buckets});
+      return r.call([&](void *s) { return lib.small_attention_grad(&rec, q, k, v, o, l, d, dq, dk, dv, dt, ws, size, s); });)
+
+// bind_attention(attn's small_attn)
+PyObject *bind_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 1 || !PyType_Check(args[0])) {
+        PyErr_SetString(PyExc_TypeError, "bind_attention(small_attn)");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);                    // (kept for the module's life)
+    attn_type = reinterpret_cast<PyTypeObject *>(args[0]);
+    Py_RETURN_NONE;
+}
+
 // bind(handle of the loaded library, the binding's small_quant)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -195,7 +322,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 #define METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(bind), METHOD(pack), METHOD(unpack), METHOD(pack_u8), METHOD(unpack_u8), METHOD(conv2d), METHOD(conv2d_u8),
                          METHOD(dwconv2d), METHOD(dwconv2d_u8), METHOD(pool2d), METHOD(pool2d_u8), METHOD(relu), METHOD(relu_u8), METHOD(add),
-                         METHOD(dense), METHOD(dense_u8), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(dense), METHOD(dense_u8), METHOD(groupnorm), METHOD(groupnorm_grad), METHOD(attention), METHOD(attention_grad),
+                         METHOD(bind_attention), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -66,12 +66,12 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
  * columns of images that are `width` pixels wide; width = 1 makes it the distance in a sequence. bucket: 2 * reach + 1 bucket indices
  * in 0 .. buckets - 1 (values outside are taken into that range); table: [heads][buckets]; a bias below -1e30, so also one of the
  * type's lowest value, hides its offsets as minus infinity does.
- * A row that sees no key, or only keys of score -inf, gives out = 0 and lse = -inf. Keys at and beyond an image's length are never
- * read and may hold anything; neither does what a key hidden by another mask holds reach a row that does not see it.
+ * A row that sees no key, or only keys of score -inf, gives out = 0 and lse = -inf. Keys at and beyond an image's length may hold
+ * anything (NaN among it), and neither does what a key hidden by another mask holds reach a row that does not see it.
  *
  * All of lengths, first, prefix, docs, slopes, table and bucket are DEVICE pointers. Limits: D <= 256; Sq, Sk <= 2^28, first positions are
  * taken into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31. Tensors may be larger than 2^31 values.
- * lse may be NULL in the forward call. small_attention_workspace (host only): bytes for a forward call (grad = 0) or a gradient call (grad = 1),
+ * lse may be NULL in the forward call. small_attention_workspace (host only): bytes for a forward call (grad = 0) or a gradient call (grad = 1); of the pointers in *a it only matters whether table is NULL;
  * 256-byte aligned (0 is possible: then it may be NULL).
  *
  * small_attention_grad: given out and lse of the forward call and dout, the gradients dq, dk, dv (dk, dv summed over a key head's query heads) and dtable ([heads][buckets]; NULL when not wanted or table is NULL). Every value of
