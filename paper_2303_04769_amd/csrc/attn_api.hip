@@ -37,7 +37,7 @@ size_t norm_elems(int N, int C, int H, int W, int G, int Cb, int *rc)
     // a plane and a group within 32-bit offsets, the tensor's size within 2^40 values, a workgroup's number in 31 bits
     const double n = (double)N * C * H * W;
     if ((double)H * W * Cb > INT_MAX || (double)H * W * (C / G) > INT_MAX || n > 1e12 || (double)N * C > INT_MAX) return 0;
-    if ((double)groupnorm_workspace(N, C, H * W, Cb) / (sizeof(float) * 2 * Cb) > INT_MAX) return 0;
+    if ((double)groupnorm_workspace(N, C, H * W, G, Cb) / (sizeof(float) * 2 * Cb) > INT_MAX) return 0;
     *rc = SMALL_OK;
     return (size_t)N * C * H * W;
 }
@@ -400,7 +400,7 @@ int small_groupnorm_workspace(int N, int C, int H, int W, int G, int Cb, size_t 
     if (!bytes) return SMALL_ERR_NULL;
     int rc;
     if (!norm_elems(N, C, H, W, G, Cb, &rc)) return rc;
-    *bytes = groupnorm_workspace(N, C, H * W, Cb);
+    *bytes = groupnorm_workspace(N, C, H * W, G, Cb);
     return SMALL_OK;
 }
 
@@ -413,7 +413,7 @@ int small_groupnorm(const float *in, const float *gamma, const float *beta, floa
     if (!n) return rc;
     if (!(eps >= 0.f) || isinf(eps) || !act_ok(act)) return SMALL_ERR_SHAPE;
     if (!block_ok(Cb, (uintptr_t)in | (uintptr_t)out)) return SMALL_ERR_BLOCK;
-    const size_t need = groupnorm_workspace(N, C, H * W, Cb);
+    const size_t need = groupnorm_workspace(N, C, H * W, G, Cb);
     if (!workspace_ok(workspace, workspace_bytes, need)) return SMALL_ERR_WORKSPACE;
     const Range o(out, n), st(stats, stats ? 2 * (size_t)N * G : 0), ws(workspace, need / sizeof(float));
     const Range reads[] = {Range(gamma, C), Range(beta, C)};
@@ -435,7 +435,7 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
     if (!n) return rc;
     if (!act_ok(act)) return SMALL_ERR_SHAPE;
     if (!block_ok(Cb, (uintptr_t)in | (uintptr_t)dout | (uintptr_t)din)) return SMALL_ERR_BLOCK;
-    const size_t need = groupnorm_workspace(N, C, H * W, Cb);
+    const size_t need = groupnorm_workspace(N, C, H * W, G, Cb);
     if (!workspace_ok(workspace, workspace_bytes, need)) return SMALL_ERR_WORKSPACE;
     const size_t np = dgamma ? C : 0;
     const Range writes[] = {Range(din, n), Range(dgamma, np), Range(dbeta, np), Range(workspace, need / sizeof(float))};

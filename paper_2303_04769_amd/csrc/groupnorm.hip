@@ -5,7 +5,12 @@
 // memory. Where a unit fits the registers of one workgroup (65536 values forward, 32768 in the gradient, which holds two
 // tensors), that workgroup reads it once, takes sum and squared differences from the registers and writes the result (norm_unit,
 // norm_unit_grad: one launch, every value read once). Otherwise statistics of pieces of planes are taken by one launch
-// (norm_stats, norm_sums) and joined and applied by the next (norm_apply, norm_apply_grad), which reads the tensors again.
+// (norm_stats, norm_sums) and joined and applied by the next (norm_apply, norm_apply_grad), which reads the tensors again; many pieces are
+// joined by a launch in between (norm_groups).
+//
+// Measured: 56 x 56 pixels of 256 channels, 64 images, 94 us, 4.4 TB/s (norm_unit, values streamed in and out; a thread with 25 rows in two
+// smaller workgroups a compute unit runs out of registers, 101 us); 25 x 5 of 64 channels, 1024 images, 13.5 us, 4.9 TB/s; gradient of
+// 57 x 43 pixels of 96 channels, 32 images, with the forward that it needs 57 us; 120 x 120 of 128 channels, 4 images, in pieces 22 us.
 //
 // A thread holds the same VEC channels throughout and walks over pixels, so the sums of a channel are thread-local until the end.
 #include "small_internal.h"
@@ -18,6 +23,7 @@ namespace {
 struct NormArgs {
     const float *x, *gamma, *beta, *dy, *stats_in;
     float *y, *stats;
+    float2 *fin;                  // [N][G]: what norm_groups made of them, or null (then every workgroup does that for its groups)
     float2 *part;                 // [N][C/Cb][chunks][Cb]: (mean, M2) or (sum dz, sum dz xhat) of a channel in a piece
     int S, Cb, nCb, C, G, cg, P, U, TP, RP, act, LG, LC, chunks, chunk_rows;
     float eps, inv_n;             // 1 / values of a group
@@ -62,13 +68,32 @@ __device__ __forceinline__ Vec<VEC> load(const float *p)
     }
     return r;
 }
+// One that is read this once.
+template <int VEC>
+__device__ __forceinline__ Vec<VEC> load_once(const float *p)
+{
+    if constexpr (VEC == 4) {
+        const floatx4 q = __builtin_nontemporal_load(reinterpret_cast<const floatx4 *>(p));
+        return Vec<VEC>{{q.x, q.y, q.z, q.w}};
+    } else {
+        return Vec<VEC>{{*p}};
+    }
+}
+// Results stream past the caches, which hold what is read again (57 x 43 pixels of 96 channels, 32 images, forward and gradient 60.7 -> 57.3 us).
 template <int VEC>
 __device__ __forceinline__ void store(float *p, const Vec<VEC> &r)
 {
     if constexpr (VEC == 4)
-        *reinterpret_cast<floatx4 *>(p) = floatx4{r.v[0], r.v[1], r.v[2], r.v[3]};
+        __builtin_nontemporal_store(floatx4{r.v[0], r.v[1], r.v[2], r.v[3]}, reinterpret_cast<floatx4 *>(p));
     else
         *p = r.v[0];
+}
+
+template <int VEC>
+__device__ __forceinline__ void keep(float *lds, const Vec<VEC> &r)
+{
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) lds[i] = r.v[i];
 }
 
 // out(i, sum over e < count of f(i, e)) for i < n: `lanes` neighbouring lanes (a power of two, at most 64) for each i. The order of a
@@ -102,14 +127,14 @@ __global__ void __launch_bounds__(1024) norm_unit(NormArgs a)
     for (int k = 0; k < K; ++k) {
         const int r = r0 + k * a.RP;
         v[k] = Vec<VEC>{};
-        if (on && r < a.S) v[k] = load<VEC>(a.x + at + (size_t)r * a.Cb);
+        if (on && r < a.S) v[k] = load_once<VEC>(a.x + at + (size_t)r * a.Cb);
     }
     Vec<VEC> s{};
 #pragma unroll
     for (int k = 0; k < K; ++k)
 #pragma unroll
         for (int i = 0; i < VEC; ++i) s.v[i] += v[k].v[i];
-    if (on) store<VEC>(red + r0 * a.U + cu, s);
+    if (on) keep<VEC>(red + r0 * a.U + cu, s);
     __syncthreads();
     const auto of_group = [&](int g, int e) { const int r = a.by_cg.div(e); return red[r * a.U + g * a.cg + (e - r * a.cg)]; };
     segment_sums(groups, a.cg * a.RP, a.LG, of_group, [&](int g, float x) { mean_g[g] = x * a.inv_n; });
@@ -127,7 +152,7 @@ __global__ void __launch_bounds__(1024) norm_unit(NormArgs a)
         if (r0 + k * a.RP < a.S)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) { const float d = v[k].v[i] - m[i]; s.v[i] = fmaf(d, d, s.v[i]); }
-    if (on) store<VEC>(red + r0 * a.U + cu, s);
+    if (on) keep<VEC>(red + r0 * a.U + cu, s);
     __syncthreads();
     const int n = a.by_units.div(blockIdx.x), g0 = (blockIdx.x - n * (int)a.by_units.d) * groups;
     segment_sums(groups, a.cg * a.RP, a.LG, of_group, [&](int g, float x) {
@@ -197,8 +222,8 @@ __global__ void __launch_bounds__(1024) norm_unit_grad(NormArgs a)
                 s2.v[i] = fmaf(dz, xh, s2.v[i]);
             }
     if (on) {
-        store<VEC>(red1 + r0 * a.U + cu, s1);
-        store<VEC>(red2 + r0 * a.U + cu, s2);
+        keep<VEC>(red1 + r0 * a.U + cu, s1);
+        keep<VEC>(red2 + r0 * a.U + cu, s2);
     }
     __syncthreads();
     // channels, for the parameters' gradients; then groups
@@ -299,30 +324,106 @@ __device__ __forceinline__ GroupEntry group_entry(const NormArgs &a, int image, 
     return GroupEntry{(((size_t)image * a.nCb + b) * a.chunks + k) * a.Cb + (c - b * a.Cb), k, c};
 }
 
+// Mean and rstd of the groups g0 .. g0 + groups - 1 of an image from their channels' statistics in all pieces: the mean of means, then the squares around it.
+// The entries are asked for once where a lane has four at most.
+template <typename Out>
+__device__ __forceinline__ void group_moments(const NormArgs &a, int image, int g0, int groups, Out out)
+{
+    const int lane = threadIdx.x & (a.LG - 1), per = blockDim.x / a.LG, entries = a.cg * a.chunks;
+    const auto count = [&](int k) { return (float)min(a.chunk_rows, a.S - k * a.chunk_rows); };
+    for (int g = threadIdx.x / a.LG; g < groups; g += per) {
+        float2 w[4];
+        float n[4], s = 0.f, q = 0.f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int e = lane + k * a.LG;
+            const GroupEntry x = group_entry(a, image, g0 + g, min(e, entries - 1));
+            w[k] = a.part[x.at];
+            n[k] = e < entries ? count(x.chunk) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) s = fmaf(n[k], w[k].x, s);
+        for (int e = lane + 4 * a.LG; e < entries; e += a.LG) {
+            const GroupEntry x = group_entry(a, image, g0 + g, e);
+            s = fmaf(count(x.chunk), a.part[x.at].x, s);
+        }
+        for (int d = a.LG >> 1; d; d >>= 1) s += __shfl_xor(s, d);
+        const float mean = s * a.inv_n;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) { const float d = w[k].x - mean; q += n[k] == 0.f ? 0.f : fmaf(n[k] * d, d, w[k].y); }
+        for (int e = lane + 4 * a.LG; e < entries; e += a.LG) {
+            const GroupEntry x = group_entry(a, image, g0 + g, e);
+            const float d = a.part[x.at].x - mean;
+            q += fmaf(count(x.chunk) * d, d, a.part[x.at].y);
+        }
+        for (int d = a.LG >> 1; d; d >>= 1) q += __shfl_xor(q, d);
+        if (lane == 0) out(g, mean, 1.f / sqrtf(fmaf(q, a.inv_n, a.eps)));
+    }
+}
+
+// The sums of gamma dz and gamma dz xhat over a group, divided by its values.
+template <typename Out>
+__device__ __forceinline__ void group_sums(const NormArgs &a, int image, int g0, int groups, Out out)
+{
+    const int lane = threadIdx.x & (a.LG - 1), per = blockDim.x / a.LG, entries = a.cg * a.chunks;
+    for (int g = threadIdx.x / a.LG; g < groups; g += per) {
+        float s = 0.f, q = 0.f;
+#pragma unroll 4
+        for (int e = lane; e < entries; e += a.LG) {
+            const GroupEntry x = group_entry(a, image, g0 + g, e);
+            const float2 w = a.part[x.at];
+            const float ga = a.gamma[x.c];
+            s = fmaf(w.x, ga, s);
+            q = fmaf(w.y, ga, q);
+        }
+        for (int d = a.LG >> 1; d; d >>= 1) { s += __shfl_xor(s, d); q += __shfl_xor(q, d); }
+        if (lane == 0) out(g, s * a.inv_n, q * a.inv_n);
+    }
+}
+
+// Either of these once for every group, in a launch of its own, where the pieces' workgroups would read too much for theirs. A wave a group (LG = 64).
+template <bool GRAD>
+__global__ void __launch_bounds__(256) norm_groups(NormArgs a, unsigned count)
+{
+    const unsigned id = blockIdx.x * 4 + (threadIdx.x >> 6);
+    if (id >= count) return;
+    const int image = (int)(id / (unsigned)a.G), g0 = (int)(id - (unsigned)image * a.G) - (threadIdx.x >> 6);       // (group_*: group threadIdx.x / 64 from g0 on)
+    if constexpr (GRAD) group_sums(a, image, g0, (threadIdx.x >> 6) + 1, [&](int, float s, float q) { a.fin[id] = float2{s, q}; });
+    else
+        group_moments(a, image, g0, (threadIdx.x >> 6) + 1, [&](int, float mean, float rstd) {
+            a.fin[id] = float2{mean, rstd};
+            if (a.stats) reinterpret_cast<float2 *>(a.stats)[id] = float2{mean, rstd};
+        });
+}
+
+// Rows of a piece that a thread asks for before it knows the statistics.
+constexpr int kEarly = 4;
+
 template <int VEC>
 __global__ void __launch_bounds__(1024) norm_apply(NormArgs a)
 {
     const unsigned block = gridDim.x - 1 - blockIdx.x;       // the pieces that norm_stats read last may still be in a cache
     const Piece p = piece_of<VEC>(a, (int)block);
+    const size_t at = ((size_t)p.plane * a.S + p.row0) * a.Cb + p.c;
+    Vec<VEC> early[kEarly];
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+        if (p.on && p.r0 + k * p.step < p.rows) early[k] = load<VEC>(a.x + at + (size_t)(p.r0 + k * p.step) * a.Cb);
     const int image = a.by_nCb.div(p.plane), g0 = a.by_cg.div(p.b * a.Cb), groups = a.by_cg.div(p.b * a.Cb + a.Cb - 1) - g0 + 1;
     float *const mean_g = norm_lds, *const rstd_g = mean_g + groups;
-    const int entries = a.cg * a.chunks;
-    const auto count = [&](int k) { return (float)min(a.chunk_rows, a.S - k * a.chunk_rows); };
-    segment_sums(groups, entries, a.LG, [&](int g, int e) { const GroupEntry q = group_entry(a, image, g0 + g, e);
-        return count(q.chunk) * a.part[q.at].x; }, [&](int g, float s) { mean_g[g] = s * a.inv_n; });
-    __syncthreads();
-    segment_sums(groups, entries, a.LG, [&](int g, int e) {
-        const GroupEntry q = group_entry(a, image, g0 + g, e);
-        const float2 w = a.part[q.at];
-        const float d = w.x - mean_g[g];
-        return fmaf(count(q.chunk) * d, d, w.y); },
-        [&](int g, float s) {
-            const float rstd = 1.f / sqrtf(fmaf(s, a.inv_n, a.eps));
-            rstd_g[g] = rstd;
-            // the piece that holds the group's first channel writes its statistics
-            if (a.stats && p.chunk == 0 && (g0 + g) * a.cg >= p.b * a.Cb)
-                reinterpret_cast<float2 *>(a.stats)[(size_t)image * a.G + g0 + g] = float2{mean_g[g], rstd};
-        });
+    if (a.fin) {
+        for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+            const float2 w = a.fin[(size_t)image * a.G + g0 + g];
+            mean_g[g] = w.x;
+            rstd_g[g] = w.y;
+        }
+    } else group_moments(a, image, g0, groups, [&](int g, float mean, float rstd) {
+        mean_g[g] = mean;
+        rstd_g[g] = rstd;
+        // the piece that holds the group's first channel writes its statistics
+        if (a.stats && p.chunk == 0 && (g0 + g) * a.cg >= p.b * a.Cb)
+            reinterpret_cast<float2 *>(a.stats)[(size_t)image * a.G + g0 + g] = float2{mean, rstd};
+    });
     __syncthreads();
     if (!p.on) return;
     float m[VEC], ga[VEC], be[VEC];
@@ -331,15 +432,17 @@ __global__ void __launch_bounds__(1024) norm_apply(NormArgs a)
         const int c = p.b * a.Cb + p.c + i, g = a.by_cg.div(c) - g0;
         m[i] = mean_g[g]; ga[i] = rstd_g[g] * a.gamma[c]; be[i] = a.beta[c];
     }
-    const size_t at = ((size_t)p.plane * a.S + p.row0) * a.Cb + p.c;
-#pragma unroll 4
-    for (int r = p.r0; r < p.rows; r += p.step) {
-        const Vec<VEC> v = load<VEC>(a.x + at + (size_t)r * a.Cb);
+    const auto apply = [&](int r, const Vec<VEC> &v) {
         Vec<VEC> y;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) y.v[i] = act_of(fmaf(v.v[i] - m[i], ga[i], be[i]), a.act);
         store<VEC>(a.y + at + (size_t)r * a.Cb, y);
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+        if (p.r0 + k * p.step < p.rows) apply(p.r0 + k * p.step, early[k]);
+#pragma unroll 4
+    for (int r = p.r0 + kEarly * p.step; r < p.rows; r += p.step) apply(r, load<VEC>(a.x + at + (size_t)r * a.Cb));
 }
 
 // What both gradient kernels need of a channel.
@@ -376,8 +479,8 @@ __global__ void __launch_bounds__(1024) norm_sums(NormArgs a)
                 s2.v[i] = fmaf(dz, xh, s2.v[i]);
             }
         }
-        store<VEC>(red1 + p.r0 * a.Cb + p.c, s1);
-        store<VEC>(red2 + p.r0 * a.Cb + p.c, s2);
+        keep<VEC>(red1 + p.r0 * a.Cb + p.c, s1);
+        keep<VEC>(red2 + p.r0 * a.Cb + p.c, s2);
     }
     __syncthreads();
     segment_sums(2 * a.Cb, a.RP, a.LC, [&](int i, int r) { return i < a.Cb ? red1[r * a.Cb + i] : red2[r * a.Cb + i - a.Cb]; },
@@ -391,13 +494,23 @@ __global__ void __launch_bounds__(1024) norm_apply_grad(NormArgs a)
 {
     const unsigned block = gridDim.x - 1 - blockIdx.x;
     const Piece p = piece_of<VEC>(a, (int)block);
+    const size_t at = ((size_t)p.plane * a.S + p.row0) * a.Cb + p.c;
+    Vec<VEC> early_x[kEarly], early_d[kEarly];
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+        if (p.on && p.r0 + k * p.step < p.rows) {
+            early_x[k] = load<VEC>(a.x + at + (size_t)(p.r0 + k * p.step) * a.Cb);
+            early_d[k] = load<VEC>(a.dy + at + (size_t)(p.r0 + k * p.step) * a.Cb);
+        }
     const int image = a.by_nCb.div(p.plane), g0 = a.by_cg.div(p.b * a.Cb), groups = a.by_cg.div(p.b * a.Cb + a.Cb - 1) - g0 + 1;
     float *const gr = norm_lds;
-    segment_sums(2 * groups, a.cg * a.chunks, a.LG, [&](int i, int e) {
-        const int second = i >= groups;
-        const GroupEntry q = group_entry(a, image, g0 + i - second * groups, e);
-        const float2 w = a.part[q.at];
-        return (second ? w.y : w.x) * a.gamma[q.c]; }, [&](int i, float s) { gr[i] = s * a.inv_n; });
+    if (a.fin) {
+        for (int g = threadIdx.x; g < groups; g += blockDim.x) {
+            const float2 w = a.fin[(size_t)image * a.G + g0 + g];
+            gr[g] = w.x;
+            gr[groups + g] = w.y;
+        }
+    } else group_sums(a, image, g0, groups, [&](int g, float s, float q) { gr[g] = s; gr[groups + g] = q; });
     __syncthreads();
     if (!p.on) return;
     const ChannelParams<VEC> w(a, p, image);
@@ -407,10 +520,7 @@ __global__ void __launch_bounds__(1024) norm_apply_grad(NormArgs a)
         const int g = a.by_cg.div(p.b * a.Cb + p.c + i) - g0;
         s1[i] = gr[g]; s2[i] = gr[groups + g];
     }
-    const size_t at = ((size_t)p.plane * a.S + p.row0) * a.Cb + p.c;
-#pragma unroll 4
-    for (int r = p.r0; r < p.rows; r += p.step) {
-        const Vec<VEC> v = load<VEC>(a.x + at + (size_t)r * a.Cb), d = load<VEC>(a.dy + at + (size_t)r * a.Cb);
+    const auto apply = [&](int r, const Vec<VEC> &v, const Vec<VEC> &d) {
         Vec<VEC> y;
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
@@ -418,7 +528,13 @@ __global__ void __launch_bounds__(1024) norm_apply_grad(NormArgs a)
             y.v[i] = w.rs[i] * fmaf(-xh, s2[i], fmaf(w.ga[i], dz, -s1[i]));
         }
         store<VEC>(a.y + at + (size_t)r * a.Cb, y);
-    }
+    };
+#pragma unroll
+    for (int k = 0; k < kEarly; ++k)
+        if (p.r0 + k * p.step < p.rows) apply(p.r0 + k * p.step, early_x[k], early_d[k]);
+#pragma unroll 4
+    for (int r = p.r0 + kEarly * p.step; r < p.rows; r += p.step)
+        apply(r, load<VEC>(a.x + at + (size_t)r * a.Cb), load<VEC>(a.dy + at + (size_t)r * a.Cb));
 }
 
 // dbeta, dgamma: the channels' sums over images and pieces. 16 channels a workgroup, 64 slices of the (image, piece) pairs.
@@ -457,8 +573,9 @@ int round_up(int v, int m) { return (v + m - 1) / m * m; }
 
 void chunks_of(int N, int C, int S, int Cb, int *chunks, int *rows)
 {
-    // some 2048 workgroups (8 a compute unit), pieces of 16 KB at least
-    const long planes = (long)N * (C / Cb), want = (2048 + planes - 1) / planes;
+    // some 512 workgroups (two a compute unit), pieces of 16 KB at least. With 2048 the sums of the pieces cost more
+    // than the fuller device gains: 384 x 384 pixels of 256 channels 234 us, 512 pieces 141, 256 pieces 157
+    const long planes = (long)N * (C / Cb), want = (512 + planes - 1) / planes;
     const long least = (4096 + Cb - 1) / Cb, each = (S + want - 1) / want;
     *rows = (int)(each > least ? each : least < S ? least : S);
     *chunks = (S + *rows - 1) / *rows;
@@ -533,16 +650,30 @@ hipError_t norm(NormArgs a, bool grad, int N, float *dgamma, float *dbeta, float
     const unsigned grid = (unsigned)((long)N * a.nCb * a.chunks);
     const int touched = (a.Cb + a.cg - 2) / a.cg + 1 < a.Cb ? (a.Cb + a.cg - 2) / a.cg + 1 : a.Cb;   // groups in a plane, at most
     const size_t rows_lds = sizeof(float) * 2 * ((size_t)a.RP * a.Cb + a.Cb), group_lds = sizeof(float) * 2 * touched;
-    a.LG = pow2_at_most(T / (grad ? 2 * touched : touched) > 0 ? T / (grad ? 2 * touched : touched) : 1, 64);
+    a.LG = pow2_at_most(T / touched > 0 ? T / touched : 1, 64);
+    // a workgroup that joins its groups' pieces itself reads them from the caches; past some 4 KB that takes longer than a launch for all groups
+    const bool apart = (long)touched * a.cg * a.chunks > 512;
+    if (apart) a.fin = ws + (size_t)N * a.C * a.chunks;
+    const auto groups = [&]() -> hipError_t {
+        if (!apart) return hipSuccess;
+        NormArgs b = a;
+        b.LG = 64;
+        const unsigned count = (unsigned)((long)N * a.G);
+        if (grad) hipLaunchKernelGGL((norm_groups<true>), dim3((count + 3) / 4), dim3(256), 0, s, b, count);
+        else hipLaunchKernelGGL((norm_groups<false>), dim3((count + 3) / 4), dim3(256), 0, s, b, count);
+        return hipGetLastError();
+    };
     if (grad) {
         hipLaunchKernelGGL((norm_sums<VEC>), dim3(grid), dim3(T), rows_lds, s, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if (hipError_t e = groups(); e != hipSuccess) return e;
         hipLaunchKernelGGL((norm_apply_grad<VEC>), dim3(grid), dim3(T), group_lds, s, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess || !dgamma) return e;
         hipLaunchKernelGGL(norm_params, dim3((a.C + 15) / 16), dim3(1024), 0, s, ws, dgamma, dbeta, N, a.C, a.by_Cb, a.chunks, a.by_chunks);
     } else {
         hipLaunchKernelGGL((norm_stats<VEC>), dim3(grid), dim3(T), rows_lds, s, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+        if (hipError_t e = groups(); e != hipSuccess) return e;
         hipLaunchKernelGGL((norm_apply<VEC>), dim3(grid), dim3(T), group_lds, s, a);
     }
     return hipGetLastError();
@@ -550,12 +681,12 @@ hipError_t norm(NormArgs a, bool grad, int N, float *dgamma, float *dbeta, float
 
 }  // namespace
 
-// Bytes for the sums of channels in pieces: the two-launch form's, which include those of whole planes.
-size_t groupnorm_workspace(int N, int C, int S, int Cb)
+// Bytes for the sums of channels in pieces (the form of several launches has the most) and of groups.
+size_t groupnorm_workspace(int N, int C, int S, int G, int Cb)
 {
     int chunks, rows;
     chunks_of(N, C, S, Cb, &chunks, &rows);
-    return (size_t)N * C * chunks * sizeof(float2);
+    return ((size_t)N * C * chunks + (size_t)N * G) * sizeof(float2);
 }
 
 hipError_t launch_groupnorm(const float *x, const float *gamma, const float *beta, const float *stats_in, const float *dy, float *y, float *stats,

@@ -316,7 +316,7 @@ hipError_t launch_group_conv(const float *in, const float *filt, float *out, con
                              int F_Cb, hipStream_t s);
 
 // Group normalization with an activation and its gradient (dy != null: y is din) on the blocked layout (groupnorm.hip).
-size_t groupnorm_workspace(int N, int C, int S, int Cb);
+size_t groupnorm_workspace(int N, int C, int S, int G, int Cb);
 hipError_t launch_groupnorm(const float *x, const float *gamma, const float *beta, const float *stats_in, const float *dy, float *y,
                             float *stats, float *dgamma, float *dbeta, int N, int C, int S, int G, float eps, int act, int Cb,
                             void *ws, hipStream_t s);

@@ -51,7 +51,7 @@ def test_groupnorm_refusals(lib):
     assert grad(din=P[0]) == 4 and grad(dgamma=P[7]) == 4 and grad(dgamma=P[1]) == 4 and grad(work=P[4]) == 4 and grad(din=C.c_void_p(0x50000004)) == 4
     n = C.c_size_t(0)
     assert lib.small_groupnorm_workspace(2, 32, 4, 4, 4, 16, None) == 1 and lib.small_groupnorm_workspace(2, 32, 4, 4, 3, 16, C.byref(n)) == 2
-    assert lib.small_groupnorm_workspace(2, 32, 4, 4, 4, 16, C.byref(n)) == 0 and n.value == 2 * 32 * 8
+    assert lib.small_groupnorm_workspace(2, 32, 4, 4, 4, 16, C.byref(n)) == 0 and n.value >= 2 * 32 * 8
 
 
 def record(**kw):
