@@ -391,40 +391,49 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
     }
 }
 
-// The table's gradient from the workgroups' sums by offset: over images and tiles of rows of a head, 32 offsets a workgroup ...
-__global__ void __launch_bounds__(256) attn_bias_offsets(const float *part, float *sums, int N, int heads, int row_tiles, int size, int blocks)
+// The sum of 32 slices' values, for slice 0, in a fixed order.
+__device__ __forceinline__ float sum_of_slices(float (*red)[32], float mine)
 {
-    __shared__ float red[8][32];
-    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, head = blockIdx.x / blocks, x = (blockIdx.x - head * blocks) * 32 + lane;
-    float s = 0.f;
-    if (x < size)
-        for (int e = slice; e < N * row_tiles; e += 8) {
-            const int n = e / row_tiles, tile = e - n * row_tiles;
-            s += part[(((size_t)n * heads + head) * row_tiles + tile) * size + x];
-        }
-    red[slice][lane] = s;
-    for (int d = 4; d; d >>= 1) {
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    red[slice][lane] = mine;
+    for (int d = 16; d; d >>= 1) {
         __syncthreads();
         if (slice < d) red[slice][lane] += red[slice + d][lane];
     }
-    if (slice == 0 && x < size) sums[(size_t)head * size + x] = red[0][lane];
+    return red[slice][lane];
+}
+
+// The table's gradient from the workgroups' sums by offset: over images and tiles of rows of a head, 32 offsets a workgroup ...
+__global__ void __launch_bounds__(1024) attn_bias_offsets(const float *part, float *sums, int N, int heads, int row_tiles, int size, int blocks)
+{
+    __shared__ float red[32][32];
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, head = blockIdx.x / blocks, x = (blockIdx.x - head * blocks) * 32 + lane;
+    float s[4] = {};
+    if (x < size)
+        for (int e0 = slice; e0 < N * row_tiles; e0 += 128)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int e = e0 + 32 * k, n = e / row_tiles, tile = e - n * row_tiles;
+                if (e < N * row_tiles) s[k] += part[(((size_t)n * heads + head) * row_tiles + tile) * size + x];
+            }
+    const float all = sum_of_slices(red, (s[0] + s[1]) + (s[2] + s[3]));
+    if (slice == 0 && x < size) sums[(size_t)head * size + x] = all;
 }
 // ... and over the offsets of a bucket, 32 buckets a workgroup.
-__global__ void __launch_bounds__(256) attn_bias_buckets(const float *sums, const int *bucket, float *dtable, int size, int buckets, int blocks)
+__global__ void __launch_bounds__(1024) attn_bias_buckets(const float *sums, const int *bucket, float *dtable, int size, int buckets, int blocks)
 {
-    __shared__ float red[8][32];
+    __shared__ float red[32][32];
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5, head = blockIdx.x / blocks, b = (blockIdx.x - head * blocks) * 32 + lane;
-    float s = 0.f;
-    for (int x = slice; x < size; x += 8) {
-        const int at = max(0, min(bucket[x], buckets - 1));
-        s += at == b ? sums[(size_t)head * size + x] : 0.f;
-    }
-    red[slice][lane] = s;
-    for (int d = 4; d; d >>= 1) {
-        __syncthreads();
-        if (slice < d) red[slice][lane] += red[slice + d][lane];
-    }
-    if (slice == 0 && b < buckets) dtable[(size_t)head * buckets + b] = red[0][lane];
+    float s[4] = {};
+    for (int x0 = slice; x0 < size; x0 += 128)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int x = min(x0 + 32 * k, size - 1), at = max(0, min(bucket[x], buckets - 1));
+            const float y = sums[(size_t)head * size + x];
+            s[k] += x == x0 + 32 * k && at == b ? y : 0.f;
+        }
+    const float all = sum_of_slices(red, (s[0] + s[1]) + (s[2] + s[3]));
+    if (slice == 0 && b < buckets) dtable[(size_t)head * buckets + b] = all;
 }
 
 }  // namespace
@@ -472,9 +481,9 @@ hipError_t launch_attn_grad_keys(const AttnArgs &a, bool vec, hipStream_t s)
 hipError_t launch_attn_grad_bias(const AttnArgs &a, float *sums, float *dtable, hipStream_t s)
 {
     const int size = 2 * a.reach + 1, by_offset = (size + 31) / 32, by_bucket = (a.buckets + 31) / 32;
-    hipLaunchKernelGGL(attn_bias_offsets, dim3(a.heads * by_offset), dim3(256), 0, s, a.part_bias, sums, a.N, a.heads, a.row_tiles, size, by_offset);
+    hipLaunchKernelGGL(attn_bias_offsets, dim3(a.heads * by_offset), dim3(1024), 0, s, a.part_bias, sums, a.N, a.heads, a.row_tiles, size, by_offset);
     if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    hipLaunchKernelGGL(attn_bias_buckets, dim3(a.heads * by_bucket), dim3(256), 0, s, sums, a.bucket, dtable, size, a.buckets, by_bucket);
+    hipLaunchKernelGGL(attn_bias_buckets, dim3(a.heads * by_bucket), dim3(1024), 0, s, sums, a.bucket, dtable, size, a.buckets, by_bucket);
     return hipGetLastError();
 }
 

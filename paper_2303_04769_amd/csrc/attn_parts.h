@@ -27,14 +27,6 @@ constexpr int kLift = 8;                       // of weights: with kSlack below 
 
 __device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-// c += a b for operands in two parts, the small products first.
-__device__ __forceinline__ floatx4 mfma_parts(half8 a_hi, half8 a_lo, half8 b_hi, half8 b_lo, floatx4 c)
-{
-    c = mfma16(a_lo, b_hi, c);
-    c = mfma16(a_hi, b_lo, c);
-    return mfma16(a_hi, b_hi, c);
-}
-
 typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef unsigned uintx4v __attribute__((ext_vector_type(4)));
@@ -67,6 +59,25 @@ __device__ __forceinline__ int parts_exponent(float most)
     return max(e, -100);
 }
 __device__ __forceinline__ float finite_magnitude(float x) { return fabsf(x) < kInf ? fabsf(x) : 0.f; }
+
+// A workgroup's tile of rows, of which (image, head), and its split of the keys. Causal rows have ever more keys, so there the longest tiles come first; where the device's eight
+// parts get whole heads, those of one head stay in one. Of the 32 workgroups that meet the 32 compute units of a part in turn, every other set comes in
+// reverse order, so that the workgroups that begin together on a compute unit have about the same work everywhere.
+struct RowTile { int group, tile, split; };
+template <bool SPLITS>
+__device__ __forceinline__ RowTile row_tile_of(const AttnArgs &a, unsigned groups)
+{
+    const unsigned tiles = (unsigned)a.row_tiles;
+    if (!a.causal || (SPLITS && a.splits > 1)) {
+        const int id = (int)xcd_contiguous(blockIdx.x, gridDim.x), by_split = SPLITS ? a.by_splits.div(id) : id, group = a.by_tiles.div(by_split);
+        return {group, (int)tiles - 1 - (by_split - group * (int)tiles), SPLITS ? id - by_split * a.splits : 0};
+    }
+    const bool whole = (groups & 7) == 0;
+    const unsigned part = whole ? blockIdx.x & 7 : 0, each = whole ? groups >> 3 : groups, at = whole ? blockIdx.x >> 3 : blockIdx.x;
+    const unsigned units = whole ? 32 : 256, set = at / units;
+    const unsigned r = (set & 1) && (set + 1) * units <= each * tiles ? (2 * set + 1) * units - 1 - at : at, by_tile = r / each;
+    return {(int)(part * each + (r - by_tile * each)), (int)(tiles - 1 - by_tile), 0};
+}
 
 struct PartsTensor {
     const float *p;

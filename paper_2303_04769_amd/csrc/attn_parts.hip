@@ -83,10 +83,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     __shared__ alignas(16) int key_doc[65];
     __shared__ int words[3];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int by_split = a.by_splits.div((int)id), split = (int)id - by_split * a.splits;
-    const int by_tile = a.by_tiles.div(by_split), tile = a.row_tiles - 1 - (by_split - by_tile * a.row_tiles);
-    const int n = a.by_sets.div(by_tile), head = by_tile - n * a.head_sets, key_head = a.by_group.div(head), kv = a.head_sets / a.group;
+    const RowTile here = row_tile_of<true>(a, (unsigned)a.N * a.head_sets);
+    const int split = here.split, tile = here.tile, n = a.by_sets.div(here.group), head = here.group - n * a.head_sets, key_head = a.by_group.div(head), kv = a.head_sets / a.group;
     const int row0 = tile * 64, i_raw = row0 + wave * 16 + m, i = min(i_raw, a.Sq - 1);      // rows past the end repeat the last one
     const ImageMask im(a, n);
     const RowState row(a, im, n, i, head);

@@ -120,15 +120,18 @@ __device__ __forceinline__ void sums_in_image(const floatx4 (&s)[4], int reach, 
             at[b][e] = (below | above | !there) ? reach + 1 : off[e];
         }
     }
+    // (Two lanes that share a place have keys as far apart as their rows, at most 15: of the keys 16 apart all places differ.)
     for (int turn = 0; turn < 4; turn += copies) {
         if ((unsigned)(g - turn) >= (unsigned)copies) continue;
 #pragma unroll
-        for (int b = 0; b < 4; ++b)
+        for (int e = 0; e < 4; ++e) {
+            float was[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                volatile float *p = mine + at[b][e];
-                *p = *p + s[b][e];
-            }
+            for (int b = 0; b < 4; ++b) was[b] = mine[at[b][e]];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) mine[at[b][e]] = was[b] + s[b][e];
+            asm volatile("" ::: "memory");
+        }
     }
 }
 
@@ -151,9 +154,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     __shared__ alignas(16) int key_doc[65];
     __shared__ int words[2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int by_tile = a.by_tiles.div((int)id), tile = a.row_tiles - 1 - ((int)id - by_tile * a.row_tiles);
-    const int n = a.by_heads.div(by_tile), head = by_tile - n * a.heads, key_head = a.by_group.div(head), kv = a.by_group.div(a.heads);
+    const RowTile here = row_tile_of<false>(a, (unsigned)a.N * a.heads);
+    const int tile = here.tile, n = a.by_heads.div(here.group), head = here.group - n * a.heads, key_head = a.by_group.div(head), kv = a.by_group.div(a.heads);
     const int row0 = tile * 64, i_raw = row0 + wave * 16 + m, i = min(i_raw, a.Sq - 1);
     const ImageMask im(a, n);
     const RowState row(a, im, n, i, head);
@@ -234,6 +236,20 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
 
     ColumnScale cs;
     floatx4 dq[DT] = {};
+    // (a wave whose rows are all past the end does its share of the copies only)
+    if (__builtin_amdgcn_readfirstlane(row0 + wave * 16) >= a.Sq)
+        for (int j0 = begin; j0 < end; j0 += 64) {
+            wait_vmcnt<0>();
+            __syncthreads();
+            copy_image(a.k_chan + (first_tile + j0 / 64) * IMAGE, IMAGE, lds + 2 * IMAGE);
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (j0 + 64 < end) {
+                copy_image(a.k_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds);
+                copy_image(a.v_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds + IMAGE);
+            }
+        }
+    else
     for (int j0 = begin; j0 < end; j0 += 64) {
         const int k_exp = k_exps[j0 / 64], v_exp = v_exps[j0 / 64];
         stage_keys<64>(a, n, j0, key_code, key_doc);
@@ -294,28 +310,29 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
 #pragma unroll
         for (int b = 0; b < 2; ++b) products(dq, kt + 2 * IMAGE + b * DT * 2048, 2048, hi_[b], lo_[b]);
     }
+    const AttnArgs z = late_args();
     if (sums) {
         __shared__ float ends[8];
         sum_lo = wave_sum(sum_lo);
         sum_hi = wave_sum(sum_hi);
         if (lane == 0) { ends[wave] = sum_lo; ends[4 + wave] = sum_hi; }
         __syncthreads();
-        float *const part = a.part_bias + at_tile * size;
+        float *const part = z.part_bias + at_tile * size;
         for (int x = threadIdx.x; x < size; x += 256) {
             float y = 0.f;
-            for (int c = 0; c < a.bias_copies; ++c) y += acc[c * stride + x];
+            for (int c = 0; c < z.bias_copies; ++c) y += acc[c * stride + x];
             if (x == 0) y += (ends[0] + ends[1]) + (ends[2] + ends[3]);
             if (x == size - 1) y += (ends[4] + ends[5]) + (ends[6] + ends[7]);
             part[x] = y;
         }
     }
-    if (i_raw < a.Sq) {
-        const float back = cs.back(a.scale);
-        float *token = const_cast<float *>(token_at(a.dq, a.dqs, n, i));
+    if (i_raw < z.Sq) {
+        const float back = cs.back(z.scale);
+        float *token = const_cast<float *>(token_at(z.dq, z.dqs, n, i));
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
-            if (a.vec) store_quad<true>(a, a.dqs, token, head * a.D, 16 * d + 4 * g, dq[d] * back);
-            else store_quad<false>(a, a.dqs, token, head * a.D, 16 * d + 4 * g, dq[d] * back);
+            if (z.vec) store_quad<true>(z, z.dqs, token, head * z.D, 16 * d + 4 * g, dq[d] * back);
+            else store_quad<false>(z, z.dqs, token, head * z.D, 16 * d + 4 * g, dq[d] * back);
         }
     }
 }
@@ -388,6 +405,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
 
     float *const bias_lds = reinterpret_cast<float *>(parts_lds + 4 * HALF);
     const unsigned lds = lds_address(parts_lds);
+    // (a wave whose keys are all past the end, of the image or of its length, does its share of the copies only)
+    const bool idle = __builtin_amdgcn_readfirstlane(j0 + wave * 16) >= im.len;
     ColumnScale cs;
     floatx4 dk[DT] = {}, dv[DT] = {};
     for (int head = h0; head < h1 && begin < end; ++head) {
@@ -407,6 +426,20 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         const auto at = [&](int i0) { return (first_tile + i0 / 64) * IMAGE + (i0 & 32 ? HALF : 0); };
         copy_image(a.q_tok + at(begin), HALF, lds);
         copy_image(a.do_tok + at(begin), HALF, lds + HALF);
+        if (idle)
+            for (int i0 = begin; i0 < end; i0 += 32) {
+                wait_vmcnt<0>();
+                __syncthreads();
+                copy_image(a.q_chan + at(i0), HALF, lds + 2 * HALF);
+                copy_image(a.do_chan + at(i0), HALF, lds + 3 * HALF);
+                wait_vmcnt<0>();
+                __syncthreads();
+                if (i0 + 32 < end) {
+                    copy_image(a.q_tok + at(i0 + 32), HALF, lds);
+                    copy_image(a.do_tok + at(i0 + 32), HALF, lds + HALF);
+                }
+            }
+        else
         for (int i0 = begin; i0 < end; i0 += 32) {
             const int q_exp = a.q_exps[first_tile + i0 / 64], d_exp = a.do_exps[first_tile + i0 / 64];
             if (threadIdx.x < 32) {
@@ -471,7 +504,13 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, u[e]);
             }
-            if (near) {
+            const int first = code - row_code[0] - 4 * g + a.reach;
+            if (near && bias && a.width == 1 && __all((first <= 2 * a.reach) & (first >= 19))) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] += bias[first - 16 * b - e];
+            } else if (near) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const int4 c4 = *reinterpret_cast<const int4 *>(row_code + 16 * b + 4 * g);
@@ -535,30 +574,31 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             products(dk, qt + 2 * HALF, 2048, s_hi, s_lo);
         }
     }
-    if (j_raw >= a.Sk) return;
-    const float dk_back = cs.back(a.scale), dv_back = d_most == -1000 ? 0.f : ldexpf(1.f, d_most - 14);
-    if (a.splits > 1) {
+    const AttnArgs z = late_args();
+    if (j_raw >= z.Sk) return;
+    const float dk_back = cs.back(z.scale), dv_back = d_most == -1000 ? 0.f : ldexpf(1.f, d_most - 14);
+    if (z.splits > 1) {
         // [part][image, key head][key][dk, dv][D]
-        float *to = a.part_o + ((((size_t)part * a.N + n) * kv + key_head) * a.Sk + j) * 2 * a.D;
+        float *to = z.part_o + ((((size_t)part * z.N + n) * kv + key_head) * z.Sk + j) * 2 * z.D;
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int c = 16 * d + 4 * g + e;
-                if (c < a.D) { to[c] = dk[d][e] * dk_back; to[a.D + c] = dv[d][e] * dv_back; }
+                if (c < z.D) { to[c] = dk[d][e] * dk_back; to[z.D + c] = dv[d][e] * dv_back; }
             }
         return;
     }
-    float *tk = const_cast<float *>(token_at(a.dk, a.dks, n, j)), *tv = const_cast<float *>(token_at(a.dv, a.dvs, n, j));
+    float *tk = const_cast<float *>(token_at(z.dk, z.dks, n, j)), *tv = const_cast<float *>(token_at(z.dv, z.dvs, n, j));
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
         const int c = 16 * d + 4 * g;
-        if (a.vec) {
-            store_quad<true>(a, a.dks, tk, key_head * a.D, c, dk[d] * dk_back);
-            store_quad<true>(a, a.dvs, tv, key_head * a.D, c, dv[d] * dv_back);
+        if (z.vec) {
+            store_quad<true>(z, z.dks, tk, key_head * z.D, c, dk[d] * dk_back);
+            store_quad<true>(z, z.dvs, tv, key_head * z.D, c, dv[d] * dv_back);
         } else {
-            store_quad<false>(a, a.dks, tk, key_head * a.D, c, dk[d] * dk_back);
-            store_quad<false>(a, a.dvs, tv, key_head * a.D, c, dv[d] * dv_back);
+            store_quad<false>(z, z.dks, tk, key_head * z.D, c, dk[d] * dk_back);
+            store_quad<false>(z, z.dvs, tv, key_head * z.D, c, dv[d] * dv_back);
         }
     }
 }

@@ -263,7 +263,14 @@ __device__ __forceinline__ void finish_scores(const AttnArgs &a, floatx4 (&s)[NB
             for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, base);
     }
     if (near) {
-        if (bias) {
+        // in a sequence the biases of a lane's keys stand one behind the other, and where the whole tile is inside the reach nothing is clamped
+        const int first = key_code[0] + 4 * g - row.code + a.reach;
+        if (bias && a.width == 1 && __all((first >= 0) & (first + 16 * NB - 13 <= 2 * a.reach))) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][e] += bias[first + 16 * b + e];
+        } else if (bias) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const int4 kc = *reinterpret_cast<const int4 *>(key_code + 16 * b + 4 * g);
