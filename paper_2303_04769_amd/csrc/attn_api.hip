@@ -194,10 +194,10 @@ hipError_t make_parts(AttnArgs &x, const AttnPlan &p, const small_attn &a, void 
     int *const exps = (int *)((char *)ws + p.exps_at);
     PartsArgs args{};
     args.count = 2;
-    args.t[0] = PartsTensor{x.k, x.ks, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.k_at, nullptr, exps, 0};
-    args.t[1] = PartsTensor{x.v, x.vs, a.kv_heads, a.Sk, tiles, 0, nullptr, (char *)ws + p.v_at, exps + (size_t)a.N * a.kv_heads * tiles, 0};
-    x.k_tok = args.t[0].by_token; x.k_exps = args.t[0].exps;
-    x.v_chan = args.t[1].by_channel; x.v_exps = args.t[1].exps;
+    args.t[0] = PartsTensor{x.k, x.ks, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.k_at, exps, 0};
+    args.t[1] = PartsTensor{x.v, x.vs, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.v_at, exps + (size_t)a.N * a.kv_heads * tiles, 0};
+    x.k_tok = args.t[0].image; x.k_exps = args.t[0].exps;
+    x.v_tok = args.t[1].image; x.v_exps = args.t[1].exps;
     return launch_make_parts(x, args, vec, s);
 }
 
@@ -231,7 +231,7 @@ bool grad_in_parts(const small_attn &a)
 struct GradPlan {
     bool parts;
     int row_tiles, key_tiles, splits, row_parts;
-    size_t part_at, sums_at, images[7], exps[4], dkv_at, bytes;
+    size_t part_at, sums_at, images[4], exps[4], dkv_at, bytes;
 };
 GradPlan plan_grad(const small_attn &a)
 {
@@ -250,7 +250,7 @@ GradPlan plan_grad(const small_attn &a)
     p.parts = grad_in_parts(a);
     if (p.parts) {
         const size_t tile = parts_tile_bytes(parts_steps(a.D)), keys = (size_t)a.N * a.kv_heads * p.key_tiles, rows = (size_t)a.N * a.heads * p.row_tiles;
-        for (int x = 0; x < 7; ++x) p.images[x] = take((x < 3 ? keys : rows) * tile);      // k, k, v; q, q, dout, dout
+        for (int x = 0; x < 4; ++x) p.images[x] = take((x < 2 ? keys : rows) * tile);      // k, v; q, dout
         for (int x = 0; x < 4; ++x) p.exps[x] = take((x < 2 ? keys : rows) * sizeof(int));
         // six workgroups a compute unit: by heads that share a key head, then by rows of 256 at least
         const long want = (6L * device_cus() + (long)keys - 1) / (long)keys;
@@ -377,12 +377,11 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
         int *const exps[] = {(int *)(at + p.exps[0]), (int *)(at + p.exps[1]), (int *)(at + p.exps[2]), (int *)(at + p.exps[3])};
         PartsArgs args{};
         args.count = 4;
-        args.t[0] = PartsTensor{k, x.ks, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[0], at + p.images[1], exps[0], 0};
-        args.t[1] = PartsTensor{v, x.vs, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[2], nullptr, exps[1], 0};
-        args.t[2] = PartsTensor{q, x.qs, a->heads, a->Sq, p.row_tiles, 1, at + p.images[3], at + p.images[4], exps[2], 0};
-        args.t[3] = PartsTensor{dout, x.dos, a->heads, a->Sq, p.row_tiles, 1, at + p.images[5], at + p.images[6], exps[3], 0};
-        x.k_tok = at + p.images[0]; x.k_chan = at + p.images[1]; x.v_tok = at + p.images[2];
-        x.q_tok = at + p.images[3]; x.q_chan = at + p.images[4]; x.do_tok = at + p.images[5]; x.do_chan = at + p.images[6];
+        args.t[0] = PartsTensor{k, x.ks, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[0], exps[0], 0};
+        args.t[1] = PartsTensor{v, x.vs, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[1], exps[1], 0};
+        args.t[2] = PartsTensor{q, x.qs, a->heads, a->Sq, p.row_tiles, 1, at + p.images[2], exps[2], 0};
+        args.t[3] = PartsTensor{dout, x.dos, a->heads, a->Sq, p.row_tiles, 1, at + p.images[3], exps[3], 0};
+        x.k_tok = at + p.images[0]; x.v_tok = at + p.images[1]; x.q_tok = at + p.images[2]; x.do_tok = at + p.images[3];
         x.k_exps = exps[0]; x.v_exps = exps[1]; x.q_exps = exps[2]; x.do_exps = exps[3];
         x.part_o = (float *)(at + p.dkv_at);
         e = launch_make_parts(x, args, x.vec, s);

@@ -9,11 +9,11 @@
 // [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-25 times the tile's largest still has 22 bits, and below that the error is
 // 2^-35 of the largest one. Magnitudes beyond fp32's own range apart, no input is out of reach; infinities and NaN become NaN.
 //
-// attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, lane l = 16 g + m with its eight values behind each other,
-// so a wave reads an operand as one linear kilobyte, and copies of tiles into LDS are linear too:
-//   tokens in lanes   [16 tokens][32 channels][part]: lane (m, g) holds channels 8g .. 8g+7 of token m
-//   channels in lanes [32 tokens][16 channels][part]: lane (m, g) holds tokens 4g .. 4g+3 and 16+4g .. 16+4g+3 of channel m -- the order in
-//                     which two results of 16 tokens each lie in a lane's registers, which are the other operand of that product.
+// attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, [16 tokens][32 channels][part], lane (m, g) with its eight
+// values behind each other (channels 8g .. 8g+7 of token m), so a wave reads an operand with tokens in lanes as one linear kilobyte, and copies of tiles into LDS
+// are linear too. The operand with channels in lanes is read from the same block by the transposing reads of LDS (across): lane (m, g) gets tokens
+// 4g .. 4g+3 and 16+4g .. 16+4g+3 of channel m, the order in which two results of 16 tokens each lie in a lane's registers, which are the other operand of
+// that product.
 #pragma once
 #include "attn_row.h"
 
@@ -83,7 +83,7 @@ struct PartsTensor {
     const float *p;
     TokenStrides s;
     int heads, tokens, tiles, rows;            // rows: not keys but queries (their masks: rows of lse = -inf are left out)
-    char *by_token, *by_channel;               // images, or null
+    char *image;
     int *exps;                                 // [N * heads][tiles]
     unsigned first_block;
 };
@@ -91,6 +91,39 @@ struct PartsArgs {
     PartsTensor t[4];
     int count;
 };
+
+// A lane's place in a block as the operand with tokens in lanes. The sixteen tokens of odd groups of channels stand in another order, their fours the other
+// way round, for the transposing reads: thirty-two lanes take eight tokens of two groups there, which then are in different banks.
+__device__ __forceinline__ int token_place(int m, int g) { return (16 * g + (m ^ (g & 1) * 12)) * 16; }
+// Left operand with channels in lanes: of the 32 tokens of pair `pair`, the 16 channels of block d, one part. at: a tile in LDS, this lane's place in it.
+__device__ __forceinline__ int across_place(int m, int g) { return ((m & 2) << 7) + ((4 * g + (m >> 2)) ^ (m >> 1 & 1) * 12) * 16 + (m & 1) * 8; }
+template <int STEPS>
+__device__ __forceinline__ half8 across(const char *at, int pair, int d, int part)
+{
+    typedef short short4v __attribute__((ext_vector_type(4)));
+    typedef __attribute__((address_space(3))) short4v *lds4;
+    const char *const from = at + (2 * pair * STEPS + d / 2) * 2048 + part * 1024 + (d & 1) * 512;
+    const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)from), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(from + STEPS * 2048));
+    return __builtin_bit_cast(half8, __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+// acc += channels of 32 tokens times results in two parts, part by part over up to four blocks of channels.
+template <int STEPS>
+__device__ __forceinline__ void products_across(floatx4 (&acc)[2 * STEPS], const char *at, int pair, half8 b_hi, half8 b_lo)
+{
+    constexpr int DT = 2 * STEPS, ND = DT < 4 ? DT : 4;
+#pragma unroll
+    for (int d0 = 0; d0 < DT; d0 += ND) {
+        half8 hi[ND], lo[ND];
+#pragma unroll
+        for (int d = 0; d < ND && d0 + d < DT; ++d) lo[d] = across<STEPS>(at, pair, d0 + d, 1);
+#pragma unroll
+        for (int d = 0; d < ND && d0 + d < DT; ++d) hi[d] = across<STEPS>(at, pair, d0 + d, 0);
+#pragma unroll
+        for (int part = 0; part < 3; ++part)
+#pragma unroll
+            for (int d = 0; d < ND && d0 + d < DT; ++d) acc[d0 + d] = mfma16(part == 0 ? lo[d] : hi[d], part == 1 ? b_lo : b_hi, acc[d0 + d]);
+    }
+}
 
 constexpr size_t parts_tile_bytes(int steps) { return (size_t)64 * 32 * steps * 4; }
 constexpr int parts_steps(int D) { return (D + 31) / 32; }

@@ -8,7 +8,7 @@ namespace {
 
 extern __shared__ __attribute__((aligned(1024))) char parts_lds[];
 
-// Tiles of 64 tokens of up to four tensors, one workgroup each: the largest magnitude, then both images. A thread takes 4 tokens x 4 channels.
+// Tiles of 64 tokens of up to four tensors, one workgroup each: the largest magnitude, then the image. A thread takes 4 tokens x 4 channels.
 template <int STEPS, bool VEC>
 __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs args)
 {
@@ -54,23 +54,12 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
                 hi[i][d] = (_Float16)y;
                 lo[i][d] = (_Float16)(y - (float)hi[i][d]);
             }
-        if (t.by_token) {
-            // token 4 tq + i of block tq / 4, channels 4 dq .. : half of lane (token, dq / 2)'s eight of step dq / 8
-            char *to = t.by_token + (size_t)id * parts_tile_bytes(STEPS) + ((tq >> 2) * STEPS + (dq >> 3)) * 2048 + (dq >> 1 & 3) * 256 + (dq & 1) * 8;
+        // token 4 tq + i of block tq / 4, channels 4 dq .. : half of lane (token, dq / 2)'s eight of step dq / 8
+        char *to = t.image + (size_t)id * parts_tile_bytes(STEPS) + ((tq >> 2) * STEPS + (dq >> 3)) * 2048 + token_place((tq & 3) * 4, dq >> 1 & 3) + (dq & 1) * 8;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                *reinterpret_cast<half4 *>(to + ((tq & 3) * 4 + i) * 16) = hi[i];
-                *reinterpret_cast<half4 *>(to + ((tq & 3) * 4 + i) * 16 + 1024) = lo[i];
-            }
-        }
-        if (t.by_channel) {
-            // channel 4 dq + d, tokens 4 tq ..: lane (channel, tq & 3)'s first or second four, by whether the block of 16 is even
-            char *to = t.by_channel + (size_t)id * parts_tile_bytes(STEPS) + ((tq >> 3) * (2 * STEPS) + (dq >> 2)) * 2048 + (tq & 3) * 256 + (tq >> 2 & 1) * 8;
-#pragma unroll
-            for (int d = 0; d < 4; ++d) {
-                *reinterpret_cast<half4 *>(to + ((dq & 3) * 4 + d) * 16) = half4{hi[0][d], hi[1][d], hi[2][d], hi[3][d]};
-                *reinterpret_cast<half4 *>(to + ((dq & 3) * 4 + d) * 16 + 1024) = half4{lo[0][d], lo[1][d], lo[2][d], lo[3][d]};
-            }
+        for (int i = 0; i < 4; ++i) {
+            *reinterpret_cast<half4 *>(to + i * 16) = hi[i];
+            *reinterpret_cast<half4 *>(to + i * 16 + 1024) = lo[i];
         }
     }
 }
@@ -142,7 +131,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     }
     const int v_exp = __builtin_amdgcn_readfirstlane(words[2]);
 
-    const char *k_image = a.k_tok + ((size_t)n * kv + key_head) * tiles * IMAGE, *v_image = a.v_chan + ((size_t)n * kv + key_head) * tiles * IMAGE;
+    const char *k_image = a.k_tok + ((size_t)n * kv + key_head) * tiles * IMAGE, *v_image = a.v_tok + ((size_t)n * kv + key_head) * tiles * IMAGE;
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)parts_lds;
     const auto copy = [&](const char *image, int j0, unsigned to) {
 #pragma unroll
@@ -175,7 +164,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
         wait_vmcnt<0>();
         __syncthreads();
         copy(v_image, j0, IMAGE);
-        const char *kt = parts_lds + lane * 16, *vt = kt + IMAGE;
+        const char *kt = parts_lds + token_place(m, g), *vt = parts_lds + IMAGE + across_place(m, g);
 
         // (products of a step part by part over all results: one that adds to the one before it would wait for it)
         floatx4 s[4] = {};
@@ -183,10 +172,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
         for (int st = 0; st < STEPS; ++st) {
             half8 k_hi[4], k_lo[4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) {
-                k_lo[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048 + 1024);
-                k_hi[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048);
-            }
+            for (int b = 0; b < 4; ++b) k_lo[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048 + 1024);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) k_hi[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048);
 #pragma unroll
             for (int part = 0; part < 3; ++part)
 #pragma unroll
@@ -216,21 +204,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
         __syncthreads();
         if (j0 + 64 < end) copy(k_image, j0 + 64, 0);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-            for (int d0 = 0; d0 < DT; d0 += 4) {
-                constexpr int ND = DT < 4 ? DT : 4;
-                half8 v_hi[ND], v_lo[ND];
-#pragma unroll
-                for (int d = 0; d < ND && d0 + d < DT; ++d) {
-                    v_lo[d] = *reinterpret_cast<const half8 *>(vt + (b * DT + d0 + d) * 2048 + 1024);
-                    v_hi[d] = *reinterpret_cast<const half8 *>(vt + (b * DT + d0 + d) * 2048);
-                }
-#pragma unroll
-                for (int part = 0; part < 3; ++part)
-#pragma unroll
-                    for (int d = 0; d < ND && d0 + d < DT; ++d) o[d0 + d] = mfma16(part == 0 ? v_lo[d] : v_hi[d], part == 1 ? p_lo[b] : p_hi[b], o[d0 + d]);
-            }
+        for (int b = 0; b < 2; ++b) products_across<STEPS>(o, vt, b, p_hi[b], p_lo[b]);
     }
 
     const AttnArgs z = late_args();

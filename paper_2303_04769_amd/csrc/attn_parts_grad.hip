@@ -46,10 +46,9 @@ __device__ __forceinline__ void products(floatx4 (&c)[NB], const char *lds, int 
 {
     half8 hi[NB], lo[NB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-        lo[b] = *reinterpret_cast<const half8 *>(lds + b * stride + 1024);
-        hi[b] = *reinterpret_cast<const half8 *>(lds + b * stride);
-    }
+    for (int b = 0; b < NB; ++b) lo[b] = *reinterpret_cast<const half8 *>(lds + b * stride + 1024);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) hi[b] = *reinterpret_cast<const half8 *>(lds + b * stride);
 #pragma unroll
     for (int part = 0; part < 3; ++part)
 #pragma unroll
@@ -180,7 +179,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     }
     half8 q_hi[STEPS], q_lo[STEPS], d_hi[STEPS], d_lo[STEPS];
     {
-        const size_t at = at_tile * IMAGE + wave * STEPS * 2048 + lane * 16;
+        const size_t at = at_tile * IMAGE + wave * STEPS * 2048 + token_place(m, g);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             q_hi[s] = *reinterpret_cast<const half8 *>(a.q_tok + at + s * 2048);
@@ -210,8 +209,17 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     const unsigned lds = lds_address(parts_lds);
     if (begin < end) {
         copy_image(a.k_tok + (first_tile + begin / 64) * IMAGE, IMAGE, lds);
-        copy_image(a.v_tok + (first_tile + begin / 64) * IMAGE, IMAGE, lds + IMAGE);
+        copy_image(a.v_tok + (first_tile + begin / 64) * IMAGE, IMAGE, lds + 2 * IMAGE);
     }
+    // The next tile's keys are copied into the other of two buffers all the while, its values behind the barrier that ends the products with these.
+    unsigned now = 0;
+    const auto next_keys = [&](int j0) {
+        now ^= IMAGE;
+        if (j0 + 64 < end) copy_image(a.k_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds + now);
+    };
+    const auto next_values = [&](int j0) {
+        if (j0 + 64 < end) copy_image(a.v_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds + 2 * IMAGE);
+    };
 
     // LDS behind the three tiles: the expanded bias; its gradient's sums by offset, as often as there are waves times 4, 2 or 1 (bias_copies)
     const int size = 2 * a.reach + 1;
@@ -241,13 +249,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
         for (int j0 = begin; j0 < end; j0 += 64) {
             wait_vmcnt<0>();
             __syncthreads();
-            copy_image(a.k_chan + (first_tile + j0 / 64) * IMAGE, IMAGE, lds + 2 * IMAGE);
-            wait_vmcnt<0>();
+            next_keys(j0);
             __syncthreads();
-            if (j0 + 64 < end) {
-                copy_image(a.k_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds);
-                copy_image(a.v_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds + IMAGE);
-            }
+            next_values(j0);
         }
     else
     for (int j0 = begin; j0 < end; j0 += 64) {
@@ -255,16 +259,16 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
         stage_keys<64>(a, n, j0, key_code, key_doc);
         wait_vmcnt<0>();
         __syncthreads();
-        copy_image(a.k_chan + (first_tile + j0 / 64) * IMAGE, IMAGE, lds + 2 * IMAGE);
-        const char *kt = parts_lds + lane * 16;
+        const char *kt = parts_lds + now, *vt = parts_lds + 2 * IMAGE + token_place(m, g);
+        next_keys(j0);
         floatx4 s[4] = {}, dp_half[2] = {}, dp_turned[2] = {};
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
-            products(s, kt + st * 2048, STEPS * 2048, q_hi[st], q_lo[st]);
-            products(dp_half, kt + IMAGE + st * 2048, STEPS * 2048, d_hi[st], d_lo[st]);
+            products(s, kt + token_place(m, g) + st * 2048, STEPS * 2048, q_hi[st], q_lo[st]);
+            products(dp_half, vt + st * 2048, STEPS * 2048, d_hi[st], d_lo[st]);
             // half of the keys with dO's sign turned: the matrix instructions round their sums to one side, by a tenth of a spacing, and over a row
             // that would add up in the bias's gradient, which is what is left of sums that cancel
-            products(dp_turned, kt + IMAGE + (2 * STEPS + st) * 2048, STEPS * 2048, -d_hi[st], -d_lo[st]);
+            products(dp_turned, vt + (2 * STEPS + st) * 2048, STEPS * 2048, -d_hi[st], -d_lo[st]);
         }
         const floatx4 dp[4] = {dp_half[0], dp_half[1], -dp_turned[0], -dp_turned[1]};
         const float dp_in = ldexpf(1.f, v_exp + d_exp);
@@ -301,14 +305,10 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
         for (int b = 0; b < 4; ++b) s[b] *= f;
 #pragma unroll
         for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], hi_[b], lo_[b]);
-        wait_vmcnt<0>();
         __syncthreads();
-        if (j0 + 64 < end) {
-            copy_image(a.k_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds);
-            copy_image(a.v_tok + (first_tile + j0 / 64 + 1) * IMAGE, IMAGE, lds + IMAGE);
-        }
+        next_values(j0);
 #pragma unroll
-        for (int b = 0; b < 2; ++b) products(dq, kt + 2 * IMAGE + b * DT * 2048, 2048, hi_[b], lo_[b]);
+        for (int b = 0; b < 2; ++b) products_across<STEPS>(dq, kt + across_place(m, g), b, hi_[b], lo_[b]);
     }
     const AttnArgs z = late_args();
     if (sums) {
@@ -341,12 +341,11 @@ template <int STEPS, int MODE>
 __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(AttnArgs a)
 {
     constexpr int DT = 2 * STEPS, IMAGE = (int)parts_tile_bytes(STEPS), HALF = IMAGE / 2;
-    __shared__ alignas(16) float row_lse[32];
-    __shared__ alignas(16) float row_delta[32];
-    __shared__ alignas(16) int row_p[32];
-    __shared__ alignas(16) int row_code[32];
-    __shared__ alignas(16) int row_bound[33];      // [32]: the smallest
-    __shared__ alignas(16) int row_doc[33];        // [32]: of all rows, or -3
+    struct Rows {
+        float lse[32], delta[32];
+        int p[32], code[32], bound[36], doc[36];       // bound[32]: the smallest; doc[32]: of all rows, or -3
+    };
+    __shared__ alignas(16) Rows rows_of[2];
     __shared__ int words[3];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -359,7 +358,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
     const size_t at_tile = ((size_t)n * kv + key_head) * a.key_tiles + tile;
     half8 k_hi[STEPS], k_lo[STEPS], v_hi[STEPS], v_lo[STEPS];
     {
-        const size_t at = at_tile * IMAGE + wave * STEPS * 2048 + lane * 16;
+        const size_t at = at_tile * IMAGE + wave * STEPS * 2048 + token_place(m, g);
 #pragma unroll
         for (int s = 0; s < STEPS; ++s) {
             k_hi[s] = *reinterpret_cast<const half8 *>(a.k_tok + at + s * 2048);
@@ -424,47 +423,45 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         }
         const size_t first_row = ((size_t)n * a.heads + head) * a.Sq, first_tile = ((size_t)n * a.heads + head) * a.row_tiles;
         const auto at = [&](int i0) { return (first_tile + i0 / 64) * IMAGE + (i0 & 32 ? HALF : 0); };
-        copy_image(a.q_tok + at(begin), HALF, lds);
-        copy_image(a.do_tok + at(begin), HALF, lds + HALF);
+        // While a tile is worked on, the next one is copied into the other of two buffers; one barrier a tile.
+        unsigned now = 0;
+        const auto copy_rows = [&](int i0, unsigned to) {
+            copy_image(a.q_tok + at(i0), HALF, lds + to);
+            copy_image(a.do_tok + at(i0), HALF, lds + to + HALF);
+        };
+        copy_rows(begin, 0);
         if (idle)
-            for (int i0 = begin; i0 < end; i0 += 32) {
+            for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
                 wait_vmcnt<0>();
                 __syncthreads();
-                copy_image(a.q_chan + at(i0), HALF, lds + 2 * HALF);
-                copy_image(a.do_chan + at(i0), HALF, lds + 3 * HALF);
-                wait_vmcnt<0>();
-                __syncthreads();
-                if (i0 + 32 < end) {
-                    copy_image(a.q_tok + at(i0 + 32), HALF, lds);
-                    copy_image(a.do_tok + at(i0 + 32), HALF, lds + HALF);
-                }
+                if (i0 + 32 < end) copy_rows(i0 + 32, now ^ 2 * HALF);
             }
         else
-        for (int i0 = begin; i0 < end; i0 += 32) {
+        for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
+            Rows &rows = rows_of[now != 0];
             const int q_exp = a.q_exps[first_tile + i0 / 64], d_exp = a.do_exps[first_tile + i0 / 64];
             if (threadIdx.x < 32) {
                 const int i = i0 + threadIdx.x, ii = min(i, a.Sq - 1);
                 const RowState row(a, im, n, i, head);
                 const float lse = i < a.Sq ? a.lse_in[first_row + ii] : -kInf;
                 const bool dead = lse == -kInf;
-                row_lse[threadIdx.x] = dead ? kInf : lse * kLog2e;
-                row_delta[threadIdx.x] = dead ? 0.f : a.delta[first_row + ii];
-                row_p[threadIdx.x] = row.p;
-                row_code[threadIdx.x] = row.code;
-                row_bound[threadIdx.x] = row.bound;
-                row_doc[threadIdx.x] = row.doc;
+                rows.lse[threadIdx.x] = dead ? kInf : lse * kLog2e;
+                rows.delta[threadIdx.x] = dead ? 0.f : a.delta[first_row + ii];
+                rows.p[threadIdx.x] = row.p;
+                rows.code[threadIdx.x] = row.code;
+                rows.bound[threadIdx.x] = row.bound;
+                rows.doc[threadIdx.x] = row.doc;
                 int least = row.bound;
                 for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor(least, d));
-                row_bound[32] = least;
-                row_doc[32] = -3;
+                rows.bound[32] = least;
+                rows.doc[32] = -3;
                 const int first = __builtin_amdgcn_readfirstlane(row.doc);
-                if (__all(row.doc == first)) row_doc[32] = first;
+                if (__all(row.doc == first)) rows.doc[32] = first;
             }
             wait_vmcnt<0>();
             __syncthreads();
-            copy_image(a.q_chan + at(i0), HALF, lds + 2 * HALF);
-            copy_image(a.do_chan + at(i0), HALF, lds + 3 * HALF);
-            const char *qt = parts_lds + lane * 16;
+            if (i0 + 32 < end) copy_rows(i0 + 32, now ^ 2 * HALF);
+            const char *tile_at = parts_lds + now, *qt = tile_at + token_place(m, g);
             floatx4 s[2] = {}, dp[2] = {};
 #pragma unroll
             for (int st = 0; st < STEPS; ++st) {
@@ -486,16 +483,16 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             bool near = false;
             float base = 0.f;
             if ((MODE & 4) && a.table) {
-                const bool all_lo = __all(code - row_code[0] <= -a.reach), all_hi = __all(code - row_code[31] >= a.reach);
+                const bool all_lo = __all(code - rows.code[0] <= -a.reach), all_hi = __all(code - rows.code[31] >= a.reach);
                 near = !all_lo && !all_hi;
                 base = all_lo ? far_lo : all_hi ? far_hi : 0.f;
             }
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const floatx4 l4 = *reinterpret_cast<const floatx4 *>(row_lse + 16 * b + 4 * g);
+                const floatx4 l4 = *reinterpret_cast<const floatx4 *>(rows.lse + 16 * b + 4 * g);
                 floatx4 u = base - l4;
                 if ((MODE & 2) && a.slopes) {
-                    const int4 p4 = *reinterpret_cast<const int4 *>(row_p + 16 * b + 4 * g);
+                    const int4 p4 = *reinterpret_cast<const int4 *>(rows.p + 16 * b + 4 * g);
                     u.x = fmaf(-slope, fabsf((float)(p4.x - j)), u.x);
                     u.y = fmaf(-slope, fabsf((float)(p4.y - j)), u.y);
                     u.z = fmaf(-slope, fabsf((float)(p4.z - j)), u.z);
@@ -504,7 +501,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, u[e]);
             }
-            const int first = code - row_code[0] - 4 * g + a.reach;
+            const int first = code - rows.code[0] - 4 * g + a.reach;
             if (near && bias && a.width == 1 && __all((first <= 2 * a.reach) & (first >= 19))) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b)
@@ -513,7 +510,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             } else if (near) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int4 c4 = *reinterpret_cast<const int4 *>(row_code + 16 * b + 4 * g);
+                    const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
                     const int codes[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
@@ -522,20 +519,20 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
                     }
                 }
             }
-            if (!__all(j_raw < row_bound[32])) {
+            if (!__all(j_raw < rows.bound[32])) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int4 x = *reinterpret_cast<const int4 *>(row_bound + 16 * b + 4 * g);
+                    const int4 x = *reinterpret_cast<const int4 *>(rows.bound + 16 * b + 4 * g);
                     s[b].x = j_raw < x.x ? s[b].x : -kInf;
                     s[b].y = j_raw < x.y ? s[b].y : -kInf;
                     s[b].z = j_raw < x.z ? s[b].z : -kInf;
                     s[b].w = j_raw < x.w ? s[b].w : -kInf;
                 }
             }
-            if (a.docs && !__all(row_doc[32] == doc)) {
+            if (a.docs && !__all(rows.doc[32] == doc)) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int4 x = *reinterpret_cast<const int4 *>(row_doc + 16 * b + 4 * g);
+                    const int4 x = *reinterpret_cast<const int4 *>(rows.doc + 16 * b + 4 * g);
                     s[b].x = x.x == doc ? s[b].x : -kInf;
                     s[b].y = x.y == doc ? s[b].y : -kInf;
                     s[b].z = x.z == doc ? s[b].z : -kInf;
@@ -545,7 +542,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             const float lift = ldexpf(1.f, max(-120, 14 + d_exp - d_most));
 #pragma unroll
             for (int b = 0; b < 2; ++b) {
-                const floatx4 d4 = *reinterpret_cast<const floatx4 *>(row_delta + 16 * b + 4 * g);
+                const floatx4 d4 = *reinterpret_cast<const floatx4 *>(rows.delta + 16 * b + 4 * g);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float p = __builtin_amdgcn_exp2f(s[b][e]);
@@ -564,14 +561,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             half8 p_hi, p_lo, s_hi, s_lo;
             split_results(s[0], s[1], p_hi, p_lo);
             split_results(dp[0], dp[1], s_hi, s_lo);
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (i0 + 32 < end) {
-                copy_image(a.q_tok + at(i0 + 32), HALF, lds);
-                copy_image(a.do_tok + at(i0 + 32), HALF, lds + HALF);
-            }
-            products(dv, qt + 3 * HALF, 2048, p_hi, p_lo);
-            products(dk, qt + 2 * HALF, 2048, s_hi, s_lo);
+            products_across<STEPS>(dv, tile_at + HALF + across_place(m, g), 0, p_hi, p_lo);
+            products_across<STEPS>(dk, tile_at + across_place(m, g), 0, s_hi, s_lo);
         }
     }
     const AttnArgs z = late_args();

@@ -35,7 +35,7 @@ struct AttnArgs {
     float *part_o;
     float2 *part_ml;              // splits > 1: results before joining, and their (maximum, sum)
     // values in two parts (attn_parts.h): images of keys and values, their powers of two
-    const char *k_tok, *k_chan, *v_tok, *v_chan, *q_tok, *q_chan, *do_tok, *do_chan;
+    const char *k_tok, *v_tok, *q_tok, *do_tok;
     const int *k_exps, *v_exps, *q_exps, *do_exps;
     // gradient
     const float *dout, *lse_in;

@@ -353,6 +353,8 @@ LARGE = {
     "buckets too many for LDS": dict(Sq=640, heads=4, D=64, bias="wide"), "heads of 16": dict(Sq=1300, heads=4, D=16, bias="log"), "heads of 8": dict(Sq=1300, heads=8, D=8),
     "heads of 40": dict(Sq=800, heads=4, D=40, Cb=8, bias="log", causal=True), "heads of 37": dict(Sq=850, heads=4, D=37, Cb=37), "heads of 80": dict(Sq=600, heads=4, D=80),
     "heads of 96": dict(Sq=540, heads=4, D=96, bias="log"), "heads of 128": dict(Sq=480, heads=4, D=128, causal=True, slopes=True, cap=9.0), "channels last": dict(Sq=640, heads=4, D=64, Cb=256),
+    "causal, sixty-four heads": dict(N=4, Sq=600, heads=16, kv=4, D=16, causal=True, bias="log"),
+    "causal, twenty-seven heads": dict(Sq=1220, heads=27, kv=9, D=8, Cb=8, causal=True), "small images": dict(N=40, Sq=196, heads=4, D=32, bias=(14, 14)),
     "few rows": dict(Sq=70, Sk=12000, heads=2, D=64, bias="log"), "everything": dict(N=3, Sq=400, cap=10.0, bias="log", slopes=True, causal=True, prefix=[50, 0, 300],
         lengths=[400, 64, 290], docs=_docs(3, 400, [[150, 235], [400], [10, 10, 370]]), heads=6, kv=3, D=48),
 }
