@@ -82,7 +82,8 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
     }
 
     floatx4 o[DT] = {};
-    float top = -kInf, sum = 0.f;
+    Reference top(a, row, begin, end);
+    float sum = 0.f;
     floatx4 kx[T::kQuads], vx[T::kQuads];
     const auto fetch = [&](int j0) {
         const auto on = [&](int j) { return j0 + j < im.len; };
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
                 for (int e = 0; e < 4; ++e) s[b] = mfma(x[e], q[4 * c + e], s[b]);
             }
 
-        finish_scores<7>(a, s, row, 0, reference_of(top), j0, key_code, key_doc, g, bias, far_lo, far_hi);
+        finish_scores<7>(a, s, row, 0, top.at, j0, key_code, key_doc, g, bias, far_lo, far_hi);
 
         raise_top(s, top, sum, o);
 #pragma unroll
@@ -157,7 +158,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
                             if (d + e < a.D) to[d + e] = y[e];
                     }
                 }
-            if (g == 0) a.part_ml[part] = float2{top, sum};
+            if (g == 0) a.part_ml[part] = float2{top.maximum(), sum};
         } else {
             const float inv = sum == 0.f ? 0.f : 1.f / sum;      // a row that saw nothing: zeros
             float *token = const_cast<float *>(token_at(a.o, a.os, n, i));
@@ -166,7 +167,7 @@ __global__ void __launch_bounds__(256, 2) attn_rows(AttnArgs a)
 #pragma unroll
                 for (int x = 0; x < VD; ++x)
                     store_quad<VEC>(a, a.os, token, head * a.D, grp * 16 * VD + 4 * g * VD + 4 * x, result_quad<DT>(o, grp, x) * inv);
-            if (a.lse && g == 0) a.lse[((size_t)n * a.heads + head) * a.Sq + i] = sum == 0.f ? -kInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+            if (a.lse && g == 0) a.lse[((size_t)n * a.heads + head) * a.Sq + i] = sum == 0.f ? -kInf : (top.at + __builtin_amdgcn_logf(sum)) * kLn2;
         }
     }
     for (unsigned left = columns; left; left &= left - 1) {

@@ -226,7 +226,7 @@ bool grad_in_parts(const small_attn &a)
     return a.D <= 128 && parts_work(a) && (!a.table || a.reach < 2048);
 }
 
-// The gradient's workspace: delta [N][heads][Sq]; with a table its sums by offset, of every tile of rows and of every head; in parts the images of keys, values,
+// The gradient's workspace: delta and share [N][heads][Sq]; with a table its sums by offset, of every tile of rows and of every head; in parts the images of keys, values,
 // queries and dout, their powers of two, and dk's and dv's parts where a key tile's rows are shared out. Places in bytes.
 struct GradPlan {
     bool parts;
@@ -241,7 +241,7 @@ GradPlan plan_grad(const small_attn &a)
     p.splits = p.row_parts = 1;
     size_t end = 0;
     const auto take = [&](size_t bytes) { const size_t at = end; end += (bytes + 255) / 256 * 256; return at; };
-    take((size_t)a.N * a.heads * a.Sq * sizeof(float));
+    take(2 * (size_t)a.N * a.heads * a.Sq * sizeof(float));
     if (a.table) {
         const size_t size = 2 * (size_t)a.reach + 1;
         p.part_at = take((size_t)a.N * a.heads * p.row_tiles * size * sizeof(float));
@@ -362,6 +362,7 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     x.by_code = make_fastdiv(2 * a->width - 1);
     char *const at = (char *)workspace;
     x.delta = (float *)at;
+    x.share = x.delta + (size_t)a->N * a->heads * a->Sq;
     x.part_bias = dtable ? (float *)(at + p.part_at) : nullptr;
     x.vec = attn_vec(*a, {q, k, v, out, dout, dq, dk, dv}) && grad_vec(*a);
     const double size = 2.0 * a->reach + 1;

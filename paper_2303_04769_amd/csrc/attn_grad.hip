@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
         acc = a.bias_acc_lds ? at_lds + 64 * (KT + 1) : part;
         for (int x = threadIdx.x; x < size; x += 256) acc[x] = 0.f;       // (behind the next barrier a place is one thread's until the loop's end)
     }
-    float sum_lo = 0.f, sum_hi = 0.f;
+    float sum_lo = 0.f, sum_hi = 0.f, total = 0.f;
 
     const Scorer sc(a);
     floatx4 dq[DT] = {};
@@ -146,7 +146,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
                 const int j = j0 + 16 * b + 4 * g + e;
                 const float core = score_core(a, sc, s[b][e]);
                 float t = score_of(a, sc, core);
-                if (a.slopes) t = fmaf(-row.slope, fabsf((float)(row.p - j)), t);
+                t += a.slopes ? fmaf(-row.slope, fabsf((float)(row.p - j)), -lse2) : -lse2;       // (large ones cancel unrounded)
                 if (a.table) {
                     if (all_lo || all_hi) t += all_lo ? far_lo : far_hi;
                     else {
@@ -154,9 +154,11 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
                         t += bias ? bias[at] : bias_gather(a, head, at);
                     }
                 }
-                const float p = __builtin_amdgcn_exp2f(t - lse2);
+                const float p = __builtin_amdgcn_exp2f(t);
                 float ds = p * (dp[b][e] - delta);
-                if (edge) ds = row.sees(j, docs[e], true) ? ds : 0.f;
+                const bool seen = !edge | row.sees(j, docs[e], true);
+                ds = seen ? ds : 0.f;
+                total += seen ? p : 0.f;
                 if (part) {
                     const int off = codes[e] - row.code;
                     sum_lo += off <= -a.reach ? ds : 0.f;
@@ -207,13 +209,15 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
             part[x] = y;
         }
     }
+    const float share = share_of(a, total);
     if (i_raw < a.Sq) {
+        if (a.slopes && g == 0) a.share[((size_t)n * a.heads + head) * a.Sq + i] = share;
         float *token = const_cast<float *>(token_at(a.dq, a.dqs, n, i));
 #pragma unroll
         for (int grp = 0; grp < GR; ++grp)
 #pragma unroll
             for (int x = 0; x < VD; ++x)
-                store_quad<VEC>(a, a.dqs, token, head * a.D, grp * 16 * VD + 4 * g * VD + 4 * x, result_quad<DT>(dq, grp, x) * a.scale);
+                store_quad<VEC>(a, a.dqs, token, head * a.D, grp * 16 * VD + 4 * g * VD + 4 * x, result_quad<DT>(dq, grp, x) * (a.scale * share));
     }
 }
 
@@ -225,6 +229,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
     __shared__ float qt[T::kFloats], dt[T::kFloats];
     __shared__ alignas(16) float row_lse[KT];
     __shared__ alignas(16) float row_delta[KT];
+    __shared__ alignas(16) float row_share[KT];
     __shared__ alignas(16) int row_p[KT];
     __shared__ alignas(16) int row_code[KT];
     __shared__ alignas(16) int row_bound[KT];
@@ -285,7 +290,8 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
             far_lo = bias_gather(a, head, 0);
             far_hi = bias_gather(a, head, 2 * a.reach);
         }
-        const float *lse_in = a.lse_in + ((size_t)n * a.heads + head) * a.Sq, *delta_in = a.delta + ((size_t)n * a.heads + head) * a.Sq;
+        const float *lse_in = a.lse_in + ((size_t)n * a.heads + head) * a.Sq, *delta_in = a.delta + ((size_t)n * a.heads + head) * a.Sq,
+                    *share_in = a.share + ((size_t)n * a.heads + head) * a.Sq;
         const auto fetch = [&](int i0) {
             // (rows that saw nothing are not read either)
             const auto on = [&](int i) { return i0 + i < a.Sq && lse_in[min(i0 + i, a.Sq - 1)] != -kInf; };
@@ -303,6 +309,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
                 const float lse = i < a.Sq ? lse_in[ii] : -kInf;
                 row_lse[threadIdx.x] = lse == -kInf ? kInf : lse * kLog2e;
                 row_delta[threadIdx.x] = lse == -kInf ? 0.f : delta_in[ii];
+                row_share[threadIdx.x] = a.slopes ? share_in[ii] : 1.f;
                 row_p[threadIdx.x] = row.p;
                 row_code[threadIdx.x] = row.code;
                 row_bound[threadIdx.x] = row.bound;
@@ -327,6 +334,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const floatx4 l4 = *reinterpret_cast<const floatx4 *>(row_lse + 16 * b + 4 * g), d4 = *reinterpret_cast<const floatx4 *>(row_delta + 16 * b + 4 * g);
+                const floatx4 h4 = *reinterpret_cast<const floatx4 *>(row_share + 16 * b + 4 * g);
                 const int4 b4 = *reinterpret_cast<const int4 *>(row_bound + 16 * b + 4 * g);
                 const int bounds[4] = {b4.x, b4.y, b4.z, b4.w};
                 int ps[4] = {}, codes[4] = {}, docs[4] = {doc, doc, doc, doc};
@@ -346,7 +354,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
                 for (int e = 0; e < 4; ++e) {
                     const float core = score_core(a, sc, s[b][e]);
                     float t = score_of(a, sc, core);
-                    if (a.slopes) t = fmaf(-slope, fabsf((float)(ps[e] - j)), t);
+                    t += a.slopes ? fmaf(-slope, fabsf((float)(ps[e] - j)), -l4[e]) : -l4[e];
                     if (a.table) {
                         if (all_lo || all_hi) t += all_lo ? far_lo : far_hi;
                         else {
@@ -355,7 +363,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
                         }
                     }
                     const bool seen = (j_raw < bounds[e]) & (docs[e] == doc);
-                    const float p = seen ? __builtin_amdgcn_exp2f(t - l4[e]) : 0.f;
+                    const float p = seen ? __builtin_amdgcn_exp2f(t) * h4[e] : 0.f;
                     const float ds = seen ? p * (dp[b][e] - d4[e]) : 0.f;
                     s[b][e] = p;
                     dp[b][e] = a.cap > 0.f ? ds * fmaf(-core, core, 1.f) : ds;

@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     }
 
     floatx4 o[DT] = {};
-    float top = -kInf, sum = 0.f;
+    Reference top(a, row, begin, end);
+    float sum = 0.f;
     // Values are on their way while scores are computed, the next keys while values are summed; a barrier in front of either, behind which the
     // other's buffer is free.
     for (int j0 = begin; j0 < end; j0 += 64) {
@@ -184,7 +185,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
         // this could lose weights from their own sum, behind it
         const int lift = kLift + v_now - v_exp;
         const float in_exponent = lift >= -40 ? (float)lift : 0.f;
-        finish_scores<MODE>(a, s, row, q_exp + k_exp, reference_of(top) - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
+        finish_scores<MODE>(a, s, row, q_exp + k_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
         raise_top(s, top, sum, o, in_exponent);
         floatx4 part = {};
 #pragma unroll
@@ -235,8 +236,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
                 store_quad<false>(z, z.os, token, head * z.D, 16 * d + 4 * g, y);
             }
         }
-        if (g == 0 && z.splits > 1) z.part_ml[part] = float2{top, all};
-        if (g == 0 && z.splits == 1 && z.lse) z.lse[((size_t)n * z.heads + head) * z.Sq + i] = all == 0.f ? -kInf : (top + __builtin_amdgcn_logf(all)) * kLn2;
+        if (g == 0 && z.splits > 1) z.part_ml[part] = float2{top.maximum(), all};
+        if (g == 0 && z.splits == 1 && z.lse) z.lse[((size_t)n * z.heads + head) * z.Sq + i] = all == 0.f ? -kInf : (top.at + __builtin_amdgcn_logf(all)) * kLn2;
     }
     for (unsigned left = columns; left; left &= left - 1) {
         const int rr = row0 + wave * 16 + __ffs((int)left) - 1;

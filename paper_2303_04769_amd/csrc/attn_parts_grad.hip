@@ -103,22 +103,30 @@ __device__ __forceinline__ void sums_in_line(const floatx4 (&s)[4], int reach, i
         for (int b = 0; b < 5; ++b) *at[b] = was[b] + t[b];
     }
 }
-// In an image of several columns: one key of each lane after another, whose rows, and so offsets, differ (there: the lane has a row of its own).
-__device__ __forceinline__ void sums_in_image(const floatx4 (&s)[4], int reach, const int *key_code, int row_code, bool there, int g, int copies, float *mine, float &lo, float &hi)
+// In an image of several columns: one key of each lane after another, whose rows, and so offsets, differ (there: the lane has a row of its own; keys: how many
+// of the tile's there are).
+__device__ __forceinline__ void sums_in_image(const floatx4 (&s)[4], int reach, const int *key_code, int row_code, bool there, int keys, int g, int copies, float *mine, float &lo, float &hi)
 {
     int at[4][4];
+    const bool inside = keys >= 64 && __all(there & (key_code[0] - row_code > -reach) & (key_code[63] - row_code < reach));
 #pragma unroll
     for (int b = 0; b < 4; ++b) {
         const int4 kc = *reinterpret_cast<const int4 *>(key_code + 16 * b + 4 * g);
         const int off[4] = {kc.x - row_code, kc.y - row_code, kc.z - row_code, kc.w - row_code};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const bool below = off[e] <= -reach, above = (off[e] >= reach) & !below;
-            lo += below ? s[b][e] : 0.f;
-            hi += above ? s[b][e] : 0.f;
-            at[b][e] = (below | above | !there) ? reach + 1 : off[e];
-        }
+        for (int e = 0; e < 4; ++e) at[b][e] = off[e];
     }
+    if (!inside)
+#pragma unroll
+        for (int b = 0; b < 4; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int off = at[b][e];
+                const bool below = off <= -reach, above = (off >= reach) & !below;
+                lo += below ? s[b][e] : 0.f;
+                hi += above ? s[b][e] : 0.f;
+                at[b][e] = (below | above | !there | (16 * b + 4 * g + e >= keys)) ? reach + 1 : off;
+            }
     // (Two lanes that share a place have keys as far apart as their rows, at most 15: of the keys 16 apart all places differ.)
     for (int turn = 0; turn < 4; turn += copies) {
         if ((unsigned)(g - turn) >= (unsigned)copies) continue;
@@ -240,7 +248,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     float *const acc = at_lds, *const mine = acc + (wave * per_wave + (g & (per_wave - 1))) * stride + a.reach;
     if (sums)
         for (int x = threadIdx.x; x < a.bias_copies * stride; x += 256) acc[x] = 0.f;
-    float sum_lo = 0.f, sum_hi = 0.f;
+    float sum_lo = 0.f, sum_hi = 0.f, total = 0.f;
 
     ColumnScale cs;
     floatx4 dq[DT] = {};
@@ -279,6 +287,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const float p = __builtin_amdgcn_exp2f(s[b][e]);
+                if (MODE & 2) total += p;
                 s[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -delta);
             }
         if (sums) {
@@ -291,7 +300,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
                 sum_hi += all_lo ? 0.f : x;
             } else {
                 if (a.width == 1) sums_in_line(s, a.reach, j0 + 4 * g - (im.first + i_raw), m, g, per_wave, mine, sum_lo, sum_hi);
-                else sums_in_image(s, a.reach, key_code, row.code, i_raw < a.Sq, g, per_wave, mine, sum_lo, sum_hi);
+                else sums_in_image(s, a.reach, key_code, row.code, i_raw < a.Sq, a.Sk - j0, g, per_wave, mine, sum_lo, sum_hi);
             }
         }
         if ((MODE & 1) && a.cap > 0.f)
@@ -326,8 +335,10 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             part[x] = y;
         }
     }
+    const float share = (MODE & 2) ? share_of(z, total) : 1.f;
     if (i_raw < z.Sq) {
-        const float back = cs.back(z.scale);
+        if ((MODE & 2) && z.slopes && g == 0) z.share[at_row] = share;
+        const float back = cs.back(z.scale) * share;
         float *token = const_cast<float *>(token_at(z.dq, z.dqs, n, i));
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
@@ -342,7 +353,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
 {
     constexpr int DT = 2 * STEPS, IMAGE = (int)parts_tile_bytes(STEPS), HALF = IMAGE / 2;
     struct Rows {
-        float lse[32], delta[32];
+        float lse[32], delta[32], share[32];
         int p[32], code[32], bound[36], doc[36];       // bound[32]: the smallest; doc[32]: of all rows, or -3
     };
     __shared__ alignas(16) Rows rows_of[2];
@@ -447,8 +458,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
                 const bool dead = lse == -kInf;
                 rows.lse[threadIdx.x] = dead ? kInf : lse * kLog2e;
                 rows.delta[threadIdx.x] = dead ? 0.f : a.delta[first_row + ii];
+                if ((MODE & 2) && a.slopes) rows.share[threadIdx.x] = a.share[first_row + ii];
                 rows.p[threadIdx.x] = row.p;
-                rows.code[threadIdx.x] = row.code;
+                rows.code[threadIdx.x] = i < a.Sq ? row.code : RowState(a, im, n, ii, head).code;
                 rows.bound[threadIdx.x] = row.bound;
                 rows.doc[threadIdx.x] = row.doc;
                 int least = row.bound;
@@ -507,6 +519,16 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
                 for (int b = 0; b < 2; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][e] += bias[first - 16 * b - e];
+            } else if (near && bias && __all((code - rows.code[31] >= -a.reach) & (code - rows.code[0] <= a.reach))) {
+                const int here = a.reach + code;
+#pragma unroll
+                for (int b = 0; b < 2; ++b) {
+                    const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
+                    s[b].x += bias[here - c4.x];
+                    s[b].y += bias[here - c4.y];
+                    s[b].z += bias[here - c4.z];
+                    s[b].w += bias[here - c4.w];
+                }
             } else if (near) {
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -544,8 +566,11 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             for (int b = 0; b < 2; ++b) {
                 const floatx4 d4 = *reinterpret_cast<const floatx4 *>(rows.delta + 16 * b + 4 * g);
 #pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
+                if ((MODE & 2) && a.slopes) s[b] *= *reinterpret_cast<const floatx4 *>(rows.share + 16 * b + 4 * g);
+#pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const float p = __builtin_amdgcn_exp2f(s[b][e]);
+                    const float p = s[b][e];
                     dp[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -d4[e]);
                     s[b][e] = p * lift;
                 }

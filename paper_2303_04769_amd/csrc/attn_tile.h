@@ -39,6 +39,7 @@ struct AttnArgs {
     const int *k_exps, *v_exps, *q_exps, *do_exps;
     // gradient
     const float *dout, *lse_in;
+    float *share;                                            // [N * heads][Sq]: what a row's weights, taken from its lse, are to be multiplied by (with slopes)
     float *dq, *dk, *dv, *delta, *part_bias;                 // part_bias: null, or [N * heads * row_tiles][2 reach + 1]
     TokenStrides dos, dqs, dks, dvs;
     int key_tiles, bias_acc_lds, bias_copies, row_parts;
@@ -263,13 +264,23 @@ __device__ __forceinline__ void finish_scores(const AttnArgs &a, floatx4 (&s)[NB
             for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, base);
     }
     if (near) {
-        // in a sequence the biases of a lane's keys stand one behind the other, and where the whole tile is inside the reach nothing is clamped
+        // Where the whole tile is inside the reach nothing is clamped, and in a sequence the biases of a lane's keys stand one behind the other.
         const int first = key_code[0] + 4 * g - row.code + a.reach;
         if (bias && a.width == 1 && __all((first >= 0) & (first + 16 * NB - 13 <= 2 * a.reach))) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b][e] += bias[first + 16 * b + e];
+        } else if (bias && __all((key_code[0] - row.code >= -a.reach) & (key_code[16 * NB - 1] - row.code <= a.reach))) {
+            const int here = a.reach - row.code;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int4 kc = *reinterpret_cast<const int4 *>(key_code + 16 * b + 4 * g);
+                s[b].x += bias[kc.x + here];
+                s[b].y += bias[kc.y + here];
+                s[b].z += bias[kc.z + here];
+                s[b].w += bias[kc.w + here];
+            }
         } else if (bias) {
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
@@ -308,13 +319,13 @@ __device__ __forceinline__ void finish_scores(const AttnArgs &a, floatx4 (&s)[NB
     }
 }
 
-// Numbers and documents of a tile's KT keys into LDS, by the first KT threads of the workgroup; key_doc[KT]: the document of all of them, or -3.
+// Numbers (keys past the end: the last one's) and documents of a tile's KT keys into LDS, by the first KT threads of the workgroup; key_doc[KT]: the document of all of them, or -3.
 template <int KT>
 __device__ __forceinline__ void stage_keys(const AttnArgs &a, int n, int j0, int *key_code, int *key_doc)
 {
     if (threadIdx.x >= KT) return;
     const int j = j0 + threadIdx.x;
-    if (a.table) key_code[threadIdx.x] = code_of(a, j);
+    if (a.table) key_code[threadIdx.x] = code_of(a, min(j, a.Sk - 1));
     if (a.docs) {
         const int doc = key_document(a, n, j), first = __builtin_amdgcn_readfirstlane(doc);
         key_doc[threadIdx.x] = doc;
@@ -381,22 +392,40 @@ __device__ __forceinline__ float over_column(float v, F f)
 __device__ __forceinline__ float column_max(float v) { return over_column(v, [](float x, float y) { return fmaxf(x, y); }); }
 __device__ __forceinline__ float column_sum(float v) { return over_column(v, [](float x, float y) { return x + y; }); }
 
+// A row's weights as its lse gives them sum to one but for the rounding of lse itself, which is a part of 2^-24 of its size: where distances make scores large
+// -- a row whose nearest key is far away, behind a length, say -- that is more than all other errors. What makes them sum to one, for a lane's row; total: of this lane's keys.
+__device__ __forceinline__ float share_of(const AttnArgs &a, float total)
+{
+    if (!a.slopes) return 1.f;
+    total = column_sum(total);
+    return total > 0.f ? 1.f / total : 0.f;
+}
+
 // A row's reference, against which its weights are taken (the same in the four lanes of its column): a score that it had, or minus infinity so far. It is
 // taken anew only where a score passes it by more than kSlack: weights are then at most 2^kSlack, and most tiles need no exchange between lanes and rescale
-// nothing. Scores s come relative to `reference_of(top)` and leave relative to the new one.
+// nothing. Scores s come relative to `top.at` and leave relative to the new one.
 constexpr float kSlack = 6.f;
-__device__ __forceinline__ float reference_of(float top) { return top == -kInf ? 0.f : top; }
+struct Reference {
+    float at;
+    bool seen;                    // a score was; until then `at` is what distances alone make of the nearest key, so that large ones cancel unrounded
+    __device__ __forceinline__ Reference(const AttnArgs &a, const RowState &row, int begin, int end) : at(0.f), seen(false)
+    {
+        if (a.slopes) at = -row.slope * fabsf((float)(row.p - max(begin, min(row.p, end - 1))));
+    }
+    __device__ __forceinline__ float maximum() const { return seen ? at : -kInf; }
+};
 template <int NB, int DT>
-__device__ __forceinline__ void raise_top(floatx4 (&s)[NB], float &top, float &sum, floatx4 (&o)[DT], float lift = 0.f)      // (s: `lift` more than that)
+__device__ __forceinline__ void raise_top(floatx4 (&s)[NB], Reference &top, float &sum, floatx4 (&o)[DT], float lift = 0.f)      // (s: `lift` more than that)
 {
     float mx = -kInf;
 #pragma unroll
     for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(s[b].x, s[b].y), fmaxf(s[b].z, s[b].w)));
-    if (!__any(mx > (top == -kInf ? -kInf : kSlack + lift))) return;
+    if (!__any(mx > (top.seen ? kSlack + lift : -kInf))) return;
     mx = column_max(mx) - lift;
-    const float by = top == -kInf ? (mx == -kInf ? 0.f : mx) : fmaxf(mx, 0.f);       // (a lower reference is never taken)
-    const float w = top == -kInf ? 1.f : __builtin_amdgcn_exp2f(-by);                // (nothing was summed so far)
-    top = top == -kInf ? mx : top + by;
+    const float by = top.seen ? fmaxf(mx, 0.f) : (mx == -kInf ? 0.f : mx);           // (a lower reference is never taken)
+    const float w = top.seen ? __builtin_amdgcn_exp2f(-by) : 1.f;                    // (nothing was summed so far)
+    top.at += by;
+    top.seen |= mx != -kInf;
     sum *= w;
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] *= w;

@@ -98,7 +98,8 @@ __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
 
     const float far_lo = a.table ? bias_gather(a, head, 0) : 0.f, far_hi = a.table ? bias_gather(a, head, 2 * a.reach) : 0.f;
     floatx4 o[DT] = {};
-    float top = -kInf, sum = 0.f;
+    Reference top(a, row, begin, end);
+    float sum = 0.f;
     const int step = waves * KT;
     int j0 = begin + first;
     if (!early && j0 < end) { fetch_k(j0); fetch_v(j0); }
@@ -130,7 +131,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b] = mfma(kx[b][c][e], q[c][e], s[b]);
         if (j0 + step < end) fetch_k(j0 + step);
-        const float base = far - reference_of(top);
+        const float base = far - top.at;
         float in = a.scale * kLog2e;
         if (a.cap > 0.f) {
 #pragma unroll
@@ -209,7 +210,7 @@ __global__ void __launch_bounds__(64 * WAVES) attn_token(AttnArgs a)
 #pragma unroll
             for (int x = 0; x < VD; ++x)
                 *reinterpret_cast<floatx4 *>(lo_ + (wave * a.rows + m) * DP + grp * 16 * VD + 4 * g * VD + 4 * x) = result_quad<DT>(o, grp, x);
-        if (g == 0) ml[wave * a.rows + m] = float2{top, sum};
+        if (g == 0) ml[wave * a.rows + m] = float2{top.maximum(), sum};
     }
     if (threadIdx.x < 16) flags[threadIdx.x] = 0;
     __syncthreads();

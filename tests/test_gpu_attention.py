@@ -365,6 +365,24 @@ def test_attention_and_its_gradient_in_parts(name):
     Case(**LARGE[name]).check()
 
 
+@pytest.mark.parametrize("shape", [dict(Sq=300, heads=2, D=16), dict(Sq=1000, heads=4, D=48)], ids=["small", "in parts"])
+def test_rows_far_behind_the_keys_they_see(shape):
+    """Scores of several hundred by distance alone, whose lse is rounded to some 2^-15: weights and gradients are not. A weight is the power of a sum of
+    at most four numbers below 16 with three roundings, 16 * 3 * 2^-24 = 2.9e-6 at most and a third of that in the mean square over hundreds of rows."""
+    c = Case(N=2, lengths=[1, 7], slopes=True, **shape)
+    leaves = [t.double().requires_grad_() for t in (c.q, c.k, c.v)]
+    ref, _ = c.ref(*leaves)
+    ref.backward(c.dout.double())
+    plan = c.plan()
+    (q, k, v), m = c.dev()
+    o, lse = c.forward(plan)
+    dq, dk, dv = (torch.empty_like(t) for t in (q, k, v))
+    plan.grad(q, k, v, o, lse, blocked(c.dout, c.Cb).to(DEV), dq, dk, dv, **m)
+    for got, leaf, name in zip((dq, dk, dv), leaves, ("dq", "dk", "dv")):
+        off = plain(got).double().cpu() - leaf.grad
+        assert float(off.norm()) <= 2e-6 * float(leaf.grad.norm()), name
+
+
 @pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** 30])
 def test_parts_carry_any_magnitude(size):
     """Tensors far from one in size, and tokens of very different sizes beside each other: fp16 alone holds neither."""
