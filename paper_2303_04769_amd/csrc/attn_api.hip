@@ -127,7 +127,14 @@ struct AttnPlan {
     int pack, head_sets, rows, row_tiles, splits;
     size_t ml_at, k_at, v_at, exps_at, bytes;          // places in the workspace, in bytes
 };
-bool parts_work(const small_attn &a) { return (double)a.N * a.heads * a.Sq * a.Sk * a.D >= 1e8; }
+// Where values in two parts take a forward call: keys and values are laid out for it once, which rows of their heads and products have to pay for. fp32 -> parts:
+// 8 x 8 pixels, 512 images, 18 -> 35 us; 10 x 10, 200 images, 30 -> 33; 14 x 14, 16 images, 21 -> 24, 64 images 61 -> 53; 400 frames, 4 heads of 64, 23 -> 22;
+// 150 frames, 4 heads a key head, 16 sequences, 31 -> 20.
+bool forward_in_parts(const small_attn &a)
+{
+    const double rows = (double)(a.heads / a.kv_heads) * a.Sq, work = (double)a.N * a.heads * a.Sq * a.Sk * a.D;
+    return a.D <= 128 && (rows >= 256 ? work >= 4e7 : rows >= 128 && work >= 3e8);
+}
 AttnPlan plan_attn(const small_attn &a)
 {
     AttnPlan p{};
@@ -137,7 +144,7 @@ AttnPlan plan_attn(const small_attn &a)
     p.pack = group > 1 && (p.token || a.Sq < 64);
     p.head_sets = p.pack ? a.kv_heads : a.heads;
     p.rows = (int)(p.pack ? packed : a.Sq);
-    p.parts = !p.token && !p.pack && a.D <= 128 && parts_work(a);
+    p.parts = !p.token && !p.pack && forward_in_parts(a);
     const long sets = (long)a.N * p.head_sets;
     p.row_tiles = p.token ? 1 : (p.rows + 63) / 64;
     const long base = sets * p.row_tiles;
@@ -220,10 +227,11 @@ size_t bias_bytes(const small_attn &a, const AttnPlan &p)
     return offsets <= kBiasLds ? (size_t)offsets * sizeof(float) : 0;
 }
 
-// Where values in two parts take a gradient call: as the forward call, and with a bias whose sums by offset fit LDS.
+// Where values in two parts take a gradient call: with a bias, one whose sums by offset fit LDS. fp32 -> parts: 20 frames, 4 heads of 16, a bias by buckets, 48 -> 43 us;
+// 100 frames, 4 heads of 32, 37 -> 33, with a bias 76 -> 53; 14 x 14 pixels, 8 images, 126 -> 76; 10 x 10, 24 images, no bias, 37 -> 38, 200 images 142 -> 109.
 bool grad_in_parts(const small_attn &a)
 {
-    return a.D <= 128 && parts_work(a) && (!a.table || a.reach < 2048);
+    return a.D <= 128 && (!a.table || a.reach < 2048);
 }
 
 // The gradient's workspace: delta and share [N][heads][Sq]; with a table its sums by offset, of every tile of rows and of every head; in parts the images of keys, values,
