@@ -422,9 +422,10 @@ __device__ __forceinline__ void raise_top(floatx4 (&s)[NB], Reference &top, floa
     for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(s[b].x, s[b].y), fmaxf(s[b].z, s[b].w)));
     if (!__any(mx > (top.seen ? kSlack + lift : -kInf))) return;
     mx = column_max(mx) - lift;
-    const float by = top.seen ? fmaxf(mx, 0.f) : (mx == -kInf ? 0.f : mx);           // (a lower reference is never taken)
+    // (a lower reference is never taken; what is taken off is what the reference gains after rounding, or old sums and new ones would stand for different ones)
+    const float now = top.at + (top.seen ? fmaxf(mx, 0.f) : (mx == -kInf ? 0.f : mx)), by = now - top.at;
     const float w = top.seen ? __builtin_amdgcn_exp2f(-by) : 1.f;                    // (nothing was summed so far)
-    top.at += by;
+    top.at = now;
     top.seen |= mx != -kInf;
     sum *= w;
 #pragma unroll

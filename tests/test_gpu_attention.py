@@ -383,6 +383,17 @@ def test_rows_far_behind_the_keys_they_see(shape):
         assert float(off.norm()) <= 2e-6 * float(leaf.grad.norm()), name
 
 
+@pytest.mark.parametrize("N,Sk", [(16, 1500), (16, 6000), (2, 40000)])
+def test_single_tokens_with_steep_distances(N, Sk):
+    """Distances of thousands of keys at a slope of a half: what the far ones round must not reach the near ones, which alone count. Weights that do are
+    powers of numbers below 16, rounded three times by 2^-21 at most, 1.4e-6, and a third of that in the mean square."""
+    c = Case(N=N, Sq=1, Sk=Sk, heads=4, kv=2, D=32, slopes=True, cap=20.0)
+    ref, _ = c.ref()
+    o, _ = c.forward()
+    off, want = ((t.double().cpu()).reshape(c.N, 4, 32) for t in (plain(o) - ref.to(DEV), ref))
+    assert float((off.norm(dim=2) / want.norm(dim=2)).max()) <= 1e-6
+
+
 @pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** 30])
 def test_parts_carry_any_magnitude(size):
     """Tensors far from one in size, and tokens of very different sizes beside each other: fp16 alone holds neither."""
