@@ -6,8 +6,9 @@
 // v_mfma_f32_16x16x4_f32 of 32 do: 5.3 times the rate.
 //
 // fp16 has little range, so values carry a power of two: one for each tile of 64 tokens of a head (its largest magnitude comes to lie in
-// [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-25 times the tile's largest still has 22 bits, and below that the error is
-// 2^-35 of the largest one. Magnitudes beyond fp32's own range apart, no input is out of reach; infinities and NaN become NaN.
+// [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-12 times the tile's largest still has 22 bits, and below that the error is
+// 2^-35 of the largest one; weighted sums over tiles, whose weights carry the difference of their powers, have an error of 2^-32 of the largest value that the
+// row's range of keys holds. So no magnitude is out of reach, and what stands beside values 2^9 times its own still has fp32's precision; infinities and NaN become NaN.
 //
 // attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, [16 tokens][32 channels][part], lane (m, g) with its eight
 // values behind each other (channels 8g .. 8g+7 of token m), so a wave reads an operand with tokens in lanes as one linear kilobyte, and copies of tiles into LDS
@@ -31,10 +32,13 @@ typedef _Float16 half2v __attribute__((ext_vector_type(2)));
 typedef float float2v __attribute__((ext_vector_type(2)));
 typedef unsigned uintx4v __attribute__((ext_vector_type(4)));
 
-// Two values into half a register's worth of parts each.
+// Two values into half a register's worth of parts each. (The factor is hidden from the compiler, which would take a subtraction for the multiply-add and with it
+// a conversion each way for the one instruction that reads and writes halves.)
 __device__ __forceinline__ void split_pair(float x, float y, unsigned &hi, unsigned &lo)
 {
-    const half2v h = __builtin_convertvector((float2v{x, y}), half2v), l = {(_Float16)fmaf((float)h.x, -1.f, x), (_Float16)fmaf((float)h.y, -1.f, y)};
+    float minus = -1.f;
+    asm("" : "+s"(minus));
+    const half2v h = __builtin_convertvector((float2v{x, y}), half2v), l = {(_Float16)fmaf((float)h.x, minus, x), (_Float16)fmaf((float)h.y, minus, y)};
     hi = __builtin_bit_cast(unsigned, h);
     lo = __builtin_bit_cast(unsigned, l);
 }
@@ -78,6 +82,9 @@ __device__ __forceinline__ RowTile row_tile_of(const AttnArgs &a, unsigned group
     const unsigned r = (set & 1) && (set + 1) * units <= each * tiles ? (2 * set + 1) * units - 1 - at : at, by_tile = r / each;
     return {(int)(part * each + (r - by_tile * each)), (int)(tiles - 1 - by_tile), 0};
 }
+
+// An exponent, by a scalar load: it counts apart from the copies into LDS, which the compiler does not see and which a wait for a vector load would include.
+__device__ __forceinline__ int exponent_at(const int *exps, size_t at) { return ((const __attribute__((address_space(4))) int *)exps)[at]; }
 
 struct PartsTensor {
     const float *p;

@@ -1,5 +1,12 @@
 // Attention over whole sequences, forward, on the fp16 matrix instructions with values in two parts (gfx950); attn_parts.h has the arithmetic and the
-// layouts. Tiles of 64 rows (16 a wave) walk over tiles of 64 keys in LDS.
+// layouts. Tiles of 64 rows (16 a wave) walk over tiles of 64 keys in LDS, four workgroups a compute unit up to 64 channels: sixteen rows a wave leave
+// registers for that (32 rows a wave, half the LDS reads but half the waves: 311 against 208 us in an early form).
+//
+// Bound by vector instructions, not by the matrix instructions that they feed: a score is scaled, capped, biased, masked, made a weight and split in two,
+// some thirty instructions, 1900 cycles for a wave's tile of 16 x 64, where the matrix instructions take 768 at 64 channels. Counters for 4096 causal frames,
+// 8 heads of 64, capped, a bias by buckets, 2 sequences: vector ALU busy some 56 % of the time, matrix pipe 26 %. Measured: that case 160 us (4 D operations
+// a pair that is seen: 215 TFLOP/s; fp32 instructions 494 us), 8192 frames of packed documents with distances 155 us, 14 x 14 pixels, 8 heads of 32, 64 images,
+// 37 us and 17 for laying keys and values out.
 #include "attn_parts.h"
 
 namespace small {
@@ -160,7 +167,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     // Values are on their way while scores are computed, the next keys while values are summed; a barrier in front of either, behind which the
     // other's buffer is free.
     for (int j0 = begin; j0 < end; j0 += 64) {
-        const int k_exp = k_exps[j0 / 64], v_now = v_exps[j0 / 64];
+        const int k_exp = exponent_at(k_exps, j0 / 64), v_now = exponent_at(v_exps, j0 / 64);
         stage_keys<64>(a, n, j0, key_code, key_doc);
         wait_vmcnt<0>();
         __syncthreads();
@@ -181,10 +188,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
 #pragma unroll
                 for (int b = 0; b < 4; ++b) s[b] = mfma16(part == 0 ? k_lo[b] : k_hi[b], part == 1 ? q_lo[st] : q_hi[st], s[b]);
         }
-        // weights near fp16's top, and at the power of two that the sums carry: in the exponent, or, where a tile's values are so small that
-        // this could lose weights from their own sum, behind it
-        const int lift = kLift + v_now - v_exp;
-        const float in_exponent = lift >= -40 ? (float)lift : 0.f;
+        // weights near fp16's top, and at the power of two that the sums carry; below 2^-40, where fp16 has nothing left of them, only their own sum matters
+        const int lift = max(kLift + v_now - v_exp, -40);
+        const float in_exponent = (float)lift;
         finish_scores<MODE>(a, s, row, q_exp + k_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
         raise_top(s, top, sum, o, in_exponent);
         floatx4 part = {};
@@ -194,10 +200,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
             for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
             part += s[b];
         }
-        sum = fmaf((part.x + part.y) + (part.z + part.w), ldexpf(1.f, lift >= -40 ? -lift : 0), sum);
-        if (lift < -40)
-#pragma unroll
-            for (int b = 0; b < 4; ++b) s[b] *= ldexpf(1.f, lift);
+        sum = fmaf((part.x + part.y) + (part.z + part.w), ldexpf(1.f, -lift), sum);
         half8 p_hi[2], p_lo[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], p_hi[b], p_lo[b]);

@@ -5,6 +5,11 @@
 // The tile that a wave holds comes straight from the images (a lane's operand is what the image has at its place), what it walks over through LDS.
 // P is at most 1 and is lifted to fp16's top. dS has no such bound worth having -- a long row's weights are small, and so are their gradients -- so it carries
 // a power of two for each column, set by the first tile and raised where a value would pass fp16's range.
+//
+// Bound as the forward kernel is, by some forty vector instructions a pair in either walk, and by waits that three workgroups a compute unit (registers; two from 65
+// channels on) do not cover: vector ALU busy 41 % and 37 %, matrix pipe 16 % and 20 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
+// buckets, 4 sequences. Measured there: rows 180 us, keys 204, and with the forward call and all else 490 (fp32
+// instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 67, keys 54.
 #include "attn_parts.h"
 
 namespace small {
@@ -263,7 +268,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
         }
     else
     for (int j0 = begin; j0 < end; j0 += 64) {
-        const int k_exp = k_exps[j0 / 64], v_exp = v_exps[j0 / 64];
+        const int k_exp = exponent_at(k_exps, j0 / 64), v_exp = exponent_at(v_exps, j0 / 64);
         stage_keys<64>(a, n, j0, key_code, key_doc);
         wait_vmcnt<0>();
         __syncthreads();
@@ -450,7 +455,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         else
         for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
             Rows &rows = rows_of[now != 0];
-            const int q_exp = a.q_exps[first_tile + i0 / 64], d_exp = a.do_exps[first_tile + i0 / 64];
+            const int q_exp = exponent_at(a.q_exps, first_tile + i0 / 64), d_exp = exponent_at(a.do_exps, first_tile + i0 / 64);
             if (threadIdx.x < 32) {
                 const int i = i0 + threadIdx.x, ii = min(i, a.Sq - 1);
                 const RowState row(a, im, n, i, head);
