@@ -3,7 +3,7 @@
 //
 // Bound by the fp32 matrix instructions: a pair of a query and a key costs 4 D of their 64 flops a cycle and SIMD, 4 cycles at D = 64, against
 // some twelve vector operations of which other waves' hide behind them, and 8 D / 64 bytes of LDS reads. It has what is too small for values in two parts (8 x 8
-// pixels, 4 heads of 16, 256 images: 10.4 us, 4 of them the launch), heads of more than 128 channels, and rows of key heads packed together.
+// pixels, 4 heads of 16, 256 images: 10 us, 4 of them the launch), heads of more than 128 channels, and rows of key heads packed together.
 #include "attn_row.h"
 
 namespace small {

@@ -4,9 +4,9 @@
 //
 // Bound by vector instructions, not by the matrix instructions that they feed: a score is scaled, capped, biased, masked, made a weight and split in two,
 // some thirty instructions, 1900 cycles for a wave's tile of 16 x 64, where the matrix instructions take 768 at 64 channels. Counters for 4096 causal frames,
-// 8 heads of 64, capped, a bias by buckets, 2 sequences: vector ALU busy some 56 % of the time, matrix pipe 26 %. Measured: that case 160 us (4 D operations
-// a pair that is seen: 215 TFLOP/s; fp32 instructions 494 us), 8192 frames of packed documents with distances 155 us, 14 x 14 pixels, 8 heads of 32, 64 images,
-// 37 us and 17 for laying keys and values out.
+// 8 heads of 64, capped, a bias by buckets, 2 sequences: vector ALU busy some 57 % of the time, matrix pipe 30 %. Measured: that case 143 us (4 D operations
+// a pair that is seen: 240 TFLOP/s; fp32 instructions 494 us), 8192 frames of packed documents with distances 142 us, 14 x 14 pixels, 8 heads of 32, 64 images,
+// 35 us and 17 for laying keys and values out.
 #include "attn_parts.h"
 
 namespace small {
@@ -229,7 +229,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
             floatx4 y;
 #pragma unroll
             for (int e = 0; e < 4; ++e) y[e] = ldexpf(o[d][e] * inv, v_exp - kLift);
-            if (z.splits > 1) {
+            if (z.splits > 1 && z.D % 4 == 0) {
+                if (16 * d + 4 * g < z.D) *reinterpret_cast<floatx4 *>(z.part_o + part * z.D + 16 * d + 4 * g) = y;
+            } else if (z.splits > 1) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
                     if (16 * d + 4 * g + e < z.D) z.part_o[part * z.D + 16 * d + 4 * g + e] = y[e];

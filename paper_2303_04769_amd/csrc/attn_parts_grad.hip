@@ -7,9 +7,9 @@
 // a power of two for each column, set by the first tile and raised where a value would pass fp16's range.
 //
 // Bound as the forward kernel is, by some forty vector instructions a pair in either walk, and by waits that three workgroups a compute unit (registers; two from 65
-// channels on) do not cover: vector ALU busy 41 % and 37 %, matrix pipe 16 % and 20 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
-// buckets, 4 sequences. Measured there: rows 180 us, keys 204, and with the forward call and all else 490 (fp32
-// instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 67, keys 54.
+// channels on) do not cover: vector ALU busy 46 % and 41 %, matrix pipe 19 % and 22 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
+// buckets, 4 sequences. Measured there: rows 175 us, keys 200, and with the forward call and all else 453 (fp32
+// instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 66, keys 53.
 #include "attn_parts.h"
 
 namespace small {
@@ -602,12 +602,19 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         // [part][image, key head][key][dk, dv][D]
         float *to = z.part_o + ((((size_t)part * z.N + n) * kv + key_head) * z.Sk + j) * 2 * z.D;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+        for (int d = 0; d < DT; ++d) {
+            const int c = 16 * d + 4 * g;
+            if (z.vec) {
+                if (c < z.D) {
+                    *reinterpret_cast<floatx4 *>(to + c) = dk[d] * dk_back;
+                    *reinterpret_cast<floatx4 *>(to + z.D + c) = dv[d] * dv_back;
+                }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int c = 16 * d + 4 * g + e;
-                if (c < z.D) { to[c] = dk[d][e] * dk_back; to[z.D + c] = dv[d][e] * dv_back; }
+                for (int e = 0; e < 4; ++e)
+                    if (c + e < z.D) { to[c + e] = dk[d][e] * dk_back; to[z.D + c + e] = dv[d][e] * dv_back; }
             }
+        }
         return;
     }
     float *tk = const_cast<float *>(token_at(z.dk, z.dks, n, j)), *tv = const_cast<float *>(token_at(z.dv, z.dvs, n, j));
@@ -624,22 +631,35 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
     }
 }
 
-// Adds the parts of dk and dv, in their order. A thread a value.
-__global__ void __launch_bounds__(256) attn_grad_join(AttnArgs a, size_t values)
+// Adds the parts of dk and dv, in their order. A thread VEC neighbouring channels; units: how many of those there are.
+template <int VEC>
+__global__ void __launch_bounds__(256) attn_grad_join(AttnArgs a, size_t units)
 {
     const size_t e = (size_t)blockIdx.x * 256 + threadIdx.x;
-    if (e >= values) return;
-    float x = 0.f;
-    for (int s = 0; s < a.splits; ++s) x += a.part_o[(size_t)s * values + e];
-    const int kv = a.by_group.div(a.heads), two = 2 * a.D;
+    if (e >= units) return;
+    float x[VEC] = {};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const float *from = a.part_o + ((size_t)s * units + e) * VEC;
+        if constexpr (VEC == 4) {
+            const floatx4 y = *reinterpret_cast<const floatx4 *>(from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] += y[i];
+        } else {
+            x[0] += *from;
+        }
+    }
+    const int kv = a.by_group.div(a.heads), two = 2 * a.D / VEC;
     const size_t token = e / (unsigned)two;
-    int c = (int)(e - token * two);
+    int c = (int)(e - token * two) * VEC;
     const size_t by_head = token / (unsigned)a.Sk;
     const int j = (int)(token - by_head * a.Sk), n = (int)(by_head / (unsigned)kv), key_head = (int)(by_head - (size_t)n * kv);
     const bool is_v = c >= a.D;
     c -= is_v ? a.D : 0;
     const TokenStrides &s = is_v ? a.dvs : a.dks;
-    const_cast<float *>(token_at(is_v ? a.dv : a.dk, s, n, j))[channel_at(a, s, key_head * a.D + c)] = x;
+    float *const to = const_cast<float *>(token_at(is_v ? a.dv : a.dk, s, n, j)) + channel_at(a, s, key_head * a.D + c);
+    if constexpr (VEC == 4) *reinterpret_cast<floatx4 *>(to) = floatx4{x[0], x[1], x[2], x[3]};
+    else *to = x[0];
 }
 
 }  // namespace
@@ -677,8 +697,9 @@ hipError_t launch_attn_grad_keys_parts(const AttnArgs &a, hipStream_t s)
     KEYS(1) KEYS(2) KEYS(3) KEYS(4)
 #undef KEYS
     if (e != hipSuccess || a.splits == 1) return e;
-    const size_t values = (size_t)a.N * kv * a.Sk * 2 * a.D;
-    hipLaunchKernelGGL(attn_grad_join, dim3((unsigned)((values + 255) / 256)), dim3(256), 0, s, a, values);
+    const size_t units = (size_t)a.N * kv * a.Sk * 2 * a.D / (a.vec ? 4 : 1);
+    if (a.vec) hipLaunchKernelGGL(attn_grad_join<4>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, a, units);
+    else hipLaunchKernelGGL(attn_grad_join<1>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, a, units);
     return hipGetLastError();
 }
 

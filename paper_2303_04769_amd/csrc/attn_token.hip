@@ -5,7 +5,7 @@
 // matrix pipe can afford: 256 bytes of cache are 32 of its cycles, 19 TB/s over the chip. The waves of a workgroup take the
 // tiles of its keys in turn and join through LDS; long caches are split over workgroups too and joined by attn_join.
 //
-// Measured: 64 streams of 2048 to 16384 keys, 16 heads of 64 on 4, 248 us, 4.9 TB/s; one stream of 777 keys, 8 heads of 32, a bias by buckets, 13.4 us, two
+// Measured: 64 streams of 2048 to 16384 keys, 16 heads of 64 on 4, 250 us, 4.9 TB/s; one stream of 777 keys, 8 heads of 32, a bias by buckets, 13.4 us, two
 // launches of some 4 us and the time that a chain of dependent loads takes (bucket, bias, keys, values).
 #include "attn_row.h"
 
