@@ -400,6 +400,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         lo = first - im.first;
         hi = last - im.first;
     }
+    // (no such row: an empty hull may lie at any distance from the rows there are, and rounding its begin down would make a tile of it)
+    if (lo >= hi) lo = hi = 0;
     int begin = __builtin_amdgcn_readfirstlane(lo) & ~31, end = __builtin_amdgcn_readfirstlane(hi);
     const int head_part = part / a.row_parts, row_part = part - head_part * a.row_parts, head_parts = a.splits / a.row_parts;
     const int h0 = key_head * a.group + a.group * head_part / head_parts, h1 = key_head * a.group + a.group * (head_part + 1) / head_parts;
