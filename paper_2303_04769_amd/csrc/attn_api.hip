@@ -227,11 +227,18 @@ size_t bias_bytes(const small_attn &a, const AttnPlan &p)
     return offsets <= kBiasLds ? (size_t)offsets * sizeof(float) : 0;
 }
 
-// Where values in two parts take a gradient call: with a bias, one whose sums by offset fit LDS. fp32 -> parts: 20 frames, 4 heads of 16, a bias by buckets, 48 -> 43 us;
+// Bytes of LDS that the rows' gradient in parts has for its tiles, the expanded bias and `copies` sets of the sums by offset (attn_parts_grad.hip).
+size_t grad_lds(const small_attn &a, int copies)
+{
+    const size_t size = a.table ? 2 * (size_t)a.reach + 1 : 0;
+    return 3 * parts_tile_bytes(parts_steps(a.D)) + sizeof(float) * (size + (size ? copies * (size + 1) : 0));
+}
+// Where values in two parts take a gradient call: with a bias, one whose sums by offset fit LDS, four sets of them at least (wanted or not: the workspace must do for both).
+// fp32 -> parts: 20 frames, 4 heads of 16, a bias by buckets, 48 -> 43 us;
 // 100 frames, 4 heads of 32, 37 -> 33, with a bias 76 -> 53; 14 x 14 pixels, 8 images, 126 -> 76; 10 x 10, 24 images, no bias, 37 -> 38, 200 images 142 -> 109.
 bool grad_in_parts(const small_attn &a)
 {
-    return a.D <= 128 && (!a.table || a.reach < 2048);
+    return a.D <= 128 && (!a.table || (a.reach < 2048 && grad_lds(a, 4) <= kGradLds));
 }
 
 // The gradient's workspace: delta and share [N][heads][Sq]; with a table its sums by offset, of every tile of rows and of every head; in parts the images of keys, values,
@@ -379,7 +386,7 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     // sets of sums by offset, 16, 8 or 4: as many as leave the three workgroups a compute unit (two from 65 channels on) that registers allow
     // (14 x 14 pixels, 8 heads, 64 images, all of the gradient: 16 sets 261 us, 8 sets 246, 4 sets 259)
     x.bias_copies = 16;
-    while (x.bias_copies > 4 && 3 * parts_tile_bytes(parts_steps(a->D)) + 4 * size * (x.bias_copies + 1) > (a->D <= 64 ? 53000 : 79000)) x.bias_copies /= 2;
+    while (x.bias_copies > 4 && grad_lds(*a, x.bias_copies) > (a->D <= 64 ? 53000 : 79000)) x.bias_copies /= 2;
     const hipStream_t s = (hipStream_t)stream;
     hipError_t e;
     if (p.parts) {

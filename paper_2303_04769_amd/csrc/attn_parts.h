@@ -134,6 +134,8 @@ __device__ __forceinline__ void products_across(floatx4 (&acc)[2 * STEPS], const
 
 constexpr size_t parts_tile_bytes(int steps) { return (size_t)64 * 32 * steps * 4; }
 constexpr int parts_steps(int D) { return (D + 31) / 32; }
+// What the rows' gradient may ask for behind the few hundred bytes that it has anyway: 160 KB a compute unit.
+constexpr size_t kGradLds = 160 * 1024 - 2048;
 
 // attn_parts.hip
 hipError_t launch_make_parts(const AttnArgs &a, PartsArgs &args, bool vec, hipStream_t s);

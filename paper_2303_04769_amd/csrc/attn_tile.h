@@ -474,7 +474,10 @@ template <typename K>
 hipError_t launch_lds(K *kernel, unsigned grid, size_t lds, const AttnArgs &a, hipStream_t s)
 {
     if (lds > 8192)
-        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) return e;
+        if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds); e != hipSuccess) {
+            (void)hipGetLastError();                     // (or the next call of somebody else would report it)
+            return e;
+        }
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(256), lds, s, a);
     return hipGetLastError();
 }

@@ -34,3 +34,124 @@ def test_documents_and_positions_wholly_outside(causal, bias):
     for t in (out, dq, dk, dv):
         assert bool((t[outside] == 0).all())
     assert bool((lse[outside] == -float("inf")).all())
+
+
+# ---------------------------------------------------------------------------------------------------- value by value
+
+U = 2.0 ** -24
+
+
+def exact(c):
+    """Results and gradients in 64 bits, each with the sum of the magnitudes that it is made of: {name: (value, magnitudes)}, plain layouts.
+
+    Rounding errors of a sum are in proportion to its terms' magnitudes, so a result is held to (32 + 4 sqrt(K)) u times the sum of these
+    (the rule of test_gpu_attention.py, there with the tensor's largest value in their place): what is far larger than a row's own
+    terms and hidden from it must not be seen in it. Gradients pass two such chains, so twice that. A weight is off by what its score is: the 32
+    holds for scores up to 16 and for those so large that their weights are 0 or 1."""
+    N, heads, kv, D, Sq, Sk = c.N, c.heads, c.kv, c.D, c.Sq, c.Sk
+    group = heads // kv
+    split = lambda t, h: t.double().reshape(N, h, D, -1).transpose(2, 3)  # noqa: E731  [N][h][S][D]
+    q, k, v, do = split(c.q, heads), split(c.k, kv), split(c.v, kv), split(c.dout, heads)
+    k, v = (t.repeat_interleave(group, 1) for t in (k, v))
+    j = torch.arange(Sk)
+    first = torch.full((N,), Sk - Sq) if c.first is None else c.first.long()
+    p_at = first[:, None] + torch.arange(Sq)
+    seen = torch.ones(N, Sq, Sk, dtype=torch.bool)
+    if c.lengths is not None:
+        seen &= (j < c.lengths[:, None])[:, None]
+    if c.causal:
+        seen &= (j <= p_at[..., None]) | (j < (torch.zeros(N, 1) if c.prefix is None else c.prefix[:, None]))[:, None]
+    if c.docs is not None:
+        mine = torch.where((p_at >= 0) & (p_at < Sk), c.docs.long().gather(1, p_at.clamp(0, Sk - 1)), torch.tensor(-1))
+        seen &= (c.docs[:, None] == mine[..., None]) & (mine >= 0)[..., None]
+    x = c.scale * q @ k.transpose(2, 3)
+    size = c.scale * q.abs() @ k.abs().transpose(2, 3)
+    slope = 1.0
+    if c.cap:
+        t = torch.tanh(x / c.cap)
+        x, slope = c.cap * t, 1 - t * t
+        size = size.clamp(max=c.cap)
+    if c.slopes is not None:
+        x = x - c.slopes.double()[:, None, None] * (p_at[:, None, :, None] - j).abs()
+    at = None
+    if c.table is not None:
+        code = lambda y: torch.div(y, c.width, rounding_mode="floor") * (2 * c.width - 1) + y % c.width  # noqa: E731
+        at = c.bucket.long()[(code(j) - code(p_at)[..., None]).clamp(-c.reach, c.reach) + c.reach]            # [N][Sq][Sk]
+        x = x + torch.stack([c.table.double()[:, at[n]] for n in range(N)])
+    x = x.masked_fill(~seen[:, None], -float("inf"))
+    lse = torch.logsumexp(x, 3)
+    p = torch.exp(x - torch.where(lse == -float("inf"), torch.zeros_like(lse), lse)[..., None])
+    out, out_size = p @ v, p @ v.abs()
+    delta = (do * out).sum(3, keepdim=True)
+    ds = p * (do @ v.transpose(2, 3) - delta)
+    ds_size = p * (do.abs() @ v.abs().transpose(2, 3) + (do.abs() * out_size).sum(3, keepdim=True))
+    fold = lambda t: t.reshape(N, kv, group, Sk, D).sum(2)  # noqa: E731
+    join = lambda t: t.transpose(2, 3).reshape(N, -1, t.shape[2])  # noqa: E731
+    db = None
+    if at is not None:
+        db = [torch.zeros_like(c.table, dtype=torch.float64) for _ in range(2)]
+        for n in range(N):
+            for to, d in zip(db, (ds, ds_size)):
+                to.index_add_(1, at[n].reshape(-1), d[n].reshape(heads, -1))
+    # (1 - tanh^2 is off by some 4 u whatever it is)
+    dx, dx_size = c.scale * ds * slope, c.scale * ds_size * (slope + 0.2 if c.cap else 1.0)
+    r = {"out": (join(out), join(out_size)), "lse": (lse, (p * size).sum(3) + lse.abs().nan_to_num(posinf=0.0) + 1),
+         "dq": (join(dx @ k), join(dx_size @ k.abs())),
+         "dk": (join(fold(dx.transpose(2, 3) @ q)), join(fold(dx_size.transpose(2, 3) @ q.abs()))),
+         "dv": (join(fold(p.transpose(2, 3) @ do)), join(fold(p.transpose(2, 3) @ do.abs())))}
+    if db:
+        r["dtable"] = tuple(db)
+    return r
+
+
+def terms(c, name):
+    rows = c.Sq * c.heads // c.kv
+    return {"out": c.D + c.Sk, "lse": c.D + c.Sk, "dq": c.D + c.Sk, "dk": c.D + rows, "dv": c.D + rows, "dtable": c.D + c.N * c.Sq}[name]
+
+
+def compare(c, got, ref, where=None):
+    """Value by value; where: {name: mask of what is to be right} (all of it)."""
+    for name, t in got.items():
+        want, size = ref[name]
+        t = t.double().cpu()
+        allowed = (32 + 4 * terms(c, name) ** 0.5) * U * (1 if name in ("out", "lse") else 2) * size
+        off = (t - want).abs()
+        off[(t == want)] = 0.0
+        bad = ~(off <= allowed)
+        if where is not None and name in where:
+            bad &= where[name]
+        if bool(bad.any()):
+            worst = torch.where(bad, off / allowed.clamp(min=1e-300), torch.zeros_like(off)).nan_to_num(nan=float("inf"))
+            i = int(worst.argmax())
+            raise AssertionError(f"{name}: {int(bad.sum())} of {bad.numel()} values off, the worst by {float(worst.max()):.2e} of what is allowed: "
+                                 f"{float(t.reshape(-1)[i])} for {float(want.reshape(-1)[i])}, place {i}")
+
+
+def everything(c):
+    return dict(zip(("out", "lse", "dq", "dk", "dv") + (("dtable",) if c.table is not None else ()), gradients(c)))
+
+
+# ---------------------------------------------------------------------------------------------------- biases
+
+def with_offsets(c, reach, buckets=None):
+    """The case with a table over offsets -reach .. reach: each its own bucket, or `buckets` in turn."""
+    size = 2 * reach + 1
+    c.reach, c.width, c.buckets = reach, 1, buckets or size
+    c.bucket = (torch.arange(size) % c.buckets).int()
+    c.table = torch.randn(c.heads, c.buckets, generator=torch.Generator().manual_seed(3))
+    c.masks.update(table=c.table, bucket=c.bucket)
+    return c
+
+
+@pytest.mark.parametrize("D", [96, 97, 100, 128])
+@pytest.mark.parametrize("reach", [1599, 1612, 1640, 2047])
+def test_wide_tables_of_wide_heads(D, reach):
+    """Tables whose sums by offset are about all that a workgroup's LDS holds beside tiles of as many channels, and more than that."""
+    c = with_offsets(Case(Sq=130, heads=2, D=D, Cb=D, causal=True), reach, 64)
+    compare(c, everything(c), exact(c))
+
+
+@pytest.mark.parametrize("side", [29, 32])
+def test_pixels_of_wide_heads(side):
+    c = Case(Sq=side * side, heads=1, D=128, bias=(side, side))
+    compare(c, everything(c), exact(c))
