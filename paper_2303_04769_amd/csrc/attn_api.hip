@@ -120,6 +120,9 @@ int attn_check(const small_attn &a)
     return SMALL_OK;
 }
 
+// Words for the powers of two of so many tiles: their tokens', 16-byte aligned, then their own.
+size_t parts_words(size_t tiles) { return (65 * tiles + 3) / 4 * 4; }
+
 // What a call of these sizes runs: few rows against the cache, or tiles of rows, these with fp32 products or with values in two parts; and over
 // how many workgroups a row's keys are split.
 struct AttnPlan {
@@ -165,7 +168,7 @@ AttnPlan plan_attn(const small_attn &a)
         p.k_at = p.bytes;
         p.v_at = p.k_at + image;
         p.exps_at = p.v_at + image;
-        p.bytes = up(p.exps_at + 2 * tiles * sizeof(int));
+        p.bytes = up(p.exps_at + 2 * parts_words(tiles) * sizeof(int));
     }
     return p;
 }
@@ -198,13 +201,14 @@ void place(AttnArgs &x, const AttnPlan &p, void *ws)
 hipError_t make_parts(AttnArgs &x, const AttnPlan &p, const small_attn &a, void *ws, bool vec, hipStream_t s)
 {
     const int tiles = (a.Sk + 63) / 64;
-    int *const exps = (int *)((char *)ws + p.exps_at);
+    const size_t all = (size_t)a.N * a.kv_heads * tiles;
+    int *const k_words = (int *)((char *)ws + p.exps_at), *const v_words = k_words + parts_words(all);
     PartsArgs args{};
     args.count = 2;
-    args.t[0] = PartsTensor{x.k, x.ks, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.k_at, exps, 0};
-    args.t[1] = PartsTensor{x.v, x.vs, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.v_at, exps + (size_t)a.N * a.kv_heads * tiles, 0};
-    x.k_tok = args.t[0].image; x.k_exps = args.t[0].exps;
-    x.v_tok = args.t[1].image; x.v_exps = args.t[1].exps;
+    args.t[0] = PartsTensor{x.k, x.ks, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.k_at, k_words + 64 * all, k_words, 0};
+    args.t[1] = PartsTensor{x.v, x.vs, a.kv_heads, a.Sk, tiles, 0, (char *)ws + p.v_at, v_words + 64 * all, v_words, 0};
+    x.k_tok = args.t[0].image; x.k_exps = args.t[0].exps; x.k_each = args.t[0].each;
+    x.v_tok = args.t[1].image; x.v_exps = args.t[1].exps; x.v_each = args.t[1].each;
     return launch_make_parts(x, args, vec, s);
 }
 
@@ -266,7 +270,7 @@ GradPlan plan_grad(const small_attn &a)
     if (p.parts) {
         const size_t tile = parts_tile_bytes(parts_steps(a.D)), keys = (size_t)a.N * a.kv_heads * p.key_tiles, rows = (size_t)a.N * a.heads * p.row_tiles;
         for (int x = 0; x < 4; ++x) p.images[x] = take((x < 2 ? keys : rows) * tile);      // k, v; q, dout
-        for (int x = 0; x < 4; ++x) p.exps[x] = take((x < 2 ? keys : rows) * sizeof(int));
+        for (int x = 0; x < 4; ++x) p.exps[x] = take(parts_words(x < 2 ? keys : rows) * sizeof(int));
         // six workgroups a compute unit: by heads that share a key head, then by rows of 256 at least
         const long want = (6L * device_cus() + (long)keys - 1) / (long)keys;
         const int group = a.heads / a.kv_heads;
@@ -390,15 +394,17 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     const hipStream_t s = (hipStream_t)stream;
     hipError_t e;
     if (p.parts) {
-        int *const exps[] = {(int *)(at + p.exps[0]), (int *)(at + p.exps[1]), (int *)(at + p.exps[2]), (int *)(at + p.exps[3])};
         PartsArgs args{};
         args.count = 4;
-        args.t[0] = PartsTensor{k, x.ks, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[0], exps[0], 0};
-        args.t[1] = PartsTensor{v, x.vs, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[1], exps[1], 0};
-        args.t[2] = PartsTensor{q, x.qs, a->heads, a->Sq, p.row_tiles, 1, at + p.images[2], exps[2], 0};
-        args.t[3] = PartsTensor{dout, x.dos, a->heads, a->Sq, p.row_tiles, 1, at + p.images[3], exps[3], 0};
-        x.k_tok = at + p.images[0]; x.v_tok = at + p.images[1]; x.q_tok = at + p.images[2]; x.do_tok = at + p.images[3];
-        x.k_exps = exps[0]; x.v_exps = exps[1]; x.q_exps = exps[2]; x.do_exps = exps[3];
+        const size_t keys = (size_t)a->N * a->kv_heads * p.key_tiles, rows = (size_t)a->N * a->heads * p.row_tiles;
+        int *const each[] = {(int *)(at + p.exps[0]), (int *)(at + p.exps[1]), (int *)(at + p.exps[2]), (int *)(at + p.exps[3])};
+        args.t[0] = PartsTensor{k, x.ks, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[0], each[0] + 64 * keys, each[0], 0};
+        args.t[1] = PartsTensor{v, x.vs, a->kv_heads, a->Sk, p.key_tiles, 0, at + p.images[1], each[1] + 64 * keys, each[1], 0};
+        args.t[2] = PartsTensor{q, x.qs, a->heads, a->Sq, p.row_tiles, 1, at + p.images[2], each[2] + 64 * rows, each[2], 0};
+        args.t[3] = PartsTensor{dout, x.dos, a->heads, a->Sq, p.row_tiles, 1, at + p.images[3], each[3] + 64 * rows, each[3], 0};
+        x.k_tok = args.t[0].image; x.v_tok = args.t[1].image; x.q_tok = args.t[2].image; x.do_tok = args.t[3].image;
+        x.k_exps = args.t[0].exps; x.v_exps = args.t[1].exps; x.q_exps = args.t[2].exps; x.do_exps = args.t[3].exps;
+        x.k_each = each[0]; x.v_each = each[1]; x.q_each = each[2]; x.do_each = each[3];
         x.part_o = (float *)(at + p.dkv_at);
         e = launch_make_parts(x, args, x.vec, s);
         if (e == hipSuccess) e = launch_attn_grad_rows_parts(x, s);

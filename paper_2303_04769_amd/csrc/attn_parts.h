@@ -7,8 +7,11 @@
 //
 // fp16 has little range, so values carry a power of two: one for each tile of 64 tokens of a head (its largest magnitude comes to lie in
 // [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-12 times the tile's largest still has 22 bits, and below that the error is
-// 2^-35 of the largest one; weighted sums over tiles, whose weights carry the difference of their powers, have an error of 2^-32 of the largest value that the
-// row's range of keys holds. So no magnitude is out of reach, and what stands beside values 2^9 times its own still has fp32's precision; infinities and NaN become NaN.
+// 2^-35 of the largest one. A mask may hide any token of a tile from a row, and what it hides must not cost the row precision: so a token whose largest value is
+// less than 2^-kSpread of the tile's carries a power of its own, and the tile says so (mixed). Weighted sums over tiles (of values by scores' weights, of dO by columns'
+// weights) are kept at one power of two where all tiles of a walk have about the same and none is mixed, and where not, at one for each row or
+// column, which follows the largest of the terms that the row sees (ColumnScale). So no magnitude is out of reach, and a result's error is in proportion to the largest
+// magnitude among the channels of the tokens that it is made of, not to anything else. Infinities and NaN become NaN.
 //
 // attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, [16 tokens][32 channels][part], lane (m, g) with its eight
 // values behind each other (channels 8g .. 8g+7 of token m), so a wave reads an operand with tokens in lanes as one linear kilobyte, and copies of tiles into LDS
@@ -56,6 +59,7 @@ __device__ __forceinline__ void split_results(const floatx4 &first, const floatx
 }
 
 // Power of two e such that a magnitude `most` times 2^-e lies in [2^kTop, 2^(kTop + 1)); nothing but zeros: a small one.
+constexpr int kSpread = 8;
 __device__ __forceinline__ int parts_exponent(float most)
 {
     if (most == 0.f) return -100;
@@ -83,15 +87,49 @@ __device__ __forceinline__ RowTile row_tile_of(const AttnArgs &a, unsigned group
     return {(int)(part * each + (r - by_tile * each)), (int)(tiles - 1 - by_tile), 0};
 }
 
-// An exponent, by a scalar load: it counts apart from the copies into LDS, which the compiler does not see and which a wait for a vector load would include.
-__device__ __forceinline__ int exponent_at(const int *exps, size_t at) { return ((const __attribute__((address_space(4))) int *)exps)[at]; }
+// What a tile's tokens carry, in a word: the power of two (kNone: nothing but zeros), and whether tokens have some of their own.
+constexpr int kNone = -1000;
+__device__ __forceinline__ int tile_exponent(int word) { return word >> 1; }
+__device__ __forceinline__ bool tile_mixed(int word) { return word & 1; }
+
+// Of the words that a wave's lanes go through one after another: the largest power of two and the smallest (of tiles that have one), and whether any tile is mixed.
+struct Powers {
+    int most = kNone, least = -kNone;
+    bool mixed = false;
+    __device__ __forceinline__ void add(int word)
+    {
+        const int e = tile_exponent(word);
+        most = max(most, e);
+        least = e == kNone ? least : min(least, e);
+        mixed |= tile_mixed(word);
+    }
+    __device__ __forceinline__ void add_mixed(int word) { mixed |= tile_mixed(word); }
+    // Over the wave: whether no tile is mixed and all are within 2^-spread of the largest. most: uniform from here on.
+    __device__ __forceinline__ bool even(int spread)
+    {
+        // (as floats, by shifts of lanes: a shuffle is a trip through LDS)
+        const auto over_wave = [](float v) {
+            v = fmaxf(v, lane_shift1<0x128>(v));                 // row_ror: 8, 4, 2, 1
+            v = fmaxf(v, lane_shift1<0x124>(v));
+            v = fmaxf(v, lane_shift1<0x122>(v));
+            v = fmaxf(v, lane_shift1<0x121>(v));
+            return __builtin_amdgcn_readfirstlane((int)column_max(v));
+        };
+        const int low = -over_wave((float)-least);
+        most = over_wave((float)most);
+        return !__any(mixed) && most - low <= spread;
+    }
+};
+
+// A tile's word, by a scalar load: it counts apart from the copies into LDS, which the compiler does not see and which a wait for a vector load would include.
+__device__ __forceinline__ int exponents_at(const int *exps, size_t at) { return ((const __attribute__((address_space(4))) int *)exps)[at]; }
 
 struct PartsTensor {
     const float *p;
     TokenStrides s;
     int heads, tokens, tiles, rows;            // rows: not keys but queries (their masks: rows of lse = -inf are left out)
     char *image;
-    int *exps;                                 // [N * heads][tiles]
+    int *exps, *each;                          // [N * heads][tiles], [N * heads][tiles][64]
     unsigned first_block;
 };
 struct PartsArgs {
@@ -131,6 +169,70 @@ __device__ __forceinline__ void products_across(floatx4 (&acc)[2 * STEPS], const
             for (int d = 0; d < ND && d0 + d < DT; ++d) acc[d0 + d] = mfma16(part == 0 ? lo[d] : hi[d], part == 1 ? b_lo : b_hi, acc[d0 + d]);
     }
 }
+
+// Values y, or results of a product with a mixed tile's tokens, of which a lane has the tokens 16b + 4g .. of the tile that `each` points to (by 4g): times their powers of
+// two, and 2^more.
+template <int NB>
+__device__ __forceinline__ void by_token(floatx4 (&y)[NB], const int *each, int more = 0)
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int4 e = *reinterpret_cast<const int4 *>(each + 16 * b);
+        y[b].x = ldexpf(y[b].x, e.x + more);
+        y[b].y = ldexpf(y[b].y, e.y + more);
+        y[b].z = ldexpf(y[b].z, e.z + more);
+        y[b].w = ldexpf(y[b].w, e.w + more);
+    }
+}
+
+// The power of two of a column's terms: they times `scale` stay within 2^14. Nothing but zeros so far: scale = limit = 0.
+struct ColumnScale {
+    float scale = 0.f, limit = 0.f;
+    // Takes terms y that count 2^exp each to the column's scale, which is set anew, and the sums acc along, where one passes the limit.
+    template <int NB, int DT>
+    __device__ __forceinline__ void apply(floatx4 (&y)[NB], int exp, floatx4 (&acc)[DT])
+    {
+        float mx = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(fabsf(y[b].x), fabsf(y[b].y)), fmaxf(fabsf(y[b].z), fabsf(y[b].w))));
+        mx = ldexpf(mx, exp);
+        if (__any(mx > limit)) {
+            mx = column_max(mx);
+            const bool more = mx > limit;
+            const int e = max(-100, (int)(__float_as_uint(mx) >> 23) - 127);
+            const float now = ldexpf(1.f, 8 - e), f = !more || scale == 0.f ? 1.f : ldexpf(now, ilogb_of(scale));
+#pragma unroll
+            for (int d = 0; d < DT; ++d) acc[d] *= f;
+            scale = more ? now : scale;
+            limit = more ? ldexpf(1.f, 6 + e) : limit;
+        }
+        float f = ldexpf(scale, exp);
+        if (__any(f == kInf)) {                                  // (tokens 2^100 times as large as what the column has seen: it does not see these)
+            const float first = ldexpf(1.f, exp);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) y[b] *= first;
+            f = scale;
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) y[b] *= f;
+    }
+    // All terms so far count 2^-by of what they did (the sums acc are that already): the scale follows, as far as floats go.
+    template <int DT>
+    __device__ __forceinline__ void follow(float by, floatx4 (&acc)[DT])
+    {
+        if (!__any((by >= 1.f) & (scale != 0.f))) return;
+        const int k = scale == 0.f ? 0 : max(0, min((int)fminf(by, 300.f), 108 + ilogb_of(scale)));
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) acc[d][x] = ldexpf(acc[d][x], k);
+        scale = ldexpf(scale, k);
+        limit = ldexpf(limit, -k);
+    }
+    static __device__ __forceinline__ int ilogb_of(float s) { return 127 - (int)(__float_as_uint(s) >> 23); }      // (of 1 / s)
+    __device__ __forceinline__ int back() const { return scale == 0.f ? 0 : ilogb_of(scale); }
+    __device__ __forceinline__ float back(float factor) const { return scale == 0.f ? 0.f : ldexpf(factor, ilogb_of(scale)); }
+};
 
 constexpr size_t parts_tile_bytes(int steps) { return (size_t)64 * 32 * steps * 4; }
 constexpr int parts_steps(int D) { return (D + 31) / 32; }

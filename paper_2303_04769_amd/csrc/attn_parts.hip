@@ -9,28 +9,31 @@
 // 35 us and 17 for laying keys and values out.
 #include "attn_parts.h"
 
+#include <type_traits>
+
 namespace small {
 
 namespace {
 
 extern __shared__ __attribute__((aligned(1024))) char parts_lds[];
 
-// Tiles of 64 tokens of up to four tensors, one workgroup each: the largest magnitude, then the image. A thread takes 4 tokens x 4 channels.
+// Tiles of 64 tokens of up to four tensors, one workgroup each: the largest magnitudes, then the image. A thread takes 4 tokens x 4 channels.
 template <int STEPS, bool VEC>
 __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs args)
 {
     constexpr int DQ = STEPS * 8, PER = (16 * DQ + 255) / 256;      // quads of channels, micro tiles a thread
-    __shared__ float most_of[4];
+    __shared__ alignas(16) float most_of[4][64];           // of the tokens, by wave
     int which = 0;
     while (which + 1 < args.count && blockIdx.x >= args.t[which + 1].first_block) ++which;
     const PartsTensor &t = args.t[which];
     const int id = (int)(blockIdx.x - t.first_block), by_tile = id / t.tiles, tile = id - by_tile * t.tiles, n = by_tile / t.heads, head = by_tile - n * t.heads;
     const int len = !t.rows && a.lengths ? max(0, min(a.lengths[n], t.tokens)) : t.tokens;
     floatx4 x[PER][4];
-    float most = 0.f;
+    const int tq = threadIdx.x >> 2 & 15;
+    floatx4 most{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int e = threadIdx.x + p * 256, tq = e >> 2 & 15, dq = (e & 3) | (e >> 6) << 2;
+        const int e = threadIdx.x + p * 256, dq = (e & 3) | (e >> 6) << 2;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int j = tile * 64 + tq * 4 + i;
@@ -40,24 +43,49 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
             x[p][i] = floatx4{0.f, 0.f, 0.f, 0.f};
             if (on) x[p][i] = load_quad<VEC>(a, t.s, token_at(t.p, t.s, n, j), head * a.D, dq * 4);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) most = fmaxf(most, finite_magnitude(x[p][i][d]));
+            for (int d = 0; d < 4; ++d) most[i] = fmaxf(most[i], finite_magnitude(x[p][i][d]));
         }
     }
-    for (int d = 32; d; d >>= 1) most = fmaxf(most, __shfl_xor(most, d));
-    if ((threadIdx.x & 63) == 0) most_of[threadIdx.x >> 6] = most;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        most[i] = fmaxf(most[i], lane_shift1<0xb1>(most[i]));      // quad_perm: the neighbour's, the other pair's
+        most[i] = fmaxf(most[i], lane_shift1<0x4e>(most[i]));
+    }
+    if ((threadIdx.x & 3) == 0) *reinterpret_cast<floatx4 *>(&most_of[threadIdx.x >> 6][tq * 4]) = most;
     __syncthreads();
-    const int ex = parts_exponent(fmaxf(fmaxf(most_of[0], most_of[1]), fmaxf(most_of[2], most_of[3])));
-    if (threadIdx.x == 0) t.exps[id] = ex;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const floatx4 y = *reinterpret_cast<const floatx4 *>(&most_of[w][tq * 4]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) most[i] = fmaxf(most[i], y[i]);
+    }
+    float all = fmaxf(fmaxf(most.x, most.y), fmaxf(most.z, most.w));
+    all = fmaxf(all, lane_shift1<0x124>(all));                         // row_ror
+    all = fmaxf(all, lane_shift1<0x128>(all));
+    all = column_max(all);
+    // (nothing but zeros: any power does for them)
+    const int ex = parts_exponent(all);
+    int own[4];
+    bool mixed = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int y = parts_exponent(most[i]);
+        own[i] = most[i] == 0.f || y >= ex - kSpread ? ex : y;
+        mixed |= own[i] != ex;
+    }
+    mixed = __any(mixed);
+    if (threadIdx.x < 64 && (threadIdx.x & 3) == 0) *reinterpret_cast<int4 *>(t.each + (size_t)id * 64 + tq * 4) = int4{own[0], own[1], own[2], own[3]};
+    if (threadIdx.x == 0) t.exps[id] = (all == 0.f ? kNone : ex) * 2 + mixed;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
-        const int e = threadIdx.x + p * 256, tq = e >> 2 & 15, dq = (e & 3) | (e >> 6) << 2;
+        const int e = threadIdx.x + p * 256, dq = (e & 3) | (e >> 6) << 2;
         if (dq >= DQ) continue;
         half4 hi[4], lo[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const float y = ldexpf(x[p][i][d], -ex);
+                const float y = ldexpf(x[p][i][d], -own[i]);
                 hi[i][d] = (_Float16)y;
                 lo[i][d] = (_Float16)(y - (float)hi[i][d]);
             }
@@ -77,7 +105,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     constexpr int DT = 2 * STEPS, IMAGE = (int)parts_tile_bytes(STEPS);
     __shared__ alignas(16) int key_code[64];
     __shared__ alignas(16) int key_doc[65];
-    __shared__ int words[3];
+    __shared__ int words[2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const RowTile here = row_tile_of<true>(a, (unsigned)a.N * a.head_sets);
     const int split = here.split, tile = here.tile, n = a.by_sets.div(here.group), head = here.group - n * a.head_sets, key_head = a.by_group.div(head), kv = a.head_sets / a.group;
@@ -112,9 +140,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
 
     int lo = 0, hi = im.len;
     if (a.causal) hi = max(0, min(hi, max(im.position(min(row0 + 63, a.Sq - 1)) + 1, im.prefix)));
-    if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; words[2] = -1000; }
-    __syncthreads();
     if (a.docs) {
+        if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; }
+        __syncthreads();
         if (row.doc >= 0) { atomicMin(&words[0], row.doc); atomicMax(&words[1], row.doc); }
         __syncthreads();
         const int d0 = words[0], d1 = words[1];
@@ -127,18 +155,20 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
         begin = min(end, begin + split * per);
         end = min(end, begin + per);
     }
-    // the largest power of two that the values of these keys carry: all weighted sums are kept at it
+    // The largest power of two that the values of these keys carry: all weighted sums are kept at it, where no tile's is less than half of it and no tile is mixed
+    // (even). Where not, each row's at its own.
     const int tiles = (a.Sk + 63) / 64;
-    const int *k_exps = a.k_exps + ((size_t)n * kv + key_head) * tiles, *v_exps = a.v_exps + ((size_t)n * kv + key_head) * tiles;
-    {
-        int most = -1000;
-        for (int x = begin / 64 + threadIdx.x; x * 64 < end; x += 256) most = max(most, v_exps[x]);
-        if (most > -1000) atomicMax(&words[2], most);
-        __syncthreads();
+    const size_t first_tile = ((size_t)n * kv + key_head) * tiles;
+    const int *k_exps = a.k_exps + first_tile, *v_exps = a.v_exps + first_tile;
+    Powers powers;
+    for (int x = begin / 64 + lane; x * 64 < end; x += 64) {
+        powers.add(v_exps[x]);
+        powers.add_mixed(k_exps[x]);
     }
-    const int v_exp = __builtin_amdgcn_readfirstlane(words[2]);
+    const bool even = powers.even(1);
+    const int v_exp = powers.most;
 
-    const char *k_image = a.k_tok + ((size_t)n * kv + key_head) * tiles * IMAGE, *v_image = a.v_tok + ((size_t)n * kv + key_head) * tiles * IMAGE;
+    const char *k_image = a.k_tok + first_tile * IMAGE, *v_image = a.v_tok + first_tile * IMAGE;
     const unsigned lds = (unsigned)(uintptr_t)(__attribute__((address_space(3))) void *)parts_lds;
     const auto copy = [&](const char *image, int j0, unsigned to) {
 #pragma unroll
@@ -164,52 +194,68 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     floatx4 o[DT] = {};
     Reference top(a, row, begin, end);
     float sum = 0.f;
+    ColumnScale vs;
     // Values are on their way while scores are computed, the next keys while values are summed; a barrier in front of either, behind which the
     // other's buffer is free.
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        const int k_exp = exponent_at(k_exps, j0 / 64), v_now = exponent_at(v_exps, j0 / 64);
-        stage_keys<64>(a, n, j0, key_code, key_doc);
-        wait_vmcnt<0>();
-        __syncthreads();
-        copy(v_image, j0, IMAGE);
-        const char *kt = parts_lds + token_place(m, g), *vt = parts_lds + IMAGE + across_place(m, g);
+    const auto walk = [&](auto is_even) {
+        constexpr bool EVEN = decltype(is_even)::value;
+        for (int j0 = begin; j0 < end; j0 += 64) {
+            const int k_word = exponents_at(k_exps, j0 / 64), v_word = exponents_at(v_exps, j0 / 64), v_now = tile_exponent(v_word);
+            int dot_exp = q_exp + tile_exponent(k_word);
+            stage_keys<64>(a, n, j0, key_code, key_doc);
+            wait_vmcnt<0>();
+            __syncthreads();
+            copy(v_image, j0, IMAGE);
+            const char *kt = parts_lds + token_place(m, g), *vt = parts_lds + IMAGE + across_place(m, g);
 
-        // (products of a step part by part over all results: one that adds to the one before it would wait for it)
-        floatx4 s[4] = {};
+            // (products of a step part by part over all results: one that adds to the one before it would wait for it)
+            floatx4 s[4] = {};
 #pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-            half8 k_hi[4], k_lo[4];
+            for (int st = 0; st < STEPS; ++st) {
+                half8 k_hi[4], k_lo[4];
 #pragma unroll
-            for (int b = 0; b < 4; ++b) k_lo[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048 + 1024);
+                for (int b = 0; b < 4; ++b) k_lo[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048 + 1024);
 #pragma unroll
-            for (int b = 0; b < 4; ++b) k_hi[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048);
+                for (int b = 0; b < 4; ++b) k_hi[b] = *reinterpret_cast<const half8 *>(kt + (b * STEPS + st) * 2048);
 #pragma unroll
-            for (int part = 0; part < 3; ++part)
+                for (int part = 0; part < 3; ++part)
 #pragma unroll
-                for (int b = 0; b < 4; ++b) s[b] = mfma16(part == 0 ? k_lo[b] : k_hi[b], part == 1 ? q_lo[st] : q_hi[st], s[b]);
+                    for (int b = 0; b < 4; ++b) s[b] = mfma16(part == 0 ? k_lo[b] : k_hi[b], part == 1 ? q_lo[st] : q_hi[st], s[b]);
+            }
+            if (!EVEN && tile_mixed(k_word)) {
+                by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g, q_exp);
+                dot_exp = 0;
+            }
+            // weights near fp16's top, and at the power of two that the sums carry
+            const int lift = !EVEN ? 0 : v_now < v_exp ? kLift - 1 : kLift;
+            const float in_exponent = (float)lift, was = top.at;
+            finish_scores<MODE>(a, s, row, dot_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
+            raise_top(s, top, sum, o, in_exponent);
+            if (!EVEN) vs.follow(top.at - was, o);
+            floatx4 part = {};
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
+                part += s[b];
+            }
+            sum = fmaf((part.x + part.y) + (part.z + part.w), ldexpf(1.f, -lift), sum);
+            if (!EVEN) {
+                if (tile_mixed(v_word)) by_token(s, a.v_each + first_tile * 64 + j0 + 4 * g);
+                vs.apply(s, tile_mixed(v_word) ? 0 : v_now, o);
+            }
+            half8 p_hi[2], p_lo[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], p_hi[b], p_lo[b]);
+            wait_vmcnt<0>();
+            __syncthreads();
+            if (j0 + 64 < end) copy(k_image, j0 + 64, 0);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) products_across<STEPS>(o, vt, b, p_hi[b], p_lo[b]);
         }
-        // weights near fp16's top, and at the power of two that the sums carry; below 2^-40, where fp16 has nothing left of them, only their own sum matters
-        const int lift = max(kLift + v_now - v_exp, -40);
-        const float in_exponent = (float)lift;
-        finish_scores<MODE>(a, s, row, q_exp + k_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
-        raise_top(s, top, sum, o, in_exponent);
-        floatx4 part = {};
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
-            part += s[b];
-        }
-        sum = fmaf((part.x + part.y) + (part.z + part.w), ldexpf(1.f, -lift), sum);
-        half8 p_hi[2], p_lo[2];
-#pragma unroll
-        for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], p_hi[b], p_lo[b]);
-        wait_vmcnt<0>();
-        __syncthreads();
-        if (j0 + 64 < end) copy(k_image, j0 + 64, 0);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) products_across<STEPS>(o, vt, b, p_hi[b], p_lo[b]);
-    }
+    };
+    if (even) walk(std::true_type{});
+    else walk(std::false_type{});
 
     const AttnArgs z = late_args();
     const float all = column_sum(sum);
@@ -223,12 +269,13 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
     if (i_raw < z.Sq && !(columns >> m & 1)) {
         const size_t part = (((size_t)n * z.heads + head) * z.Sq + i) * z.splits + split;
         const float inv = z.splits > 1 ? 1.f : all == 0.f ? 0.f : 1.f / all;
+        const int back = even ? v_exp - kLift : vs.back();
         float *token = const_cast<float *>(token_at(z.o, z.os, n, i));
 #pragma unroll
         for (int d = 0; d < DT; ++d) {
             floatx4 y;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = ldexpf(o[d][e] * inv, v_exp - kLift);
+            for (int e = 0; e < 4; ++e) y[e] = ldexpf(o[d][e] * inv, back);
             if (z.splits > 1 && z.D % 4 == 0) {
                 if (16 * d + 4 * g < z.D) *reinterpret_cast<floatx4 *>(z.part_o + part * z.D + 16 * d + 4 * g) = y;
             } else if (z.splits > 1) {

@@ -12,38 +12,13 @@
 // instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 66, keys 53.
 #include "attn_parts.h"
 
+#include <type_traits>
+
 namespace small {
 
 namespace {
 
 extern __shared__ __attribute__((aligned(1024))) char parts_lds[];
-
-// The power of two of a column's gradients: values times `scale` stay within 2^14. Zero so far: scale = limit = 0.
-struct ColumnScale {
-    float scale = 0.f, limit = 0.f;
-    // For values y that count 2^exp each: raises the scale where one passes the limit, and the sums acc along; returns the factor for y.
-    template <int NB, int DT>
-    __device__ __forceinline__ float raise(const floatx4 (&y)[NB], int exp, floatx4 (&acc)[DT])
-    {
-        float mx = 0.f;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(fabsf(y[b].x), fabsf(y[b].y)), fmaxf(fabsf(y[b].z), fabsf(y[b].w))));
-        mx = ldexpf(mx, exp);
-        if (__any(mx > limit)) {
-            mx = column_max(mx);
-            const bool more = mx > limit;
-            const int e = max(-100, (int)(__float_as_uint(mx) >> 23) - 127);
-            const float now = ldexpf(1.f, 8 - e), f = !more || scale == 0.f ? 1.f : ldexpf(now, ilogb_of(scale));
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] *= f;
-            scale = more ? now : scale;
-            limit = more ? ldexpf(1.f, 6 + e) : limit;
-        }
-        return ldexpf(scale, exp);
-    }
-    static __device__ __forceinline__ int ilogb_of(float s) { return 127 - (int)(__float_as_uint(s) >> 23); }      // (of 1 / s)
-    __device__ __forceinline__ float back(float factor) const { return scale == 0.f ? 0.f : ldexpf(factor, ilogb_of(scale)); }
-};
 
 // Two or four operands in two parts against one right operand in two parts, part by part.
 template <int NB>
@@ -201,7 +176,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             d_lo[s] = *reinterpret_cast<const half8 *>(a.do_tok + at + s * 2048 + 1024);
         }
     }
-    const int q_exp = a.q_exps[at_tile], d_exp = a.do_exps[at_tile];
+    const int q_word = exponents_at(a.q_exps, at_tile), d_word = exponents_at(a.do_exps, at_tile);
 
     int lo = 0, hi = im.len;
     if (a.causal) hi = max(0, min(hi, max(im.position(min(row0 + 63, a.Sq - 1)) + 1, im.prefix)));
@@ -219,6 +194,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     const int tiles = (a.Sk + 63) / 64;
     const size_t first_tile = ((size_t)n * kv + key_head) * tiles;
     const int *k_exps = a.k_exps + first_tile, *v_exps = a.v_exps + first_tile;
+    bool mixed = tile_mixed(q_word | d_word);
+    for (int x = begin / 64 + lane; x * 64 < end; x += 64) mixed |= tile_mixed(k_exps[x] | v_exps[x]);
     const unsigned lds = lds_address(parts_lds);
     if (begin < end) {
         copy_image(a.k_tok + (first_tile + begin / 64) * IMAGE, IMAGE, lds);
@@ -257,6 +234,76 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
 
     ColumnScale cs;
     floatx4 dq[DT] = {};
+    // (where tiles are mixed: tokens with powers of two of their own)
+    const auto walk = [&](auto is_mixed) {
+        constexpr bool MIXED = decltype(is_mixed)::value;
+        const int q_exp = MIXED ? a.q_each[at_tile * 64 + wave * 16 + m] : tile_exponent(q_word), d_exp = MIXED ? a.do_each[at_tile * 64 + wave * 16 + m] : tile_exponent(d_word);
+        for (int j0 = begin; j0 < end; j0 += 64) {
+            const int k_word = exponents_at(k_exps, j0 / 64), v_word = exponents_at(v_exps, j0 / 64);
+            int dot_exp = q_exp + tile_exponent(k_word), dp_exp = d_exp + tile_exponent(v_word);
+            stage_keys<64>(a, n, j0, key_code, key_doc);
+            wait_vmcnt<0>();
+            __syncthreads();
+            const char *kt = parts_lds + now, *vt = parts_lds + 2 * IMAGE + token_place(m, g);
+            next_keys(j0);
+            floatx4 s[4] = {}, dp_half[2] = {}, dp_turned[2] = {};
+#pragma unroll
+            for (int st = 0; st < STEPS; ++st) {
+                products(s, kt + token_place(m, g) + st * 2048, STEPS * 2048, q_hi[st], q_lo[st]);
+                products(dp_half, vt + st * 2048, STEPS * 2048, d_hi[st], d_lo[st]);
+                // half of the keys with dO's sign turned: the matrix instructions round their sums to one side, by a tenth of a spacing, and over a row
+                // that would add up in the bias's gradient, which is what is left of sums that cancel
+                products(dp_turned, vt + (2 * STEPS + st) * 2048, STEPS * 2048, -d_hi[st], -d_lo[st]);
+            }
+            floatx4 dp[4] = {dp_half[0], dp_half[1], -dp_turned[0], -dp_turned[1]};
+            if (MIXED && tile_mixed(v_word)) {
+                by_token(dp, a.v_each + first_tile * 64 + j0 + 4 * g, d_exp);
+                dp_exp = 0;
+            }
+            if (MIXED && tile_mixed(k_word)) {
+                by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g, q_exp);
+                dot_exp = 0;
+            }
+            const float dp_in = ldexpf(1.f, dp_exp);
+            floatx4 core[4];
+            finish_scores<MODE>(a, s, row, dot_exp, lse2, j0, key_code, key_doc, g, bias, far_lo, far_hi, (MODE & 1) ? core : nullptr);
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const float p = __builtin_amdgcn_exp2f(s[b][e]);
+                    if (MODE & 2) total += p;
+                    s[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -delta);
+                }
+            if (sums) {
+                const bool all_lo = __all(key_code[63] - row.code <= -a.reach), all_hi = __all(key_code[0] - row.code >= a.reach);
+                if (all_lo || all_hi) {
+                    float x = 0.f;
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) x += (s[b].x + s[b].y) + (s[b].z + s[b].w);
+                    sum_lo += all_lo ? x : 0.f;
+                    sum_hi += all_lo ? 0.f : x;
+                } else {
+                    if (a.width == 1) sums_in_line(s, a.reach, j0 + 4 * g - (im.first + i_raw), m, g, per_wave, mine, sum_lo, sum_hi);
+                    else sums_in_image(s, a.reach, key_code, row.code, i_raw < a.Sq, a.Sk - j0, g, per_wave, mine, sum_lo, sum_hi);
+                }
+            }
+            if ((MODE & 1) && a.cap > 0.f)
+#pragma unroll
+                for (int b = 0; b < 4; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
+            if (MIXED && tile_mixed(k_word)) by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g);
+            cs.apply(s, MIXED && tile_mixed(k_word) ? 0 : tile_exponent(k_word), dq);
+            half8 hi_[2], lo_[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], hi_[b], lo_[b]);
+            __syncthreads();
+            next_values(j0);
+#pragma unroll
+            for (int b = 0; b < 2; ++b) products_across<STEPS>(dq, kt + across_place(m, g), b, hi_[b], lo_[b]);
+        }
+    };
     // (a wave whose rows are all past the end does its share of the copies only)
     if (__builtin_amdgcn_readfirstlane(row0 + wave * 16) >= a.Sq)
         for (int j0 = begin; j0 < end; j0 += 64) {
@@ -266,64 +313,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             __syncthreads();
             next_values(j0);
         }
-    else
-    for (int j0 = begin; j0 < end; j0 += 64) {
-        const int k_exp = exponent_at(k_exps, j0 / 64), v_exp = exponent_at(v_exps, j0 / 64);
-        stage_keys<64>(a, n, j0, key_code, key_doc);
-        wait_vmcnt<0>();
-        __syncthreads();
-        const char *kt = parts_lds + now, *vt = parts_lds + 2 * IMAGE + token_place(m, g);
-        next_keys(j0);
-        floatx4 s[4] = {}, dp_half[2] = {}, dp_turned[2] = {};
-#pragma unroll
-        for (int st = 0; st < STEPS; ++st) {
-            products(s, kt + token_place(m, g) + st * 2048, STEPS * 2048, q_hi[st], q_lo[st]);
-            products(dp_half, vt + st * 2048, STEPS * 2048, d_hi[st], d_lo[st]);
-            // half of the keys with dO's sign turned: the matrix instructions round their sums to one side, by a tenth of a spacing, and over a row
-            // that would add up in the bias's gradient, which is what is left of sums that cancel
-            products(dp_turned, vt + (2 * STEPS + st) * 2048, STEPS * 2048, -d_hi[st], -d_lo[st]);
-        }
-        const floatx4 dp[4] = {dp_half[0], dp_half[1], -dp_turned[0], -dp_turned[1]};
-        const float dp_in = ldexpf(1.f, v_exp + d_exp);
-        floatx4 core[4];
-        finish_scores<MODE>(a, s, row, q_exp + k_exp, lse2, j0, key_code, key_doc, g, bias, far_lo, far_hi, (MODE & 1) ? core : nullptr);
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float p = __builtin_amdgcn_exp2f(s[b][e]);
-                if (MODE & 2) total += p;
-                s[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -delta);
-            }
-        if (sums) {
-            const bool all_lo = __all(key_code[63] - row.code <= -a.reach), all_hi = __all(key_code[0] - row.code >= a.reach);
-            if (all_lo || all_hi) {
-                float x = 0.f;
-#pragma unroll
-                for (int b = 0; b < 4; ++b) x += (s[b].x + s[b].y) + (s[b].z + s[b].w);
-                sum_lo += all_lo ? x : 0.f;
-                sum_hi += all_lo ? 0.f : x;
-            } else {
-                if (a.width == 1) sums_in_line(s, a.reach, j0 + 4 * g - (im.first + i_raw), m, g, per_wave, mine, sum_lo, sum_hi);
-                else sums_in_image(s, a.reach, key_code, row.code, i_raw < a.Sq, a.Sk - j0, g, per_wave, mine, sum_lo, sum_hi);
-            }
-        }
-        if ((MODE & 1) && a.cap > 0.f)
-#pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
-        const float f = cs.raise(s, k_exp, dq);
-        half8 hi_[2], lo_[2];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) s[b] *= f;
-#pragma unroll
-        for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], hi_[b], lo_[b]);
-        __syncthreads();
-        next_values(j0);
-#pragma unroll
-        for (int b = 0; b < 2; ++b) products_across<STEPS>(dq, kt + across_place(m, g), b, hi_[b], lo_[b]);
-    }
+    else if (__any(mixed)) walk(std::true_type{});
+    else walk(std::false_type{});
     const AttnArgs z = late_args();
     if (sums) {
         __shared__ float ends[8];
@@ -362,7 +353,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         int p[32], code[32], bound[36], doc[36];       // bound[32]: the smallest; doc[32]: of all rows, or -3
     };
     __shared__ alignas(16) Rows rows_of[2];
-    __shared__ int words[3];
+    __shared__ int words[2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
     const int by_part = a.by_splits.div((int)id), part = (int)id - by_part * a.splits;
@@ -383,13 +374,13 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             v_lo[s] = *reinterpret_cast<const half8 *>(a.v_tok + at + s * 2048 + 1024);
         }
     }
-    const int k_exp = a.k_exps[at_tile], v_exp = a.v_exps[at_tile];
+    const int k_word = exponents_at(a.k_exps, at_tile), v_word = exponents_at(a.v_exps, at_tile);
     // rows that can see any of the keys; this part's heads, and of their rows its share
     int lo = 0, hi = j0 < im.len ? a.Sq : 0;
     if (a.causal && im.prefix <= j0) lo = max(0, min(a.Sq, j0 - im.first));
-    if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; words[2] = -1000; }
-    __syncthreads();
     if (a.docs) {
+        if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; }
+        __syncthreads();
         if (j_raw < im.len && doc >= 0) { atomicMin(&words[0], doc); atomicMax(&words[1], doc); }
         __syncthreads();
         const int d0 = words[0], d1 = words[1];
@@ -410,196 +401,219 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         begin = min(end, begin + row_part * per);
         end = min(end, begin + per);
     }
-    // the largest power of two that these rows' dO carry: all of dV's sums are kept at it
-    {
-        int most = -1000;
-        for (int h = h0; h < h1; ++h)
-            for (int x = begin / 64 + threadIdx.x; x * 64 < end; x += 256) most = max(most, a.do_exps[((size_t)n * a.heads + h) * a.row_tiles + x]);
-        if (most > -1000) atomicMax(&words[2], most);
-        __syncthreads();
-    }
-    const int d_most = __builtin_amdgcn_readfirstlane(words[2]);
+    // The largest power of two that these rows' dO carry: all of dV's sums are kept at it, where no tile's is less than 2^-4 of it and no tile is mixed, these keys' included (even).
+    // Where not, each key's at its own.
+    Powers powers;
+    powers.add_mixed(k_word | v_word);
+    for (int h = h0; h < h1; ++h)
+        for (int x = begin / 64 + lane; x * 64 < end; x += 64) {
+            const size_t at = ((size_t)n * a.heads + h) * a.row_tiles + x;
+            powers.add(a.do_exps[at]);
+            powers.add_mixed(a.q_exps[at]);
+        }
+    const bool even = powers.even(4);
+    const int d_most = powers.most;
 
     float *const bias_lds = reinterpret_cast<float *>(parts_lds + 4 * HALF);
     const unsigned lds = lds_address(parts_lds);
     // (a wave whose keys are all past the end, of the image or of its length, does its share of the copies only)
     const bool idle = __builtin_amdgcn_readfirstlane(j0 + wave * 16) >= im.len;
-    ColumnScale cs;
+    ColumnScale cs, vs;
     floatx4 dk[DT] = {}, dv[DT] = {};
-    for (int head = h0; head < h1 && begin < end; ++head) {
-        const float slope = (MODE & 2) && a.slopes ? a.slopes[head] * kLog2e : 0.f;
-        const float *bias = nullptr;
-        float far_lo = 0.f, far_hi = 0.f;
-        __syncthreads();                                                        // (the last head's tiles and bias are still read)
-        if ((MODE & 4) && a.table) {
-            if (a.bias_lds) {
-                expand_bias(a, head, bias_lds);
-                bias = bias_lds;
+    const auto walk = [&](auto is_even) {
+        constexpr bool EVEN = decltype(is_even)::value;
+        const int k_exp = EVEN ? tile_exponent(k_word) : a.k_each[at_tile * 64 + wave * 16 + m], v_exp = EVEN ? tile_exponent(v_word) : a.v_each[at_tile * 64 + wave * 16 + m];
+        for (int head = h0; head < h1 && begin < end; ++head) {
+            const float slope = (MODE & 2) && a.slopes ? a.slopes[head] * kLog2e : 0.f;
+            const float *bias = nullptr;
+            float far_lo = 0.f, far_hi = 0.f;
+            __syncthreads();                                                        // (the last head's tiles and bias are still read)
+            if ((MODE & 4) && a.table) {
+                if (a.bias_lds) {
+                    expand_bias(a, head, bias_lds);
+                    bias = bias_lds;
+                }
+                far_lo = bias_gather(a, head, 0);
+                far_hi = bias_gather(a, head, 2 * a.reach);
             }
-            far_lo = bias_gather(a, head, 0);
-            far_hi = bias_gather(a, head, 2 * a.reach);
-        }
-        const size_t first_row = ((size_t)n * a.heads + head) * a.Sq, first_tile = ((size_t)n * a.heads + head) * a.row_tiles;
-        const auto at = [&](int i0) { return (first_tile + i0 / 64) * IMAGE + (i0 & 32 ? HALF : 0); };
-        // While a tile is worked on, the next one is copied into the other of two buffers; one barrier a tile.
-        unsigned now = 0;
-        const auto copy_rows = [&](int i0, unsigned to) {
-            copy_image(a.q_tok + at(i0), HALF, lds + to);
-            copy_image(a.do_tok + at(i0), HALF, lds + to + HALF);
-        };
-        copy_rows(begin, 0);
-        if (idle)
+            const size_t first_row = ((size_t)n * a.heads + head) * a.Sq, first_tile = ((size_t)n * a.heads + head) * a.row_tiles;
+            const auto at = [&](int i0) { return (first_tile + i0 / 64) * IMAGE + (i0 & 32 ? HALF : 0); };
+            // While a tile is worked on, the next one is copied into the other of two buffers; one barrier a tile.
+            unsigned now = 0;
+            const auto copy_rows = [&](int i0, unsigned to) {
+                copy_image(a.q_tok + at(i0), HALF, lds + to);
+                copy_image(a.do_tok + at(i0), HALF, lds + to + HALF);
+            };
+            copy_rows(begin, 0);
+            if (idle)
+                for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
+                    wait_vmcnt<0>();
+                    __syncthreads();
+                    if (i0 + 32 < end) copy_rows(i0 + 32, now ^ 2 * HALF);
+                }
+            else
             for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
+                Rows &rows = rows_of[now != 0];
+                const int q_word = exponents_at(a.q_exps, first_tile + i0 / 64), d_word = exponents_at(a.do_exps, first_tile + i0 / 64);
+                const int q_exp = tile_exponent(q_word), d_exp = tile_exponent(d_word);
+                int dot_exp = q_exp + k_exp, dp_exp = v_exp + d_exp;
+                if (threadIdx.x < 32) {
+                    const int i = i0 + threadIdx.x, ii = min(i, a.Sq - 1);
+                    const RowState row(a, im, n, i, head);
+                    const float lse = i < a.Sq ? a.lse_in[first_row + ii] : -kInf;
+                    const bool dead = lse == -kInf;
+                    rows.lse[threadIdx.x] = dead ? kInf : lse * kLog2e;
+                    rows.delta[threadIdx.x] = dead ? 0.f : a.delta[first_row + ii];
+                    if ((MODE & 2) && a.slopes) rows.share[threadIdx.x] = a.share[first_row + ii];
+                    rows.p[threadIdx.x] = row.p;
+                    rows.code[threadIdx.x] = i < a.Sq ? row.code : RowState(a, im, n, ii, head).code;
+                    rows.bound[threadIdx.x] = row.bound;
+                    rows.doc[threadIdx.x] = row.doc;
+                    int least = row.bound;
+                    for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor(least, d));
+                    rows.bound[32] = least;
+                    rows.doc[32] = -3;
+                    const int first = __builtin_amdgcn_readfirstlane(row.doc);
+                    if (__all(row.doc == first)) rows.doc[32] = first;
+                }
                 wait_vmcnt<0>();
                 __syncthreads();
                 if (i0 + 32 < end) copy_rows(i0 + 32, now ^ 2 * HALF);
-            }
-        else
-        for (int i0 = begin; i0 < end; i0 += 32, now ^= 2 * HALF) {
-            Rows &rows = rows_of[now != 0];
-            const int q_exp = exponent_at(a.q_exps, first_tile + i0 / 64), d_exp = exponent_at(a.do_exps, first_tile + i0 / 64);
-            if (threadIdx.x < 32) {
-                const int i = i0 + threadIdx.x, ii = min(i, a.Sq - 1);
-                const RowState row(a, im, n, i, head);
-                const float lse = i < a.Sq ? a.lse_in[first_row + ii] : -kInf;
-                const bool dead = lse == -kInf;
-                rows.lse[threadIdx.x] = dead ? kInf : lse * kLog2e;
-                rows.delta[threadIdx.x] = dead ? 0.f : a.delta[first_row + ii];
-                if ((MODE & 2) && a.slopes) rows.share[threadIdx.x] = a.share[first_row + ii];
-                rows.p[threadIdx.x] = row.p;
-                rows.code[threadIdx.x] = i < a.Sq ? row.code : RowState(a, im, n, ii, head).code;
-                rows.bound[threadIdx.x] = row.bound;
-                rows.doc[threadIdx.x] = row.doc;
-                int least = row.bound;
-                for (int d = 16; d; d >>= 1) least = min(least, __shfl_xor(least, d));
-                rows.bound[32] = least;
-                rows.doc[32] = -3;
-                const int first = __builtin_amdgcn_readfirstlane(row.doc);
-                if (__all(row.doc == first)) rows.doc[32] = first;
-            }
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (i0 + 32 < end) copy_rows(i0 + 32, now ^ 2 * HALF);
-            const char *tile_at = parts_lds + now, *qt = tile_at + token_place(m, g);
-            floatx4 s[2] = {}, dp[2] = {};
+                const char *tile_at = parts_lds + now, *qt = tile_at + token_place(m, g);
+                floatx4 s[2] = {}, dp[2] = {};
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                products(s, qt + st * 2048, STEPS * 2048, k_hi[st], k_lo[st]);
-                products(dp, qt + HALF + st * 2048, STEPS * 2048, v_hi[st], v_lo[st]);
-            }
-            const float dp_in = ldexpf(1.f, v_exp + d_exp);
-            const bool capped = (MODE & 1) && a.cap > 0.f;
-            float in = ldexpf(capped ? a.scale / a.cap : a.scale * kLog2e, q_exp + k_exp);
-            floatx4 core[2];
-            if (capped) {
+                for (int st = 0; st < STEPS; ++st) {
+                    products(s, qt + st * 2048, STEPS * 2048, k_hi[st], k_lo[st]);
+                    products(dp, qt + HALF + st * 2048, STEPS * 2048, v_hi[st], v_lo[st]);
+                }
+                if (!EVEN && tile_mixed(q_word)) {
+                    by_token(s, a.q_each + first_tile * 64 + i0 + 4 * g, k_exp);
+                    dot_exp = 0;
+                }
+                if (!EVEN && tile_mixed(d_word)) {
+                    by_token(dp, a.do_each + first_tile * 64 + i0 + 4 * g, v_exp);
+                    dp_exp = 0;
+                }
+                const float dp_in = ldexpf(1.f, dp_exp);
+                const bool capped = (MODE & 1) && a.cap > 0.f;
+                float in = ldexpf(capped ? a.scale / a.cap : a.scale * kLog2e, dot_exp);
+                floatx4 core[2];
+                if (capped) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b) s[b] *= in;
-                tanh_all(s);
+                    for (int b = 0; b < 2; ++b) s[b] *= in;
+                    tanh_all(s);
 #pragma unroll
-                for (int b = 0; b < 2; ++b) core[b] = s[b];
-                in = a.cap * kLog2e;
-            }
-            bool near = false;
-            float base = 0.f;
-            if ((MODE & 4) && a.table) {
-                const bool all_lo = __all(code - rows.code[0] <= -a.reach), all_hi = __all(code - rows.code[31] >= a.reach);
-                near = !all_lo && !all_hi;
-                base = all_lo ? far_lo : all_hi ? far_hi : 0.f;
-            }
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const floatx4 l4 = *reinterpret_cast<const floatx4 *>(rows.lse + 16 * b + 4 * g);
-                floatx4 u = base - l4;
-                if ((MODE & 2) && a.slopes) {
-                    const int4 p4 = *reinterpret_cast<const int4 *>(rows.p + 16 * b + 4 * g);
-                    u.x = fmaf(-slope, fabsf((float)(p4.x - j)), u.x);
-                    u.y = fmaf(-slope, fabsf((float)(p4.y - j)), u.y);
-                    u.z = fmaf(-slope, fabsf((float)(p4.z - j)), u.z);
-                    u.w = fmaf(-slope, fabsf((float)(p4.w - j)), u.w);
+                    for (int b = 0; b < 2; ++b) core[b] = s[b];
+                    in = a.cap * kLog2e;
+                }
+                bool near = false;
+                float base = 0.f;
+                if ((MODE & 4) && a.table) {
+                    const bool all_lo = __all(code - rows.code[0] <= -a.reach), all_hi = __all(code - rows.code[31] >= a.reach);
+                    near = !all_lo && !all_hi;
+                    base = all_lo ? far_lo : all_hi ? far_hi : 0.f;
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, u[e]);
-            }
-            const int first = code - rows.code[0] - 4 * g + a.reach;
-            if (near && bias && a.width == 1 && __all((first <= 2 * a.reach) & (first >= 19))) {
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b][e] += bias[first - 16 * b - e];
-            } else if (near && bias && __all((code - rows.code[31] >= -a.reach) & (code - rows.code[0] <= a.reach))) {
-                const int here = a.reach + code;
-#pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
-                    s[b].x += bias[here - c4.x];
-                    s[b].y += bias[here - c4.y];
-                    s[b].z += bias[here - c4.z];
-                    s[b].w += bias[here - c4.w];
+                    const floatx4 l4 = *reinterpret_cast<const floatx4 *>(rows.lse + 16 * b + 4 * g);
+                    floatx4 u = base - l4;
+                    if ((MODE & 2) && a.slopes) {
+                        const int4 p4 = *reinterpret_cast<const int4 *>(rows.p + 16 * b + 4 * g);
+                        u.x = fmaf(-slope, fabsf((float)(p4.x - j)), u.x);
+                        u.y = fmaf(-slope, fabsf((float)(p4.y - j)), u.y);
+                        u.z = fmaf(-slope, fabsf((float)(p4.z - j)), u.z);
+                        u.w = fmaf(-slope, fabsf((float)(p4.w - j)), u.w);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, u[e]);
                 }
-            } else if (near) {
+                const int first = code - rows.code[0] - 4 * g + a.reach;
+                if (near && bias && a.width == 1 && __all((first <= 2 * a.reach) & (first >= 19))) {
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
-                    const int codes[4] = {c4.x, c4.y, c4.z, c4.w};
+                    for (int b = 0; b < 2; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const int x = offset_at(a, code, codes[e]);
-                        s[b][e] += bias ? bias[x] : bias_gather(a, head, x);
+                        for (int e = 0; e < 4; ++e) s[b][e] += bias[first - 16 * b - e];
+                } else if (near && bias && __all((code - rows.code[31] >= -a.reach) & (code - rows.code[0] <= a.reach))) {
+                    const int here = a.reach + code;
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
+                        s[b].x += bias[here - c4.x];
+                        s[b].y += bias[here - c4.y];
+                        s[b].z += bias[here - c4.z];
+                        s[b].w += bias[here - c4.w];
+                    }
+                } else if (near) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int4 c4 = *reinterpret_cast<const int4 *>(rows.code + 16 * b + 4 * g);
+                        const int codes[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const int x = offset_at(a, code, codes[e]);
+                            s[b][e] += bias ? bias[x] : bias_gather(a, head, x);
+                        }
                     }
                 }
-            }
-            if (!__all(j_raw < rows.bound[32])) {
+                if (!__all(j_raw < rows.bound[32])) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int4 x = *reinterpret_cast<const int4 *>(rows.bound + 16 * b + 4 * g);
+                        s[b].x = j_raw < x.x ? s[b].x : -kInf;
+                        s[b].y = j_raw < x.y ? s[b].y : -kInf;
+                        s[b].z = j_raw < x.z ? s[b].z : -kInf;
+                        s[b].w = j_raw < x.w ? s[b].w : -kInf;
+                    }
+                }
+                if (a.docs && !__all(rows.doc[32] == doc)) {
+#pragma unroll
+                    for (int b = 0; b < 2; ++b) {
+                        const int4 x = *reinterpret_cast<const int4 *>(rows.doc + 16 * b + 4 * g);
+                        s[b].x = x.x == doc ? s[b].x : -kInf;
+                        s[b].y = x.y == doc ? s[b].y : -kInf;
+                        s[b].z = x.z == doc ? s[b].z : -kInf;
+                        s[b].w = x.w == doc ? s[b].w : -kInf;
+                    }
+                }
+                const float lift = EVEN ? ldexpf(1.f, max(0, 14 + d_exp - d_most)) : 1.f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
-                    const int4 x = *reinterpret_cast<const int4 *>(rows.bound + 16 * b + 4 * g);
-                    s[b].x = j_raw < x.x ? s[b].x : -kInf;
-                    s[b].y = j_raw < x.y ? s[b].y : -kInf;
-                    s[b].z = j_raw < x.z ? s[b].z : -kInf;
-                    s[b].w = j_raw < x.w ? s[b].w : -kInf;
+                    const floatx4 d4 = *reinterpret_cast<const floatx4 *>(rows.delta + 16 * b + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
+                    if ((MODE & 2) && a.slopes) s[b] *= *reinterpret_cast<const floatx4 *>(rows.share + 16 * b + 4 * g);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float p = s[b][e];
+                        dp[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -d4[e]);
+                        s[b][e] = p * lift;
+                    }
                 }
-            }
-            if (a.docs && !__all(rows.doc[32] == doc)) {
+                if (capped)
 #pragma unroll
-                for (int b = 0; b < 2; ++b) {
-                    const int4 x = *reinterpret_cast<const int4 *>(rows.doc + 16 * b + 4 * g);
-                    s[b].x = x.x == doc ? s[b].x : -kInf;
-                    s[b].y = x.y == doc ? s[b].y : -kInf;
-                    s[b].z = x.z == doc ? s[b].z : -kInf;
-                    s[b].w = x.w == doc ? s[b].w : -kInf;
+                    for (int b = 0; b < 2; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) dp[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
+                const bool q_mixed = !EVEN && tile_mixed(q_word);
+                if (q_mixed) by_token(dp, a.q_each + first_tile * 64 + i0 + 4 * g);
+                cs.apply(dp, q_mixed ? 0 : q_exp, dk);
+                if (!EVEN) {
+                    if (tile_mixed(d_word)) by_token(s, a.do_each + first_tile * 64 + i0 + 4 * g);
+                    vs.apply(s, tile_mixed(d_word) ? 0 : d_exp, dv);
                 }
+                half8 p_hi, p_lo, s_hi, s_lo;
+                split_results(s[0], s[1], p_hi, p_lo);
+                split_results(dp[0], dp[1], s_hi, s_lo);
+                products_across<STEPS>(dv, tile_at + HALF + across_place(m, g), 0, p_hi, p_lo);
+                products_across<STEPS>(dk, tile_at + across_place(m, g), 0, s_hi, s_lo);
             }
-            const float lift = ldexpf(1.f, max(-120, 14 + d_exp - d_most));
-#pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const floatx4 d4 = *reinterpret_cast<const floatx4 *>(rows.delta + 16 * b + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
-                if ((MODE & 2) && a.slopes) s[b] *= *reinterpret_cast<const floatx4 *>(rows.share + 16 * b + 4 * g);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float p = s[b][e];
-                    dp[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -d4[e]);
-                    s[b][e] = p * lift;
-                }
-            }
-            if (capped)
-#pragma unroll
-                for (int b = 0; b < 2; ++b)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) dp[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
-            const float f = cs.raise(dp, q_exp, dk);
-#pragma unroll
-            for (int b = 0; b < 2; ++b) dp[b] *= f;
-            half8 p_hi, p_lo, s_hi, s_lo;
-            split_results(s[0], s[1], p_hi, p_lo);
-            split_results(dp[0], dp[1], s_hi, s_lo);
-            products_across<STEPS>(dv, tile_at + HALF + across_place(m, g), 0, p_hi, p_lo);
-            products_across<STEPS>(dk, tile_at + across_place(m, g), 0, s_hi, s_lo);
         }
-    }
+    };
+    if (even) walk(std::true_type{});
+    else walk(std::false_type{});
     const AttnArgs z = late_args();
     if (j_raw >= z.Sk) return;
-    const float dk_back = cs.back(z.scale), dv_back = d_most == -1000 ? 0.f : ldexpf(1.f, d_most - 14);
+    const float dk_back = cs.back(z.scale), dv_back = even ? ldexpf(1.f, d_most - 14) : vs.back(1.f);
     if (z.splits > 1) {
         // [part][image, key head][key][dk, dv][D]
         float *to = z.part_o + ((((size_t)part * z.N + n) * kv + key_head) * z.Sk + j) * 2 * z.D;

@@ -34,9 +34,10 @@ struct AttnArgs {
     FastDiv by_Cb, by_Sq, by_width, by_tiles, by_sets, by_splits, by_group;
     float *part_o;
     float2 *part_ml;              // splits > 1: results before joining, and their (maximum, sum)
-    // values in two parts (attn_parts.h): images of keys and values, their powers of two
+    // values in two parts (attn_parts.h): images of keys and values, their powers of two by tile and by token
     const char *k_tok, *v_tok, *q_tok, *do_tok;
     const int *k_exps, *v_exps, *q_exps, *do_exps;
+    const int *k_each, *v_each, *q_each, *do_each;
     // gradient
     const float *dout, *lse_in;
     float *share;                                            // [N * heads][Sq]: what a row's weights, taken from its lse, are to be multiplied by (with slopes)

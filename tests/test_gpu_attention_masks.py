@@ -131,6 +131,83 @@ def everything(c):
     return dict(zip(("out", "lse", "dq", "dk", "dv") + (("dtable",) if c.table is not None else ()), gradients(c)))
 
 
+# Shapes of each kernel: fp16 parts (with one workgroup a row tile, with keys split over several, with the forms of their biases), fp32 (gradients: heads of
+# more than 128 channels or a reach past 2047), few rows.
+SHAPES = {
+    "parts": dict(Sq=640, heads=4, D=64), "parts, many rows": dict(Sq=640, heads=24, kv=8, D=32), "parts, odd heads": dict(Sq=700, heads=4, D=37, Cb=37),
+    "parts, 128 channels": dict(Sq=500, heads=4, D=128), "parts, distances": dict(Sq=640, heads=4, D=64, slopes=True),
+    "parts, capped, buckets": dict(Sq=640, heads=4, kv=2, D=64, cap=10.0, bias="log"), "parts, everything": dict(Sq=640, heads=4, D=48, cap=10.0, bias="log", slopes=True),
+    "fp32": dict(Sq=200, heads=2, D=32, bias="wide"), "fp32, wide heads": dict(Sq=150, heads=2, D=200, Cb=8), "small": dict(Sq=100, heads=2, D=16),
+}
+
+
+def causal(S):
+    return dict(causal=True)
+
+
+def documents(S):
+    return dict(docs=_docs(1, S, [[S // 3 + 5, S - S // 3 - 5]]))
+
+
+@pytest.mark.parametrize("big", [1e6, 1e20])
+@pytest.mark.parametrize("mask", [causal, documents], ids=["causal", "documents"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_large_values_in_hidden_places(shape, mask, big):
+    """Finite values far larger than the others, in places that a part of the rows does not see (for queries and dout: whose row does not see a part of
+    the keys): in no tensor do they change what does not depend on them. One tensor after another; the others keep their size. (What does depend on a large key or query
+    has scores of its size, and is left out.)"""
+    S = SHAPES[shape]["Sq"]
+    edge = S // 3 + 5                                            # the first row of the second document
+    rows = torch.arange(S)
+    for name in ("v", "k", "dout", "q"):
+        c = Case(**SHAPES[shape], **mask(S))
+        # (keys: late tokens of the first document, and of the sequence; rows: early ones of both)
+        places = [edge - 2, S - 40] if name in "kv" else [edge - 15, edge + 7]
+        if mask is documents and name in "kq":
+            places = places[:1]                                  # (one document keeps its size)
+        getattr(c, name)[0, :, places] *= big
+        where = None
+        if name == "k":
+            good_rows = rows < places[0] if mask is causal else rows >= edge
+            good_keys = torch.zeros(S, dtype=torch.bool) if mask is causal else rows >= edge
+            where = {"out": good_rows, "lse": good_rows, "dq": good_rows, "dk": good_keys, "dv": good_keys, "dtable": torch.tensor(False)}
+        elif name == "q":
+            good_rows = torch.ones(S, dtype=torch.bool)
+            good_rows[places] = False
+            good_keys = rows > places[-1] if mask is causal else rows >= edge
+            where = {"out": good_rows, "lse": good_rows, "dq": good_rows, "dk": good_keys, "dv": good_keys, "dtable": torch.tensor(False)}
+        try:
+            compare(c, everything(c), exact(c), where)
+        except AssertionError as e:
+            raise AssertionError(f"{name}: {e}") from None
+
+
+@pytest.mark.parametrize("step", [1.0, 20.0])
+@pytest.mark.parametrize("shape", ["parts", "parts, many rows", "parts, capped, buckets", "fp32"])
+def test_magnitudes_that_rise_along_a_sequence(shape, step):
+    """Values and dout that double every `step` tokens: early rows see small values only, late keys only small rows."""
+    S = SHAPES[shape]["Sq"]
+    c = Case(**SHAPES[shape], causal=True)
+    rise = 2.0 ** (torch.arange(S) / step).floor().clamp(max=60)
+    c.v, c.dout = c.v * rise, c.dout * rise.flip(0)
+    compare(c, everything(c), exact(c))
+
+
+@pytest.mark.parametrize("Sq,Sk", [(300, 3100), (64, 4000), (1, 3000)])
+def test_large_values_in_hidden_places_of_long_caches(Sq, Sk):
+    """Rows whose keys are split over workgroups, and single tokens."""
+    for name in ("v", "k"):
+        c = Case(N=2, Sq=Sq, Sk=Sk, heads=4, D=64, docs=_docs(2, Sk, [[1500, Sk - 1500], [Sk - 5, 5]]))
+        getattr(c, name)[:, :, [10, 1499, Sk - 7]] *= 1e20
+        got = c.forward()
+        where = None
+        if name == "k":                                          # (rows that see none of these)
+            at = Sk - Sq + torch.arange(Sq)
+            good = torch.stack([torch.zeros(Sq, dtype=torch.bool), at >= Sk - 5])[:, None].expand(2, 1, Sq)
+            where = {"out": good, "lse": good}
+        compare(c, {"out": plain(got[0]), "lse": got[1]}, exact(c), where)
+
+
 # ---------------------------------------------------------------------------------------------------- biases
 
 def with_offsets(c, reach, buckets=None):
