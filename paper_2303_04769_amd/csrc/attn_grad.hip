@@ -27,6 +27,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
     __shared__ float kt[T::kFloats], vt[T::kFloats];
     __shared__ alignas(16) int key_code[KT];
     __shared__ alignas(16) int key_doc[KT];
+    __shared__ int key_bad[KT], any_bad;                          // j0 of a tile in which the key, or any, is bad (put_finite)
     __shared__ int row_code[64], words[2];
     __shared__ float ends[8];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
@@ -61,6 +62,8 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
         if (g == 0 && i_raw < a.Sq) a.delta[at_row] = delta;
     }
     if (g == 0) row_code[wave * 16 + m] = row.code;
+    if (threadIdx.x < KT) key_bad[threadIdx.x] = -1;              // (a barrier is in front of the first tile)
+    if (threadIdx.x == 0) any_bad = -1;
 
     int lo = 0, hi = im.len;
     if (a.causal) hi = max(0, min(hi, max(im.position(min(row0 + 63, a.Sq - 1)) + 1, im.prefix)));
@@ -107,7 +110,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
     if (lo < hi) fetch(lo);
     for (int j0 = lo; j0 < hi; j0 += KT) {
         __syncthreads();
-        T::put(kt, kx);
+        T::put_finite(kt, kx, key_bad, &any_bad, j0);
         T::put(vt, vx);
         if (threadIdx.x < KT) {
             const int j = j0 + threadIdx.x;
@@ -129,7 +132,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
                     dp[b] = mfma(y[e], dout[c][e], dp[b]);
                 }
             }
-        const bool edge = a.docs || !__all(j0 + KT <= row.bound);
+        const bool edge = a.docs || !__all(j0 + KT <= row.bound), bad = any_bad == j0;
         const bool all_lo = a.table && __all(key_code[KT - 1] - row.code <= -a.reach), all_hi = a.table && __all(key_code[0] - row.code >= a.reach);
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
@@ -155,6 +158,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
                         t += bias ? bias[at] : bias_gather(a, head, at);
                     }
                 }
+                if (bad) t = key_bad[16 * b + 4 * g + e] == j0 ? __builtin_nanf("") : t;
                 const float p = __builtin_amdgcn_exp2f(t);
                 float ds = p * (dp[b][e] - delta);
                 const bool seen = !edge | row.sees(j, docs[e], true);
@@ -235,6 +239,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
     __shared__ alignas(16) int row_code[KT];
     __shared__ alignas(16) int row_bound[KT];
     __shared__ alignas(16) int row_doc[KT];
+    __shared__ int row_bad[KT], any_bad;                          // number of a tile in which the row, or any, is bad (put_finite)
     __shared__ int words[2];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
     const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
@@ -276,6 +281,9 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
     }
     const int size = 2 * a.reach + 1;
     const Scorer sc(a);
+    if (threadIdx.x < KT) row_bad[threadIdx.x] = -1;              // (a barrier is in front of the first tile)
+    if (threadIdx.x == 0) any_bad = -1;
+    int number = 0;
     floatx4 dk[DT] = {}, dv[DT] = {};
     floatx4 qx[T::kQuads], dx[T::kQuads];
     for (int head = key_head * a.group; head < (key_head + 1) * a.group && lo < hi; ++head) {
@@ -300,10 +308,10 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
             T::template fetch<VEC>(dx, a, a.dos, a.dout, n, head * a.D, i0, on);
         };
         fetch(lo);
-        for (int i0 = lo; i0 < hi; i0 += KT) {
+        for (int i0 = lo; i0 < hi; i0 += KT, ++number) {
             __syncthreads();
-            T::put(qt, qx);
-            T::put(dt, dx);
+            T::put_finite(qt, qx, row_bad, &any_bad, number);
+            T::put_finite(dt, dx, row_bad, &any_bad, number);
             if (threadIdx.x < KT) {
                 const int i = i0 + threadIdx.x, ii = min(i, a.Sq - 1);
                 const RowState row(a, im, n, i, head);
@@ -331,7 +339,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
                         dp[b] = mfma(y[e], v[c][e], dp[b]);
                     }
                 }
-            const bool all_lo = a.table && __all(code - row_code[0] <= -a.reach), all_hi = a.table && __all(code - row_code[KT - 1] >= a.reach);
+            const bool all_lo = a.table && __all(code - row_code[0] <= -a.reach), all_hi = a.table && __all(code - row_code[KT - 1] >= a.reach), bad = any_bad == number;
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 const floatx4 l4 = *reinterpret_cast<const floatx4 *>(row_lse + 16 * b + 4 * g), d4 = *reinterpret_cast<const floatx4 *>(row_delta + 16 * b + 4 * g);
@@ -363,11 +371,12 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_keys(AttnArgs 
                             t += bias ? bias[at] : bias_gather(a, head, at);
                         }
                     }
+                    if (bad) t = row_bad[16 * b + 4 * g + e] == number ? __builtin_nanf("") : t;
                     const bool seen = (j_raw < bounds[e]) & (docs[e] == doc);
                     const float p = seen ? __builtin_amdgcn_exp2f(t) * h4[e] : 0.f;
                     const float ds = seen ? p * (dp[b][e] - d4[e]) : 0.f;
                     s[b][e] = p;
-                    dp[b][e] = a.cap > 0.f ? ds * fmaf(-core, core, 1.f) : ds;
+                    dp[b][e] = a.cap > 0.f && ds != 0.f ? ds * fmaf(-core, core, 1.f) : ds;      // (of a hidden key core may be NaN)
                 }
             }
 #pragma unroll

@@ -11,7 +11,8 @@
 // less than 2^-kSpread of the tile's carries a power of its own, and the tile says so (mixed). Weighted sums over tiles (of values by scores' weights, of dO by columns'
 // weights) are kept at one power of two where all tiles of a walk have about the same and none is mixed, and where not, at one for each row or
 // column, which follows the largest of the terms that the row sees (ColumnScale). So no magnitude is out of reach, and a result's error is in proportion to the largest
-// magnitude among the channels of the tokens that it is made of, not to anything else. Infinities and NaN become NaN.
+// magnitude among the channels of the tokens that it is made of, not to anything else. A token that holds an infinity or NaN is laid out as zeros (0 times it would not
+// be 0) and says so in place of its power of two (kBad); scores of those that see it become NaN.
 //
 // attn_make_parts lays tiles out once, as the matrix instructions want them: blocks of 1 KB, [16 tokens][32 channels][part], lane (m, g) with its eight
 // values behind each other (channels 8g .. 8g+7 of token m), so a wave reads an operand with tokens in lanes as one linear kilobyte, and copies of tiles into LDS
@@ -67,6 +68,7 @@ __device__ __forceinline__ int parts_exponent(float most)
     return max(e, -100);
 }
 __device__ __forceinline__ float finite_magnitude(float x) { return fabsf(x) < kInf ? fabsf(x) : 0.f; }
+__device__ __forceinline__ float any_magnitude(float x) { return fabsf(x) < kInf ? fabsf(x) : kInf; }     // (NaN, too)
 
 // A workgroup's tile of rows, of which (image, head), and its split of the keys. Causal rows have ever more keys, so there the longest tiles come first; where the device's eight
 // parts get whole heads, those of one head stay in one. Of the 32 workgroups that meet the 32 compute units of a part in turn, every other set comes in
@@ -88,7 +90,7 @@ __device__ __forceinline__ RowTile row_tile_of(const AttnArgs &a, unsigned group
 }
 
 // What a tile's tokens carry, in a word: the power of two (kNone: nothing but zeros), and whether tokens have some of their own.
-constexpr int kNone = -1000;
+constexpr int kNone = -1000, kBad = 10000;
 __device__ __forceinline__ int tile_exponent(int word) { return word >> 1; }
 __device__ __forceinline__ bool tile_mixed(int word) { return word & 1; }
 
@@ -182,6 +184,20 @@ __device__ __forceinline__ void by_token(floatx4 (&y)[NB], const int *each, int 
         y[b].y = ldexpf(y[b].y, e.y + more);
         y[b].z = ldexpf(y[b].z, e.z + more);
         y[b].w = ldexpf(y[b].w, e.w + more);
+    }
+}
+
+// Scores behind their masks, minus infinity where the token is hidden: NaN where it is not and is bad.
+template <int NB>
+__device__ __forceinline__ void bad_tokens(floatx4 (&s)[NB], const int *each)
+{
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int4 e = *reinterpret_cast<const int4 *>(each + 16 * b);
+        s[b].x = (e.x == kBad) & (s[b].x != -kInf) ? __builtin_nanf("") : s[b].x;
+        s[b].y = (e.y == kBad) & (s[b].y != -kInf) ? __builtin_nanf("") : s[b].y;
+        s[b].z = (e.z == kBad) & (s[b].z != -kInf) ? __builtin_nanf("") : s[b].z;
+        s[b].w = (e.w == kBad) & (s[b].w != -kInf) ? __builtin_nanf("") : s[b].w;
     }
 }
 

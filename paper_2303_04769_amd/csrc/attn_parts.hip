@@ -43,7 +43,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
             x[p][i] = floatx4{0.f, 0.f, 0.f, 0.f};
             if (on) x[p][i] = load_quad<VEC>(a, t.s, token_at(t.p, t.s, n, j), head * a.D, dq * 4);
 #pragma unroll
-            for (int d = 0; d < 4; ++d) most[i] = fmaxf(most[i], finite_magnitude(x[p][i][d]));
+            for (int d = 0; d < 4; ++d) most[i] = fmaxf(most[i], any_magnitude(x[p][i][d]));
         }
     }
 #pragma unroll
@@ -59,7 +59,9 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
 #pragma unroll
         for (int i = 0; i < 4; ++i) most[i] = fmaxf(most[i], y[i]);
     }
-    float all = fmaxf(fmaxf(most.x, most.y), fmaxf(most.z, most.w));
+    float all = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all = fmaxf(all, finite_magnitude(most[i]));
     all = fmaxf(all, lane_shift1<0x124>(all));                         // row_ror
     all = fmaxf(all, lane_shift1<0x128>(all));
     all = column_max(all);
@@ -70,7 +72,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int y = parts_exponent(most[i]);
-        own[i] = most[i] == 0.f || y >= ex - kSpread ? ex : y;
+        own[i] = most[i] == kInf ? kBad : most[i] == 0.f || y >= ex - kSpread ? ex : y;
         mixed |= own[i] != ex;
     }
     mixed = __any(mixed);
@@ -85,7 +87,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
-                const float y = ldexpf(x[p][i][d], -own[i]);
+                const float y = own[i] == kBad ? 0.f : ldexpf(x[p][i][d], -own[i]);
                 hi[i][d] = (_Float16)y;
                 lo[i][d] = (_Float16)(y - (float)hi[i][d]);
             }
@@ -230,6 +232,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
             const int lift = !EVEN ? 0 : v_now < v_exp ? kLift - 1 : kLift;
             const float in_exponent = (float)lift, was = top.at;
             finish_scores<MODE>(a, s, row, dot_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
+            if (!EVEN && tile_mixed(k_word)) bad_tokens(s, a.k_each + first_tile * 64 + j0 + 4 * g);
+            if (!EVEN && tile_mixed(v_word)) bad_tokens(s, a.v_each + first_tile * 64 + j0 + 4 * g);
             raise_top(s, top, sum, o, in_exponent);
             if (!EVEN) vs.follow(top.at - was, o);
             floatx4 part = {};
@@ -254,7 +258,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn
             for (int b = 0; b < 2; ++b) products_across<STEPS>(o, vt, b, p_hi[b], p_lo[b]);
         }
     };
-    if (even) walk(std::true_type{});
+    // (uneven tiles are rare, and their walk must not cost this one registers: it is the one that spills)
+    if (__builtin_expect(even, 1)) walk(std::true_type{});
     else walk(std::false_type{});
 
     const AttnArgs z = late_args();

@@ -150,7 +150,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     // a row that saw nothing has no gradient, and neither has one past the end: weights exp2(-inf)
     const float lse = a.lse_in[at_row];
     const bool dead = lse == -kInf || i_raw >= a.Sq;
-    const float lse2 = dead ? kInf : lse * kLog2e;
+    float lse2 = dead ? kInf : lse * kLog2e;
     float delta = 0.f;
     {
         const float *td = token_at(a.dout, a.dos, n, i), *to = token_at(a.o, a.os, n, i);
@@ -237,7 +237,14 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     // (where tiles are mixed: tokens with powers of two of their own)
     const auto walk = [&](auto is_mixed) {
         constexpr bool MIXED = decltype(is_mixed)::value;
-        const int q_exp = MIXED ? a.q_each[at_tile * 64 + wave * 16 + m] : tile_exponent(q_word), d_exp = MIXED ? a.do_each[at_tile * 64 + wave * 16 + m] : tile_exponent(d_word);
+        int q_exp = tile_exponent(q_word), d_exp = tile_exponent(d_word);
+        if (MIXED) {
+            q_exp = a.q_each[at_tile * 64 + wave * 16 + m];
+            d_exp = a.do_each[at_tile * 64 + wave * 16 + m];
+            if ((q_exp == kBad) | (d_exp == kBad)) lse2 = __builtin_nanf("");       // (in every score that is not hidden)
+            q_exp = q_exp == kBad ? 0 : q_exp;
+            d_exp = d_exp == kBad ? 0 : d_exp;
+        }
         for (int j0 = begin; j0 < end; j0 += 64) {
             const int k_word = exponents_at(k_exps, j0 / 64), v_word = exponents_at(v_exps, j0 / 64);
             int dot_exp = q_exp + tile_exponent(k_word), dp_exp = d_exp + tile_exponent(v_word);
@@ -267,6 +274,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             const float dp_in = ldexpf(1.f, dp_exp);
             floatx4 core[4];
             finish_scores<MODE>(a, s, row, dot_exp, lse2, j0, key_code, key_doc, g, bias, far_lo, far_hi, (MODE & 1) ? core : nullptr);
+            if (MIXED && tile_mixed(k_word)) bad_tokens(s, a.k_each + first_tile * 64 + j0 + 4 * g);      // (of V: delta is NaN)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -422,7 +430,15 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
     floatx4 dk[DT] = {}, dv[DT] = {};
     const auto walk = [&](auto is_even) {
         constexpr bool EVEN = decltype(is_even)::value;
-        const int k_exp = EVEN ? tile_exponent(k_word) : a.k_each[at_tile * 64 + wave * 16 + m], v_exp = EVEN ? tile_exponent(v_word) : a.v_each[at_tile * 64 + wave * 16 + m];
+        int k_exp = tile_exponent(k_word), v_exp = tile_exponent(v_word);
+        bool k_bad = false;
+        if (!EVEN) {
+            k_exp = a.k_each[at_tile * 64 + wave * 16 + m];
+            v_exp = a.v_each[at_tile * 64 + wave * 16 + m];
+            k_bad = k_exp == kBad;
+            k_exp = k_bad ? 0 : k_exp;
+            v_exp = v_exp == kBad ? 0 : v_exp;                              // (delta is NaN in the rows that see it)
+        }
         for (int head = h0; head < h1 && begin < end; ++head) {
             const float slope = (MODE & 2) && a.slopes ? a.slopes[head] * kLog2e : 0.f;
             const float *bias = nullptr;
@@ -513,6 +529,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
                     near = !all_lo && !all_hi;
                     base = all_lo ? far_lo : all_hi ? far_hi : 0.f;
                 }
+                if (!EVEN && k_bad) base = __builtin_nanf("");
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const floatx4 l4 = *reinterpret_cast<const floatx4 *>(rows.lse + 16 * b + 4 * g);
@@ -575,6 +592,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
                         s[b].w = x.w == doc ? s[b].w : -kInf;
                     }
                 }
+                if (!EVEN && tile_mixed(q_word)) bad_tokens(s, a.q_each + first_tile * 64 + i0 + 4 * g);
+                if (!EVEN && tile_mixed(d_word)) bad_tokens(s, a.do_each + first_tile * 64 + i0 + 4 * g);
                 const float lift = EVEN ? ldexpf(1.f, max(0, 14 + d_exp - d_most)) : 1.f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
@@ -609,7 +628,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
             }
         }
     };
-    if (even) walk(std::true_type{});
+    if (__builtin_expect(even, 1)) walk(std::true_type{});
     else walk(std::false_type{});
     const AttnArgs z = late_args();
     if (j_raw >= z.Sk) return;
@@ -685,12 +704,15 @@ hipError_t launch_attn_grad_rows_parts(const AttnArgs &a, hipStream_t s)
     const unsigned grid = (unsigned)((long)a.N * a.heads * a.row_tiles);
     const size_t size = 2 * (size_t)a.reach + 1;
     const size_t more = ((a.bias_lds ? size : 0) + (a.part_bias ? a.bias_copies * (size + 1) : 0)) * sizeof(float);
+    // (a cap and a table without distances have a form of their own: the walk over mixed tiles beside the other one leaves registers for no more. 2048 frames
+    // with a prefix, 4 sequences, 190 us by the form for everything, 178 by this one)
     const int mode = attn_mode(a);
 #define ROWS(st) \
     if (a.D <= 32 * st) { \
         const size_t lds = 3 * parts_tile_bytes(st) + more; \
         return mode == 0 ? launch_lds(attn_grad_rows_parts<st, 0>, grid, lds, a, s) \
-             : mode == 4 ? launch_lds(attn_grad_rows_parts<st, 4>, grid, lds, a, s) : launch_lds(attn_grad_rows_parts<st, 7>, grid, lds, a, s); \
+             : mode == 4 ? launch_lds(attn_grad_rows_parts<st, 4>, grid, lds, a, s) \
+             : mode == 5 ? launch_lds(attn_grad_rows_parts<st, 5>, grid, lds, a, s) : launch_lds(attn_grad_rows_parts<st, 7>, grid, lds, a, s); \
     }
     ROWS(1) ROWS(2) ROWS(3) ROWS(4)
 #undef ROWS

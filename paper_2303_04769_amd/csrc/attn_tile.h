@@ -359,6 +359,24 @@ struct Tile {
             if (kAll % 256 == 0 || e < kAll) *reinterpret_cast<floatx4 *>(lds + c * kChunk + j * 16 + q * 4) = x[i];
         }
     }
+    // The same for what sums with weights are taken of, where 0 times a hidden token's infinity or NaN would not be 0: such values become zeros, and
+    // their tokens' words, and `any`, get the stamp.
+    static __device__ __forceinline__ void put_finite(float *lds, floatx4 (&x)[kQuads], int *bad, int *any, int stamp)
+    {
+#pragma unroll
+        for (int i = 0; i < kQuads; ++i) {
+            const int e = threadIdx.x + i * 256, j = (e >> 2) % KT;
+            bool off = false;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                const bool here = !(fabsf(x[i][d]) < kInf);
+                x[i][d] = here ? 0.f : x[i][d];
+                off |= here;
+            }
+            if (off && (kAll % 256 == 0 || e < kAll)) { bad[j] = stamp; *any = stamp; }
+        }
+        put(lds, x);
+    }
     // Left operand with tokens in lanes: channels 16c + 4g .. +3 of token 16b + m.
     static __device__ __forceinline__ floatx4 tokens(const float *lds, int b, int c, int m, int g)
     {

@@ -67,7 +67,13 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
  * in 0 .. buckets - 1 (values outside are taken into that range); table: [heads][buckets]; a bias below -1e30, so also one of the
  * type's lowest value, hides its offsets as minus infinity does.
  * A row that sees no key, or only keys of score -inf, gives out = 0 and lse = -inf. Keys at and beyond an image's length may hold
- * anything (NaN among it), and neither does what a key hidden by another mask holds reach a row that does not see it.
+ * anything (NaN among it), and neither does what a key hidden by another mask holds, however large, infinite or NaN, reach a row that does not see it. So it is
+ * in the gradients: dq of rows that do not see such a key, dk and dv of keys that no row sees which is such itself or sees one. Gradients of those that do are not finite.
+ *
+ * Precision. Larger calls hold values as two fp16 numbers at a power of two of their token's largest channel: 22 bits of values down to 2^-12 of that, one less for every
+ * halving below; their products are summed in fp32. So results are as near to 64 bits as those of fp32 products (which round every addition)
+ * where the channels of a token are of like size, and a channel 2^-35 of its neighbours is lost. The gradients take their weights from lse, and so have the error of lse's
+ * rounding, 2^-24 of its size (with slopes, which make lse large, weights are scaled to sum to one).
  *
  * All of lengths, first, prefix, docs, slopes, table and bucket are DEVICE pointers. Limits: D <= 256; Sq, Sk <= 2^28, first positions are
  * taken into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31. Tensors may be larger than 2^31 values.

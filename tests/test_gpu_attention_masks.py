@@ -208,6 +208,58 @@ def test_large_values_in_hidden_places_of_long_caches(Sq, Sk):
         compare(c, {"out": plain(got[0]), "lse": got[1]}, exact(c), where)
 
 
+@pytest.mark.parametrize("shape", SHAPES)
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+def test_nan_and_infinities_in_hidden_places(shape, value):
+    """Tokens and rows that hold NaN or infinities: results and gradients of rows that do not see such a token are what they are without it, and so are the gradients of
+    keys that no such row sees; those that do see it are not finite."""
+    S = SHAPES[shape]["Sq"]
+    at = S // 3 + 12                                             # the second document's; rows of the first do not see it, nor does that row see its keys
+    for mask in (causal, documents):
+        ref = exact(Case(**SHAPES[shape], **mask(S)))
+        for name in ("k", "v", "q", "dout"):
+            c = Case(**SHAPES[shape], **mask(S))
+            getattr(c, name)[0, 3, at] = value
+            got = everything(c)
+            got.pop("dtable", None)
+            keys = name in "kv"
+            rows_ok, keys_ok = (torch.zeros(S, dtype=torch.bool) for _ in range(2))
+            if mask is causal:
+                rows_ok[:at if keys else S] = True
+                if not keys:
+                    rows_ok[at] = False
+                keys_ok[at + 1:] = not keys                      # (keys up to `at` are seen by a row that sees it, or by the row that holds it)
+            else:
+                keys_ok[:S // 3 + 5] = True
+                rows_ok[:S // 3 + 5 if keys else S] = True
+                if not keys:
+                    rows_ok[at] = False
+            forward = rows_ok if name != "dout" else torch.ones_like(rows_ok)
+            where = {"out": forward, "lse": forward, "dq": rows_ok, "dk": keys_ok, "dv": keys_ok}
+            try:
+                compare(c, got, ref, where)
+            except AssertionError as e:
+                raise AssertionError(f"{name}, {mask.__name__}: {e}") from None
+            if name != "v":
+                assert not bool(torch.isfinite(got["dk"][0, :c.D, at if keys else at - 1]).any()), name
+            if name in "kv":
+                assert not bool(torch.isfinite(got["dq"][0, :c.D, at + 1]).any()), name
+            if name == "dout":
+                assert not bool(torch.isfinite(got["dv"][0, 3, at - 1])), name
+
+
+@pytest.mark.parametrize("shape", SHAPES)
+def test_what_stands_past_lengths_reaches_no_gradient(shape):
+    S = SHAPES[shape]["Sq"]
+    for length in (S - 7, S // 2, 1):
+        c = Case(**SHAPES[shape], lengths=[length])
+        ref = exact(c)
+        c.k[0, :, length:], c.v[0, :, length:] = float("nan"), float("inf")
+        got = everything(c)
+        compare(c, got, ref)
+        assert bool((got["dk"][:, :, length:] == 0).all()) and bool((got["dv"][:, :, length:] == 0).all())
+
+
 # ---------------------------------------------------------------------------------------------------- biases
 
 def with_offsets(c, reach, buckets=None):
