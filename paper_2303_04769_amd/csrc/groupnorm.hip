@@ -31,12 +31,13 @@ struct NormArgs {
 };
 
 // z / (1 + exp(-z)) and the logistic function itself. exp(-z) as a power of two whose exponent keeps the bits that the product
-// with log2(e) rounds away, so that it is as exact for large |z| as for small ones.
+// with log2(e) rounds away, so that it is as exact for large |z| as for small ones. Past 2^126 and below 2^-126 there is nothing to keep, and where the product
+// overflows nothing to keep it from (infinity less infinity).
 __device__ __forceinline__ float logistic(float z)
 {
     const float t = z * -1.44269504f, lo = fmaf(z, -1.44269504f, -t) + z * -1.92596303e-8f;
     const float e = __builtin_amdgcn_exp2f(t);
-    return __builtin_amdgcn_rcpf(1.f + (t < 126.f ? fmaf(e, lo * 0.693147181f, e) : e));
+    return __builtin_amdgcn_rcpf(1.f + (fabsf(t) < 126.f ? fmaf(e, lo * 0.693147181f, e) : e));
 }
 __device__ __forceinline__ float act_of(float z, int act)
 {
