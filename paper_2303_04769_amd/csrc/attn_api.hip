@@ -392,7 +392,10 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     x.bias_copies = 16;
     while (x.bias_copies > 4 && grad_lds(*a, x.bias_copies) > (a->D <= 64 ? 53000 : 79000)) x.bias_copies /= 2;
     const hipStream_t s = (hipStream_t)stream;
-    hipError_t e;
+    hipError_t e = hipSuccess;
+    x.share_known = a->slopes && dtable;
+    if (x.share_known) e = launch_attn_grad_shares(x, x.vec, s);
+    if (e != hipSuccess) return from_hip(e);
     if (p.parts) {
         PartsArgs args{};
         args.count = 4;

@@ -19,6 +19,82 @@ extern __shared__ __attribute__((aligned(16))) float grad_lds[];
 __device__ __forceinline__ float score_core(const AttnArgs &a, const Scorer &sc, float dot) { return a.cap > 0.f ? tanh_of(dot * sc.cap_in) : dot; }
 __device__ __forceinline__ float score_of(const AttnArgs &a, const Scorer &sc, float core) { return core * (a.cap > 0.f ? sc.cap2 : sc.scale2); }
 
+// What each row's weights are to be multiplied by (share_of), on its own: dq takes that at the end of its walk over the keys, when their sum is known, but the bias's gradient sums
+// over rows all along. So with distances and a table's gradient this runs first: scores only, one product of seven (2048 frames with a prefix,
+// capped, 8 heads of 64 on 2, 4 sequences: 190 us of some 650 with the forward call; 400 frames, 2 sequences: 21).
+template <int DT, int KT, bool VEC>
+__global__ void __launch_bounds__(256, 2) attn_grad_shares(AttnArgs a)
+{
+    constexpr int NB = KT / 16;
+    using T = Tile<DT, KT>;
+    __shared__ float kt[T::kFloats];
+    __shared__ alignas(16) int key_code[KT];
+    __shared__ alignas(16) int key_doc[KT + 1];
+    __shared__ int words[2];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int by_tile = a.by_tiles.div((int)id), tile = a.row_tiles - 1 - ((int)id - by_tile * a.row_tiles);
+    const int n = a.by_heads.div(by_tile), head = by_tile - n * a.heads, key_head = a.by_group.div(head);
+    const int row0 = tile * 64, i_raw = row0 + wave * 16 + m, i = min(i_raw, a.Sq - 1);
+    const ImageMask im(a, n);
+    const RowState row(a, im, n, i, head);
+    const float lse = a.lse_in[((size_t)n * a.heads + head) * a.Sq + i];
+    const float lse2 = lse == -kInf ? kInf : lse * kLog2e;
+    float q[DT * 4];
+    {
+        const float *token = token_at(a.q, a.qs, n, i);
+#pragma unroll
+        for (int c = 0; c < DT; ++c) {
+            const floatx4 x = load_quad<VEC>(a, a.qs, token, head * a.D, 16 * c + 4 * g);
+            q[4 * c] = x.x; q[4 * c + 1] = x.y; q[4 * c + 2] = x.z; q[4 * c + 3] = x.w;
+        }
+    }
+    int lo = 0, hi = im.len;
+    if (a.causal) hi = max(0, min(hi, max(im.position(min(row0 + 63, a.Sq - 1)) + 1, im.prefix)));
+    if (a.docs) {
+        if (threadIdx.x == 0) { words[0] = 0x7fffffff; words[1] = -1; }
+        __syncthreads();
+        if (row.doc >= 0) { atomicMin(&words[0], row.doc); atomicMax(&words[1], row.doc); }
+        __syncthreads();
+        const int d0 = words[0], d1 = words[1];
+        __syncthreads();
+        document_hull(a.docs + (size_t)n * a.Sk, 0, hi, d0, d1, words, &lo, &hi);
+    }
+    const float *bias = nullptr;
+    if (a.bias_lds) {
+        expand_bias(a, head, grad_lds);
+        bias = grad_lds;
+    }
+    const float far_lo = bias_gather(a, head, 0), far_hi = bias_gather(a, head, 2 * a.reach);
+    floatx4 kx[T::kQuads];
+    const auto fetch = [&](int j0) { T::template fetch<VEC>(kx, a, a.ks, a.k, n, key_head * a.D, j0, [&](int j) { return j0 + j < im.len; }); };
+    if (lo < hi) fetch(lo);
+    float total = 0.f;
+    for (int j0 = lo; j0 < hi; j0 += KT) {
+        __syncthreads();
+        T::put(kt, kx);
+        stage_keys<KT>(a, n, j0, key_code, key_doc);
+        __syncthreads();
+        if (j0 + KT < hi) fetch(j0 + KT);
+        floatx4 s[NB] = {};
+#pragma unroll
+        for (int c = 0; c < DT; ++c)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const floatx4 x = T::tokens(kt, b, c, m, g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[b] = mfma(x[e], q[4 * c + e], s[b]);
+            }
+        finish_scores<7>(a, s, row, 0, lse2, j0, key_code, key_doc, g, bias, far_lo, far_hi);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) total += __builtin_amdgcn_exp2f(s[b][e]);
+    }
+    const float share = share_of(a, total);
+    if (i_raw < a.Sq && g == 0) a.share[((size_t)n * a.heads + head) * a.Sq + i] = share;
+}
+
 template <int DT, int KT, bool VEC>
 __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs a)
 {
@@ -98,6 +174,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
         for (int x = threadIdx.x; x < size; x += 256) acc[x] = 0.f;       // (behind the next barrier a place is one thread's until the loop's end)
     }
     float sum_lo = 0.f, sum_hi = 0.f, total = 0.f;
+    const float known = a.share_known ? a.share[at_row] : 1.f;
 
     const Scorer sc(a);
     floatx4 dq[DT] = {};
@@ -160,7 +237,7 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
                 }
                 if (bad) t = key_bad[16 * b + 4 * g + e] == j0 ? __builtin_nanf("") : t;
                 const float p = __builtin_amdgcn_exp2f(t);
-                float ds = p * (dp[b][e] - delta);
+                float ds = p * (dp[b][e] - delta) * known;
                 const bool seen = !edge | row.sees(j, docs[e], true);
                 ds = seen ? ds : 0.f;
                 total += seen ? p : 0.f;
@@ -214,9 +291,9 @@ __global__ void __launch_bounds__(256, DT <= 6 ? 2 : 1) attn_grad_rows(AttnArgs 
             part[x] = y;
         }
     }
-    const float share = share_of(a, total);
+    const float share = a.share_known ? 1.f : share_of(a, total);
     if (i_raw < a.Sq) {
-        if (a.slopes && g == 0) a.share[((size_t)n * a.heads + head) * a.Sq + i] = share;
+        if (a.slopes && !a.share_known && g == 0) a.share[((size_t)n * a.heads + head) * a.Sq + i] = share;
         float *token = const_cast<float *>(token_at(a.dq, a.dqs, n, i));
 #pragma unroll
         for (int grp = 0; grp < GR; ++grp)
@@ -465,6 +542,19 @@ int attn_grad_tile(int D)
     GRAD_FORMS(FORM)
 #undef FORM
     return 0;
+}
+
+hipError_t launch_attn_grad_shares(const AttnArgs &a, bool vec, hipStream_t s)
+{
+    const unsigned grid = (unsigned)((long)a.N * a.heads * a.row_tiles);
+    const size_t lds = a.bias_lds ? (2 * (size_t)a.reach + 1) * sizeof(float) : 0;
+#define FORM(dt, kt) \
+    if (a.D <= 16 * dt) { \
+        return vec ? launch_lds(attn_grad_shares<dt, kt, true>, grid, lds, a, s) : launch_lds(attn_grad_shares<dt, kt, false>, grid, lds, a, s); \
+    }
+    GRAD_FORMS(FORM)
+#undef FORM
+    return hipErrorInvalidValue;
 }
 
 hipError_t launch_attn_grad_rows(const AttnArgs &a, bool vec, hipStream_t s)

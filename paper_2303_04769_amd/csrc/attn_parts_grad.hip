@@ -231,6 +231,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     if (sums)
         for (int x = threadIdx.x; x < a.bias_copies * stride; x += 256) acc[x] = 0.f;
     float sum_lo = 0.f, sum_hi = 0.f, total = 0.f;
+    const float known = (MODE & 2) && a.share_known ? a.share[at_row] : 1.f;
 
     ColumnScale cs;
     floatx4 dq[DT] = {};
@@ -283,6 +284,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
                     if (MODE & 2) total += p;
                     s[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -delta);
                 }
+            if ((MODE & 2) && a.share_known)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) s[b] *= known;
             if (sums) {
                 const bool all_lo = __all(key_code[63] - row.code <= -a.reach), all_hi = __all(key_code[0] - row.code >= a.reach);
                 if (all_lo || all_hi) {
@@ -339,9 +343,9 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             part[x] = y;
         }
     }
-    const float share = (MODE & 2) ? share_of(z, total) : 1.f;
+    const float share = (MODE & 2) && !z.share_known ? share_of(z, total) : 1.f;
     if (i_raw < z.Sq) {
-        if ((MODE & 2) && z.slopes && g == 0) z.share[at_row] = share;
+        if ((MODE & 2) && z.slopes && !z.share_known && g == 0) z.share[at_row] = share;
         const float back = cs.back(z.scale) * share;
         float *token = const_cast<float *>(token_at(z.dq, z.dqs, n, i));
 #pragma unroll

@@ -41,6 +41,7 @@ struct AttnArgs {
     // gradient
     const float *dout, *lse_in;
     float *share;                                            // [N * heads][Sq]: what a row's weights, taken from its lse, are to be multiplied by (with slopes)
+    int share_known;                                         // by attn_grad_shares, before the rows' gradient
     float *dq, *dk, *dv, *delta, *part_bias;                 // part_bias: null, or [N * heads * row_tiles][2 reach + 1]
     TokenStrides dos, dqs, dks, dvs;
     int key_tiles, bias_acc_lds, bias_copies, row_parts;
@@ -505,6 +506,7 @@ hipError_t launch_lds(K *kernel, unsigned grid, size_t lds, const AttnArgs &a, h
 inline int attn_mode(const AttnArgs &a) { return (a.cap > 0.f ? 1 : 0) | (a.slopes ? 2 : 0) | (a.table ? 4 : 0); }
 hipError_t launch_attn_rows(const AttnArgs &a, bool vec, size_t bias_bytes, hipStream_t s);
 hipError_t launch_attn_join(const AttnArgs &a, hipStream_t s);
+hipError_t launch_attn_grad_shares(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_rows(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_keys(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_bias(const AttnArgs &a, float *sums, float *dtable, hipStream_t s);

@@ -284,3 +284,14 @@ def test_wide_tables_of_wide_heads(D, reach):
 def test_pixels_of_wide_heads(side):
     c = Case(Sq=side * side, heads=1, D=128, bias=(side, side))
     compare(c, everything(c), exact(c))
+
+
+@pytest.mark.parametrize("D", [16, 48, 160])
+def test_table_gradient_of_rows_far_behind_the_keys_they_see(D):
+    """As test_rows_far_behind_the_keys_they_see (whose bound this is), the table's gradient beside distances: a bucket for every offset, so that what rounding
+    leaves of a row's lse does not cancel within one."""
+    S = 400
+    c = with_offsets(Case(N=2, Sq=S, heads=2, D=D, lengths=[2, 7], slopes=True), S - 1)
+    want = exact(c)["dtable"][0]
+    off = gradients(c)[5].double().cpu() - want
+    assert float(off.norm()) <= 2e-6 * float(want.norm())
