@@ -131,7 +131,7 @@ struct PartsTensor {
     TokenStrides s;
     int heads, tokens, tiles, rows;            // rows: not keys but queries (their masks: rows of lse = -inf are left out)
     char *image;
-    int *exps, *each;                          // [N * heads][tiles], [N * heads][tiles][64]
+    int *exps, *each;                          // [N * heads][tiles], [N * heads][tiles][64] (written for mixed tiles)
     unsigned first_block;
 };
 struct PartsArgs {

@@ -76,7 +76,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
         mixed |= own[i] != ex;
     }
     mixed = __any(mixed);
-    if (threadIdx.x < 64 && (threadIdx.x & 3) == 0) *reinterpret_cast<int4 *>(t.each + (size_t)id * 64 + tq * 4) = int4{own[0], own[1], own[2], own[3]};
+    if (mixed && threadIdx.x < 64 && (threadIdx.x & 3) == 0) *reinterpret_cast<int4 *>(t.each + (size_t)id * 64 + tq * 4) = int4{own[0], own[1], own[2], own[3]};
     if (threadIdx.x == 0) t.exps[id] = (all == 0.f ? kNone : ex) * 2 + mixed;
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
@@ -102,7 +102,8 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
 }
 
 template <int STEPS, int MODE>
-__global__ void __launch_bounds__(256, STEPS <= 2 ? 4 : STEPS == 3 ? 3 : 2) attn_rows_parts(AttnArgs a)
+// (waves a SIMD: what the walk over even tiles has registers for)
+__global__ void __launch_bounds__(256, STEPS == 1 && MODE <= 2 ? 5 : STEPS <= 2 ? 4 : STEPS == 3 || MODE <= 4 ? 3 : 2) attn_rows_parts(AttnArgs a)
 {
     constexpr int DT = 2 * STEPS, IMAGE = (int)parts_tile_bytes(STEPS);
     __shared__ alignas(16) int key_code[64];

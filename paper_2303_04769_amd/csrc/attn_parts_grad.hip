@@ -240,8 +240,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
         constexpr bool MIXED = decltype(is_mixed)::value;
         int q_exp = tile_exponent(q_word), d_exp = tile_exponent(d_word);
         if (MIXED) {
-            q_exp = a.q_each[at_tile * 64 + wave * 16 + m];
-            d_exp = a.do_each[at_tile * 64 + wave * 16 + m];
+            if (tile_mixed(q_word)) q_exp = a.q_each[at_tile * 64 + wave * 16 + m];
+            if (tile_mixed(d_word)) d_exp = a.do_each[at_tile * 64 + wave * 16 + m];
             if ((q_exp == kBad) | (d_exp == kBad)) lse2 = __builtin_nanf("");       // (in every score that is not hidden)
             q_exp = q_exp == kBad ? 0 : q_exp;
             d_exp = d_exp == kBad ? 0 : d_exp;
@@ -357,7 +357,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
 }
 
 template <int STEPS, int MODE>
-__global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(AttnArgs a)
+// (waves a SIMD: what the walk over even tiles has registers for)
+__global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 3 && MODE == 0) ? 3 : 2) attn_grad_keys_parts(AttnArgs a)
 {
     constexpr int DT = 2 * STEPS, IMAGE = (int)parts_tile_bytes(STEPS), HALF = IMAGE / 2;
     struct Rows {
@@ -437,8 +438,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_keys_parts(
         int k_exp = tile_exponent(k_word), v_exp = tile_exponent(v_word);
         bool k_bad = false;
         if (!EVEN) {
-            k_exp = a.k_each[at_tile * 64 + wave * 16 + m];
-            v_exp = a.v_each[at_tile * 64 + wave * 16 + m];
+            if (tile_mixed(k_word)) k_exp = a.k_each[at_tile * 64 + wave * 16 + m];
+            if (tile_mixed(v_word)) v_exp = a.v_each[at_tile * 64 + wave * 16 + m];
             k_bad = k_exp == kBad;
             k_exp = k_bad ? 0 : k_exp;
             v_exp = v_exp == kBad ? 0 : v_exp;                              // (delta is NaN in the rows that see it)
