@@ -341,7 +341,7 @@ def test_attention_and_its_gradient(name):
     Case(**CASES[name]).check()
 
 
-# Sizes that are computed with values in two parts (10^8 multiply-adds a product and more).
+# Larger sizes: all gradients but one (a table too large for LDS) and most forward calls are computed with values in two parts (which, test_gpu_attention_forms.py says).
 LARGE = {
     "plain": dict(Sq=640, heads=4, D=64), "odd": dict(Sq=651, heads=4, D=64, Cb=8), "rows and keys of unlike number": dict(Sq=130, Sk=3100, heads=4, D=64),
     "causal, shared": dict(Sq=660, heads=8, kv=2, D=32, causal=True), "causal, distances": dict(Sq=700, heads=4, D=64, causal=True, slopes=True),
