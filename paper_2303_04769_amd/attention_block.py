@@ -85,6 +85,9 @@ class ImageBlock:
         return din, dgamma, dbeta, dtable
 
 
+KEPT_PLANS = 4
+
+
 class FrameBlock:
     """The block over sequences of up to `room` frames, channels last: [N][S][Cc]. Each frame is normalized by itself and sees itself and
     the frames before it. gamma, beta: [Cc]; table, bucket: a bias over distances (log_buckets). To the convolutions the frames are images
@@ -102,17 +105,22 @@ class FrameBlock:
         self.length, self._plans = 0, {}
 
     def _plan(self, S, Sk):
-        """What calls of S new frames on Sk in all need (for a single frame: on the whole cache, up to lengths)."""
-        if (S, Sk) not in self._plans:
+        """What calls of S new frames on Sk in all need (for a single frame: on the whole cache, up to lengths). The last few are kept: a sequence in pieces comes to
+        ever new sizes."""
+        plan = self._plans.pop((S, Sk), None)
+        if plan is None:
             dev, tokens = self.cache.device, self.N * S
-            self._plans[S, Sk] = (
+            plan = (
                 A.GroupNorm(tokens, self.C, 1, 1, self.G, act="silu", Cb=self.C, device=dev),
                 A.Attention(self.N, S, Sk, self.heads, self.kv_heads, self.D, Cb=self.D, cap=self.cap, causal=True, reach=self.bucket.numel() // 2,
                             buckets=self.table.shape[1], device=dev),
                 torch.empty(tokens, self.C, device=dev), torch.empty(tokens, self.Cq, device=dev), torch.empty(tokens, 2 * self.Ck, device=dev),
                 torch.empty(tokens, self.Cq, device=dev),
                 torch.empty(self.N, dtype=torch.int32, device=dev), torch.empty(self.N, dtype=torch.int32, device=dev))
-        return self._plans[S, Sk]
+            while len(self._plans) >= KEPT_PLANS:
+                del self._plans[next(iter(self._plans))]                   # (the one that was not used for longest)
+        self._plans[S, Sk] = plan
+        return plan
 
     def _heads(self, t, first, heads):
         """View of `heads` heads from channel `first` on of frames [N][S][channels], each head a block of its own."""
