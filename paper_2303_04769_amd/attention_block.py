@@ -27,6 +27,11 @@ def _packed(weight, Cib, Cob):
     return out
 
 
+def _shaped(t, shape):
+    if tuple(t.shape) != shape:
+        raise ValueError(f"expected a tensor {list(shape)}, got {list(t.shape)}")
+
+
 def _conv1x1(inp, filt, out, N, Ci, Co, H, W, Cib, Cob):
     B.small_conv2d(inp, filt, out, N, Ci, Co, H, W, 1, 1, 1, (0, 0, 0, 0), Cib, Cob)
 
@@ -65,6 +70,7 @@ class ImageBlock:
 
     def forward(self, inp, gamma, beta, table):
         """inp: [N][C/Cb][H*W][Cb]; table: [heads][buckets]. Returns the output; what grad needs stays in the block."""
+        _shaped(inp, (self.N, self.C // self.Cb, self.H * self.W, self.Cb))
         out = torch.empty_like(inp)
         self.norm.run(inp, gamma, beta, self.h, self.stats)
         self._conv(self.h, self.w_in, self.qkv)
@@ -75,6 +81,7 @@ class ImageBlock:
 
     def grad(self, inp, gamma, beta, table, dout):
         """Gradients (inp, gamma, beta, table) of the last forward call, which had the same arguments."""
+        _shaped(dout, (self.N, self.C // self.Cb, self.H * self.W, self.Cb))
         din, dgamma, dbeta, dtable = (torch.empty_like(t) for t in (inp, gamma, beta, table))
         self._conv(dout, self.w_out_t, self.dctx)
         self.attention.grad(*self._parts(self.qkv), self.ctx, self.lse, self.dctx, *self._parts(self.dqkv), dtable=dtable, table=table,
@@ -98,6 +105,8 @@ class FrameBlock:
         self.N, self.room, self.C, self.G = N, room, Cc, G
         self.heads, self.kv_heads, self.D, self.cap, self.Cb = heads, kv_heads, D, cap, Cb
         self.Cq, self.Ck = heads * D, kv_heads * D
+        _shaped(w_in, (self.Cq + 2 * self.Ck, Cc))
+        _shaped(w_out, (Cc, self.Cq))
         self.w_q, self.w_kv = _packed(w_in[:self.Cq], Cb, Cb), _packed(w_in[self.Cq:], Cb, Cb)
         self.w_out = _packed(w_out, Cb, Cb)
         self.gamma, self.beta, self.table, self.bucket = gamma, beta, table, bucket
@@ -130,6 +139,7 @@ class FrameBlock:
     def forward(self, frames):
         """The next frames [N][S][Cc] of every sequence: their outputs; their keys and values go into the cache."""
         S, start = frames.shape[1], self.length
+        _shaped(frames, (self.N, S, self.C))
         if start + S > self.room:
             raise ValueError(f"{start} frames and {S} more do not fit {self.room}")
         Sk = self.room if S == 1 else start + S                            # (one plan for every single frame)

@@ -83,10 +83,19 @@ def small_groupnorm_workspace(N, Cc, H, W, G, Cb):
     return n.value
 
 
+def _holds(*tensors):
+    """Each tensor that there is has as many values as are written behind it (sizes that the library refuses are its to refuse)."""
+    for t, values in zip(tensors[::2], tensors[1::2]):
+        if t is not None and values > 0 and t.numel() != values:
+            raise TypeError(f"expected {values} values, got {tuple(t.shape)}")
+
+
 def small_groupnorm(inp, gamma, beta, out, stats, N, Cc, H, W, G, eps, act, Cb, workspace, stream=None):
     rc = _fast().groupnorm(inp, gamma, beta, out, stats, N, Cc, H, W, G, eps, act, Cb, workspace, None) if stream is None else None
     if rc is not None:
         return B._check(rc, "small_groupnorm")
+    values = N * Cc * H * W
+    _holds(inp, values, gamma, Cc, beta, Cc, out, values, stats, 2 * N * G)
     ws, size = _bytes(workspace)
     B._check(load().small_groupnorm(B._ptr(inp), B._ptr(gamma), B._ptr(beta), B._ptr(out), B._ptr(stats), N, Cc, H, W, G, eps, act, Cb,
                                     ws, size, B._stream(stream)), "small_groupnorm")
@@ -96,6 +105,8 @@ def small_groupnorm_grad(inp, gamma, beta, stats, dout, din, dgamma, dbeta, N, C
     rc = _fast().groupnorm_grad(inp, gamma, beta, stats, dout, din, dgamma, dbeta, N, Cc, H, W, G, act, Cb, workspace, None) if stream is None else None
     if rc is not None:
         return B._check(rc, "small_groupnorm_grad")
+    values = N * Cc * H * W
+    _holds(inp, values, gamma, Cc, beta, Cc, stats, 2 * N * G, dout, values, din, values, dgamma, Cc, dbeta, Cc)
     ws, size = _bytes(workspace)
     B._check(load().small_groupnorm_grad(B._ptr(inp), B._ptr(gamma), B._ptr(beta), B._ptr(stats), B._ptr(dout), B._ptr(din),
                                          B._ptr(dgamma), B._ptr(dbeta), N, Cc, H, W, G, act, Cb, ws, size, B._stream(stream)),

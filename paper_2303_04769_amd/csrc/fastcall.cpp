@@ -157,6 +157,12 @@ struct Reader {
         }
         return static_cast<T *>(t.data_ptr());
     }
+    // Argument k, if there is one, has so many values (the binding says so where not; sizes that the library refuses are its to refuse).
+    void holds(int k, long long values)
+    {
+        if (!plain || error || a[k] == Py_None || values <= 0) return;
+        if (THPVariable_Unpack(a[k]).numel() != values) plain = false;
+    }
     void *bytes(int k, size_t *size)
     {
         *size = 0;
@@ -260,10 +266,12 @@ ENTRY(dense_u8, 11, const int N = r.i(3), Ci = r.i(4), Co = r.i(5), Cib = r.i(6)
 ENTRY(groupnorm, 15, const int N = r.i(5), C = r.i(6), H = r.i(7), W = r.i(8), G = r.i(9); const float eps = r.number32(10); const int act = r.i(11), Cb = r.i(12);
       size_t size; void *ws = r.bytes(13, &size);
       auto *x = r.f32(0); auto *ga = r.f32(1); auto *be = r.f32(2); auto *y = r.f32(3); auto *st = r.f32(4);
+      const long long all = (long long)N * C * H * W; r.holds(0, all); r.holds(1, C); r.holds(2, C); r.holds(3, all); r.holds(4, 2LL * N * G);
       return r.call([&](void *s) { return lib.small_groupnorm(x, ga, be, y, st, N, C, H, W, G, eps, act, Cb, ws, size, s); });)
 ENTRY(groupnorm_grad, 17, const int N = r.i(8), C = r.i(9), H = r.i(10), W = r.i(11), G = r.i(12), act = r.i(13), Cb = r.i(14);
       size_t size; void *ws = r.bytes(15, &size);
       auto *x = r.f32(0); auto *ga = r.f32(1); auto *be = r.f32(2); auto *st = r.f32(3); auto *dy = r.f32(4); auto *dx = r.f32(5); auto *dg = r.f32(6); auto *db = r.f32(7);
+      const long long all = (long long)N * C * H * W; r.holds(0, all); r.holds(1, C); r.holds(2, C); r.holds(3, 2LL * N * G); r.holds(4, all); r.holds(5, all); r.holds(6, C); r.holds(7, C);
       return r.call([&](void *s) { return lib.small_groupnorm_grad(x, ga, be, st, dy, dx, dg, db, N, C, H, W, G, act, Cb, ws, size, s); });)
 
 // (record, q, k, v, out, lse, workspace, lengths, first, prefix, docs, slopes, table, bucket, stream): of a plan

@@ -26,3 +26,39 @@ def test_a_sequence_in_many_pieces_keeps_few_plans():
         at += n
         assert len(block._plans) <= AB.KEPT_PLANS
     assert at == 60 and float((torch.cat(got, 1) - want).abs().max()) <= 2.2e-3 * (1 + float(want.abs().max()))
+
+
+def test_tensors_of_other_sizes_are_refused():
+    """Group normalization reads as many values as its plan says, the blocks as many images, frames and channels: a tensor that has others is refused before anything
+    is enqueued, by the extension's calls and by those with a stream."""
+    import paper_2303_04769_amd as S
+    plan = S.GroupNorm(2, 32, 4, 4, 4)
+    e = lambda *s: torch.zeros(*s, device="cuda")  # noqa: E731
+    x, c, st = e(2, 2, 16, 16), e(32), e(2, 4, 2)
+    for stream in (None, torch.cuda.current_stream()):
+        plan.run(x, c, c, e(2, 2, 16, 16), st, stream=stream)
+        plan.grad(x, c, c, st, x, e(2, 2, 16, 16), e(32), e(32), stream=stream)
+        for at in range(5):
+            args = [x, c, c, e(2, 2, 16, 16), st]
+            args[at] = args[at][:1].contiguous()
+            with pytest.raises(TypeError):
+                plan.run(*args, stream=stream)
+        for at in range(8):
+            args = [x, c, c, st, x, e(2, 2, 16, 16), e(32), e(32)]
+            args[at] = args[at][:1].contiguous()
+            with pytest.raises(TypeError):
+                plan.grad(*args, stream=stream)
+    block = frame_block(8)
+    for shape in ((1, 3, 32), (2, 3, 16), (3, 3, 32)):
+        with pytest.raises(ValueError):
+            block.forward(e(*shape))
+    with pytest.raises(ValueError):
+        AB.FrameBlock(e(48, 32), e(32, 32), c, c, e(2, 8), e(25).int(), 2, 8, 32, 4, 2, 1, 16)
+    with pytest.raises(ValueError):
+        AB.FrameBlock(e(64, 32), e(32, 48), c, c, e(2, 8), e(25).int(), 2, 8, 32, 4, 2, 1, 16)
+    image = AB.ImageBlock(e(64, 32), e(32, 32), 2, 32, 3, 4, 4, 2, 1, 16)
+    with pytest.raises(ValueError):
+        image.forward(e(1, 2, 12, 16), c, c, e(2, image.buckets))
+    out = image.forward(e(2, 2, 12, 16), c, c, e(2, image.buckets))
+    with pytest.raises(ValueError):
+        image.grad(e(2, 2, 12, 16), c, c, e(2, image.buckets), out[:1].contiguous())
