@@ -285,6 +285,18 @@ GradPlan plan_grad(const small_attn &a)
     p.bytes = end;
     return p;
 }
+// Whether every launch of a call is one: a grid has fewer than 2^32 threads. (Asked for before the first, so that a call is enqueued whole or not at all.)
+bool launches(double workgroups, double threads) { return workgroups * threads < 4294967296.0; }
+bool attn_launches(const small_attn &a, const AttnPlan &p)
+{
+    return p.token || (launches((double)a.N * p.head_sets * p.row_tiles * p.splits, 256) && (!p.parts || launches(2.0 * a.N * a.kv_heads * ((a.Sk + 63) / 64), 256)));
+}
+bool grad_launches(const small_attn &a, const GradPlan &p)
+{
+    const double keys = (double)a.N * a.kv_heads * p.key_tiles, rows = (double)a.N * a.heads * p.row_tiles;
+    const double sums = a.table ? (double)a.heads * ((2.0 * a.reach + 1) / 32 + 1) : 0, buckets = a.table ? (double)a.heads * (a.buckets / 32.0 + 1) : 0;
+    return launches(2 * (keys + rows), 256) && launches(sums, 1024) && launches(buckets, 1024);
+}
 bool grad_vec(const small_attn &a)
 {
     size_t bits = 0;
@@ -311,7 +323,10 @@ int small_attention_workspace(const small_attn *a, int grad, size_t *bytes)
 {
     if (!a || !bytes) return SMALL_ERR_NULL;
     if (const int rc = attn_check(*a)) return rc;
-    *bytes = grad ? plan_grad(*a).bytes : plan_attn(*a).bytes;
+    const AttnPlan forward = plan_attn(*a);
+    const GradPlan gradient = plan_grad(*a);
+    if (!(grad ? grad_launches(*a, gradient) : attn_launches(*a, forward))) return SMALL_ERR_SHAPE;
+    *bytes = grad ? gradient.bytes : forward.bytes;
     return SMALL_OK;
 }
 
@@ -321,6 +336,7 @@ int small_attention(const small_attn *a, const float *q, const float *k, const f
     if (!a || !q || !k || !v || !out) return SMALL_ERR_NULL;
     if (const int rc = attn_check(*a)) return rc;
     const AttnPlan p = plan_attn(*a);
+    if (!attn_launches(*a, p)) return SMALL_ERR_SHAPE;
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return SMALL_ERR_WORKSPACE;
     const Laid o = laid(*a, out, a->out, a->heads, a->Sq);
     const Laid in[] = {laid(*a, q, a->q, a->heads, a->Sq), laid(*a, k, a->k, a->kv_heads, a->Sk), laid(*a, v, a->v, a->kv_heads, a->Sk)};
@@ -352,6 +368,7 @@ int small_attention_grad(const small_attn *a, const float *q, const float *k, co
     if (const int rc = attn_check(*a)) return rc;
     if (dtable && !a->table) return SMALL_ERR_NULL;
     const GradPlan p = plan_grad(*a);
+    if (!grad_launches(*a, p)) return SMALL_ERR_SHAPE;
     if (!workspace_ok(workspace, workspace_bytes, p.bytes)) return SMALL_ERR_WORKSPACE;
     const Laid in[] = {laid(*a, q, a->q, a->heads, a->Sq), laid(*a, k, a->k, a->kv_heads, a->Sk), laid(*a, v, a->v, a->kv_heads, a->Sk),
                        laid(*a, out, a->out, a->heads, a->Sq), laid(*a, dout, a->dout, a->heads, a->Sq)};

@@ -76,7 +76,8 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
  * rounding, 2^-24 of its size (with slopes, which make lse large, weights are scaled to sum to one).
  *
  * All of lengths, first, prefix, docs, slopes, table and bucket are DEVICE pointers. Limits: D <= 256; Sq, Sk <= 2^28, first positions are
- * taken into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31. Tensors may be larger than 2^31 values.
+ * taken into -2^28 .. 2^28; heads / kv_heads * Sq and N * heads * Sq < 2^31, and of the launches none has 2^32 threads (tiles of
+ * 64 tokens of all heads and images below 2^24 forward and 2^23 in the gradient; heads times offsets of a table below 2^27 there). Tensors may be larger than 2^31 values.
  * lse may be NULL in the forward call. small_attention_workspace (host only): bytes for a forward call (grad = 0) or a gradient call (grad = 1); of the pointers in *a it only matters whether table is NULL;
  * 256-byte aligned (0 is possible: then it may be NULL).
  *
