@@ -443,7 +443,9 @@ __device__ __forceinline__ void raise_top(floatx4 (&s)[NB], Reference &top, floa
     if (!__any(mx > (top.seen ? kSlack + lift : -kInf))) return;
     mx = column_max(mx) - lift;
     // (a lower reference is never taken; what is taken off is what the reference gains after rounding, or old sums and new ones would stand for different ones)
-    const float now = top.at + (top.seen ? fmaxf(mx, 0.f) : (mx == -kInf ? 0.f : mx)), by = now - top.at;
+    const float gain = top.seen ? fmaxf(mx, 0.f) : (mx == -kInf ? 0.f : mx), now = top.at + gain, by = now - top.at;
+    // (from 2^23 on a reference's rounding is a whole power of two or more: there the largest score is the reference by decree, or its weight could be 0 or infinite)
+    const float off = fabsf(now) < 8388608.f ? by : gain;
     const float w = top.seen ? __builtin_amdgcn_exp2f(-by) : 1.f;                    // (nothing was summed so far)
     top.at = now;
     top.seen |= mx != -kInf;
@@ -451,7 +453,7 @@ __device__ __forceinline__ void raise_top(floatx4 (&s)[NB], Reference &top, floa
 #pragma unroll
     for (int d = 0; d < DT; ++d) o[d] *= w;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) s[b] -= by;
+    for (int b = 0; b < NB; ++b) s[b] -= off;
 }
 
 // 4 VD neighbouring channels of a lane's column from result tiles grp * VD .. : quad x of them.

@@ -295,3 +295,23 @@ def test_table_gradient_of_rows_far_behind_the_keys_they_see(D):
     want = exact(c)["dtable"][0]
     off = gradients(c)[5].double().cpu() - want
     assert float(off.norm()) <= 2e-6 * float(want.norm())
+
+
+@pytest.mark.parametrize("big", [1e9, 1e20])
+@pytest.mark.parametrize("shape", ["parts", "parts, many rows", "parts, distances", "parts, everything", "fp32", "fp32, wide heads", "small"])
+def test_large_scores_that_are_seen(shape, big):
+    """A few keys far larger than the others, which rows do see: their scores are so far apart that a row's weights are 0 or 1 (or theirs are 0 and the
+    others' what they are without them). Forward calls; a score's rounding, which is that of its size, must not become a weight."""
+    S = SHAPES[shape]["Sq"]
+    c = Case(**SHAPES[shape], causal=True)
+    c.k[0, :, [5, S // 2, S // 2 + 1, S - 40]] *= torch.tensor([1.0, 3.0, 0.5, 2.0]) * big
+    o, l = c.forward()
+    compare(c, {"out": plain(o), "lse": l}, exact(c))
+
+
+@pytest.mark.parametrize("Sk", [33, 900, 5000])
+def test_large_scores_that_single_tokens_see(Sk):
+    c = Case(N=3, Sq=1, Sk=Sk, heads=8, kv=2, D=32)
+    c.k[:, :, [3, 17, Sk - 2]] *= torch.tensor([1.0, 3.0, 0.5]) * 1e20
+    o, l = c.forward()
+    compare(c, {"out": plain(o), "lse": l}, exact(c))
