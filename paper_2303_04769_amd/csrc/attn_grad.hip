@@ -536,14 +536,6 @@ __global__ void __launch_bounds__(1024) attn_bias_buckets(const float *sums, con
 // Tiles of the streamed side.
 #define GRAD_FORMS(X) X(1, 64) X(2, 64) X(3, 64) X(4, 64) X(5, 32) X(6, 32) X(8, 32) X(16, 16)
 
-int attn_grad_tile(int D)
-{
-#define FORM(dt, kt) if (D <= 16 * dt) return kt;
-    GRAD_FORMS(FORM)
-#undef FORM
-    return 0;
-}
-
 hipError_t launch_attn_grad_shares(const AttnArgs &a, bool vec, hipStream_t s)
 {
     const unsigned grid = (unsigned)((long)a.N * a.heads * a.row_tiles);

@@ -512,7 +512,6 @@ hipError_t launch_attn_grad_shares(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_rows(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_keys(const AttnArgs &a, bool vec, hipStream_t s);
 hipError_t launch_attn_grad_bias(const AttnArgs &a, float *sums, float *dtable, hipStream_t s);
-int attn_grad_tile(int D);                                   // tokens of a tile that the gradient kernels stream
 hipError_t launch_attn_token(const AttnArgs &a, bool vec, hipStream_t s);
 
 }  // namespace small
