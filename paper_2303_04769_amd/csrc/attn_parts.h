@@ -28,7 +28,7 @@ typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTop = 10;                       // exponent of a tile's or row's largest value
-constexpr int kLift = 8;                       // of weights: with kSlack below 2^15
+constexpr int kLift = 9, kFall = 2;            // of weights: with kSlack 2^15 at most; tiles of values that may be 2^-kFall of the largest keep weights that much lower
 
 __device__ __forceinline__ floatx4 mfma16(half8 a, half8 b, floatx4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
@@ -187,47 +187,46 @@ __device__ __forceinline__ void by_token(floatx4 (&y)[NB], const int *each, int 
     }
 }
 
-// Scores behind their masks, minus infinity where the token is hidden: NaN where it is not and is bad.
-template <int NB>
+// Scores, of tokens of a mixed tile: NaN where the token is bad. MASKED: behind their masks, minus infinity where the token is hidden, which stays so.
+template <bool MASKED, int NB>
 __device__ __forceinline__ void bad_tokens(floatx4 (&s)[NB], const int *each)
 {
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
         const int4 e = *reinterpret_cast<const int4 *>(each + 16 * b);
-        s[b].x = (e.x == kBad) & (s[b].x != -kInf) ? __builtin_nanf("") : s[b].x;
-        s[b].y = (e.y == kBad) & (s[b].y != -kInf) ? __builtin_nanf("") : s[b].y;
-        s[b].z = (e.z == kBad) & (s[b].z != -kInf) ? __builtin_nanf("") : s[b].z;
-        s[b].w = (e.w == kBad) & (s[b].w != -kInf) ? __builtin_nanf("") : s[b].w;
+        s[b].x = (e.x == kBad) & (!MASKED | (s[b].x != -kInf)) ? __builtin_nanf("") : s[b].x;
+        s[b].y = (e.y == kBad) & (!MASKED | (s[b].y != -kInf)) ? __builtin_nanf("") : s[b].y;
+        s[b].z = (e.z == kBad) & (!MASKED | (s[b].z != -kInf)) ? __builtin_nanf("") : s[b].z;
+        s[b].w = (e.w == kBad) & (!MASKED | (s[b].w != -kInf)) ? __builtin_nanf("") : s[b].w;
     }
 }
 
-// The power of two of a column's terms: they times `scale` stay within 2^14. Nothing but zeros so far: scale = limit = 0.
+// The power of two of a column's terms: they times `scale` stay within 2^14. Nothing but zeros so far: scale = 2^127, which any term passes.
 struct ColumnScale {
-    float scale = 0.f, limit = 0.f;
-    // Takes terms y that count 2^exp each to the column's scale, which is set anew, and the sums acc along, where one passes the limit.
+    float scale = 0x1p127f;
+    // Takes terms y that count 2^exp each to the column's scale, which is set anew, and the sums acc along, where one passes 2^14.
     template <int NB, int DT>
     __device__ __forceinline__ void apply(floatx4 (&y)[NB], int exp, floatx4 (&acc)[DT])
     {
         float mx = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b) mx = fmaxf(mx, fmaxf(fmaxf(fabsf(y[b].x), fabsf(y[b].y)), fmaxf(fabsf(y[b].z), fabsf(y[b].w))));
-        mx = ldexpf(mx, exp);
-        if (__any(mx > limit)) {
-            mx = column_max(mx);
-            const bool more = mx > limit;
-            const int e = max(-100, (int)(__float_as_uint(mx) >> 23) - 127);
-            const float now = ldexpf(1.f, 8 - e), f = !more || scale == 0.f ? 1.f : ldexpf(now, ilogb_of(scale));
-#pragma unroll
-            for (int d = 0; d < DT; ++d) acc[d] *= f;
-            scale = more ? now : scale;
-            limit = more ? ldexpf(1.f, 6 + e) : limit;
-        }
         float f = ldexpf(scale, exp);
-        if (__any(f == kInf)) {                                  // (tokens 2^100 times as large as what the column has seen: it does not see these)
-            const float first = ldexpf(1.f, exp);
+        if (__any(!(mx * f <= 0x1p14f))) {
+            mx = column_max(ldexpf(mx, exp));
+            const bool more = mx * scale > 0x1p14f;
+            const int e = max(-100, (int)(__float_as_uint(mx) >> 23) - 127);
+            const float now = more ? ldexpf(1.f, 8 - e) : scale, by = ldexpf(now, back());
 #pragma unroll
-            for (int b = 0; b < NB; ++b) y[b] *= first;
-            f = scale;
+            for (int d = 0; d < DT; ++d) acc[d] *= by;
+            scale = now;
+            f = ldexpf(scale, exp);
+            if (__any(f == kInf)) {                              // (tokens 2^20 times and more as large as what the column has seen: it does not see these)
+                const float first = ldexpf(1.f, exp);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) y[b] *= first;
+                f = scale;
+            }
         }
 #pragma unroll
         for (int b = 0; b < NB; ++b) y[b] *= f;
@@ -236,18 +235,16 @@ struct ColumnScale {
     template <int DT>
     __device__ __forceinline__ void follow(float by, floatx4 (&acc)[DT])
     {
-        if (!__any((by >= 1.f) & (scale != 0.f))) return;
-        const int k = scale == 0.f ? 0 : max(0, min((int)fminf(by, 300.f), 108 + ilogb_of(scale)));
+        if (!__any(by >= 1.f)) return;
+        const int k = max(0, min((int)fminf(by, 300.f), 108 + back()));
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
             for (int x = 0; x < 4; ++x) acc[d][x] = ldexpf(acc[d][x], k);
         scale = ldexpf(scale, k);
-        limit = ldexpf(limit, -k);
     }
-    static __device__ __forceinline__ int ilogb_of(float s) { return 127 - (int)(__float_as_uint(s) >> 23); }      // (of 1 / s)
-    __device__ __forceinline__ int back() const { return scale == 0.f ? 0 : ilogb_of(scale); }
-    __device__ __forceinline__ float back(float factor) const { return scale == 0.f ? 0.f : ldexpf(factor, ilogb_of(scale)); }
+    __device__ __forceinline__ int back() const { return 127 - (int)(__float_as_uint(scale) >> 23); }      // scale = 2^-back
+    __device__ __forceinline__ float back(float factor) const { return ldexpf(factor, back()); }
 };
 
 constexpr size_t parts_tile_bytes(int steps) { return (size_t)64 * 32 * steps * 4; }

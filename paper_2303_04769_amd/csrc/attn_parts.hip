@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(256, STEPS == 1 && MODE <= 2 ? 5 : STEPS <= 2 
         begin = min(end, begin + split * per);
         end = min(end, begin + per);
     }
-    // The largest power of two that the values of these keys carry: all weighted sums are kept at it, where no tile's is less than half of it and no tile is mixed
+    // The largest power of two that the values of these keys carry: all weighted sums are kept at it, where no tile's is less than a quarter of it and no tile is mixed
     // (even). Where not, each row's at its own.
     const int tiles = (a.Sk + 63) / 64;
     const size_t first_tile = ((size_t)n * kv + key_head) * tiles;
@@ -168,7 +168,7 @@ __global__ void __launch_bounds__(256, STEPS == 1 && MODE <= 2 ? 5 : STEPS <= 2 
         powers.add(v_exps[x]);
         powers.add_mixed(k_exps[x]);
     }
-    const bool even = powers.even(1);
+    const bool even = powers.even(kFall);
     const int v_exp = powers.most;
 
     const char *k_image = a.k_tok + first_tile * IMAGE, *v_image = a.v_tok + first_tile * IMAGE;
@@ -227,14 +227,14 @@ __global__ void __launch_bounds__(256, STEPS == 1 && MODE <= 2 ? 5 : STEPS <= 2 
             }
             if (!EVEN && tile_mixed(k_word)) {
                 by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g, q_exp);
+                bad_tokens<false>(s, a.k_each + first_tile * 64 + j0 + 4 * g);
                 dot_exp = 0;
             }
+            if (!EVEN && tile_mixed(v_word)) bad_tokens<false>(s, a.v_each + first_tile * 64 + j0 + 4 * g);
             // weights near fp16's top, and at the power of two that the sums carry
-            const int lift = !EVEN ? 0 : v_now < v_exp ? kLift - 1 : kLift;
+            const int lift = !EVEN ? 0 : kLift + max(v_now - v_exp, -kFall);
             const float in_exponent = (float)lift, was = top.at;
             finish_scores<MODE>(a, s, row, dot_exp, top.at - in_exponent, j0, key_code, key_doc, g, bias, far_lo, far_hi);
-            if (!EVEN && tile_mixed(k_word)) bad_tokens(s, a.k_each + first_tile * 64 + j0 + 4 * g);
-            if (!EVEN && tile_mixed(v_word)) bad_tokens(s, a.v_each + first_tile * 64 + j0 + 4 * g);
             raise_top(s, top, sum, o, in_exponent);
             if (!EVEN) vs.follow(top.at - was, o);
             floatx4 part = {};

@@ -275,7 +275,7 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             const float dp_in = ldexpf(1.f, dp_exp);
             floatx4 core[4];
             finish_scores<MODE>(a, s, row, dot_exp, lse2, j0, key_code, key_doc, g, bias, far_lo, far_hi, (MODE & 1) ? core : nullptr);
-            if (MIXED && tile_mixed(k_word)) bad_tokens(s, a.k_each + first_tile * 64 + j0 + 4 * g);      // (of V: delta is NaN)
+            if (MIXED && tile_mixed(k_word)) bad_tokens<true>(s, a.k_each + first_tile * 64 + j0 + 4 * g);      // (of V: delta is NaN)
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
@@ -597,8 +597,8 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
                         s[b].w = x.w == doc ? s[b].w : -kInf;
                     }
                 }
-                if (!EVEN && tile_mixed(q_word)) bad_tokens(s, a.q_each + first_tile * 64 + i0 + 4 * g);
-                if (!EVEN && tile_mixed(d_word)) bad_tokens(s, a.do_each + first_tile * 64 + i0 + 4 * g);
+                if (!EVEN && tile_mixed(q_word)) bad_tokens<true>(s, a.q_each + first_tile * 64 + i0 + 4 * g);
+                if (!EVEN && tile_mixed(d_word)) bad_tokens<true>(s, a.do_each + first_tile * 64 + i0 + 4 * g);
                 const float lift = EVEN ? ldexpf(1.f, max(0, 14 + d_exp - d_most)) : 1.f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
