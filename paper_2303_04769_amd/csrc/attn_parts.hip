@@ -2,11 +2,11 @@
 // layouts. Tiles of 64 rows (16 a wave) walk over tiles of 64 keys in LDS, four workgroups a compute unit up to 64 channels: sixteen rows a wave leave
 // registers for that (32 rows a wave, half the LDS reads but half the waves: 311 against 208 us in an early form).
 //
-// Bound by vector instructions, not by the matrix instructions that they feed: a score is scaled, capped, biased, masked, made a weight and split in two,
+// Bound by vector instructions, not by the matrix instructions that they feed, and by waits at the two barriers of a tile: a score is scaled, capped, biased, masked, made a weight and split in two,
 // some thirty instructions, 1900 cycles for a wave's tile of 16 x 64, where the matrix instructions take 768 at 64 channels. Counters for 4096 causal frames,
-// 8 heads of 64, capped, a bias by buckets, 2 sequences: vector ALU busy some 57 % of the time, matrix pipe 30 %. Measured: that case 143 us (4 D operations
-// a pair that is seen: 240 TFLOP/s; fp32 instructions 494 us), 8192 frames of packed documents with distances 142 us, 14 x 14 pixels, 8 heads of 32, 64 images,
-// 35 us and 17 for laying keys and values out.
+// 8 heads of 64, capped, a bias by buckets, 2 sequences: vector ALU busy some 57 % of the time, matrix pipe 30 %. Measured: that case 140 to 151 us (4 D operations
+// a pair that is seen: 235 TFLOP/s; fp32 instructions 494 us), 8192 frames of packed documents with distances 138 to 147 us, 14 x 14 pixels, 8 heads of 32, 64 images,
+// 36 us and 18 for laying keys and values out. Uneven tiles (below): 212 us, 152 us.
 #include "attn_parts.h"
 
 #include <type_traits>

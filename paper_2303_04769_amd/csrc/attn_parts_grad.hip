@@ -4,12 +4,12 @@
 //
 // The tile that a wave holds comes straight from the images (a lane's operand is what the image has at its place), what it walks over through LDS.
 // P is at most 1 and is lifted to fp16's top. dS has no such bound worth having -- a long row's weights are small, and so are their gradients -- so it carries
-// a power of two for each column, set by the first tile and raised where a value would pass fp16's range.
+// a power of two for each column, set by the first tile and raised where a value would pass fp16's range; and so do dV's terms where dO's tiles are uneven.
 //
 // Bound as the forward kernel is, by some forty vector instructions a pair in either walk, and by waits that three workgroups a compute unit (registers; two from 65
 // channels on) do not cover: vector ALU busy 46 % and 41 %, matrix pipe 19 % and 22 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
-// buckets, 4 sequences. Measured there: rows 175 us, keys 200, and with the forward call and all else 453 (fp32
-// instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 66, keys 53.
+// buckets, 4 sequences. Measured there: rows 175 us, keys 191, and with the forward call and all else 446 to 455 (fp32
+// instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 67, keys 53.
 #include "attn_parts.h"
 
 #include <type_traits>
