@@ -8,9 +8,9 @@
 // fp16 has little range, so values carry a power of two: one for each tile of 64 tokens of a head (its largest magnitude comes to lie in
 // [2^10, 2^11)), one for each row that a wave holds in registers. A value 2^-12 times the tile's largest still has 22 bits, and below that the error is
 // 2^-35 of the largest one. A mask may hide any token of a tile from a row, and what it hides must not cost the row precision: so a token whose largest value is
-// less than 2^-kSpread of the tile's carries a power of its own, and the tile says so (mixed). Weighted sums over tiles (of values by scores' weights, of dO by columns'
-// weights) are kept at one power of two where all tiles of a walk have about the same and none is mixed, and where not, at one for each row or
-// column, which follows the largest of the terms that the row sees (ColumnScale). So no magnitude is out of reach, and a result's error is in proportion to the largest
+// less than 2^-kSpread of the tile's carries a power of its own, and the tile says so (mixed). Weighted sums over tiles are kept at a power of two for each row (column of
+// a product), which follows the largest of the terms that the row sees (ColumnScale) -- those of values at one for all rows where all tiles of a walk have about the same
+// and none is mixed (even). So no magnitude is out of reach, and a result's error is in proportion to the largest
 // magnitude among the channels of the tokens that it is made of, not to anything else. A token that holds an infinity or NaN is laid out as zeros (0 times it would not
 // be 0) and says so in place of its power of two (kBad); scores of those that see it become NaN.
 //
@@ -89,21 +89,26 @@ __device__ __forceinline__ RowTile row_tile_of(const AttnArgs &a, unsigned group
     return {(int)(part * each + (r - by_tile * each)), (int)(tiles - 1 - by_tile), 0};
 }
 
-// What a tile's tokens carry, in a word: the power of two (kNone: nothing but zeros), and whether tokens have some of their own.
+// What a tile's tokens carry, in a word: the power of two (kNone: nothing but zeros), whether tokens have some of their own (mixed), and whether there are zeros
+// among them. A token of zeros has no size: where sums follow the largest term, one that carried its tile's power would raise them to the size of what may be hidden. So there its
+// power is the smallest one, as if the tile were mixed (by_tokens); where sums are kept at one power of two anyway, it may carry any.
 constexpr int kNone = -1000, kBad = 10000;
-__device__ __forceinline__ int tile_exponent(int word) { return word >> 1; }
+__device__ __forceinline__ int tile_word(int exponent, bool zeros, bool mixed) { return exponent * 4 + zeros * 2 + mixed; }
+__device__ __forceinline__ int tile_exponent(int word) { return word >> 2; }
 __device__ __forceinline__ bool tile_mixed(int word) { return word & 1; }
+__device__ __forceinline__ bool tile_by_tokens(int word) { return word & 3; }
 
 // Of the words that a wave's lanes go through one after another: the largest power of two and the smallest (of tiles that have one), and whether any tile is mixed.
 struct Powers {
     int most = kNone, least = -kNone;
-    bool mixed = false;
+    bool mixed = false, zeros = false;
     __device__ __forceinline__ void add(int word)
     {
         const int e = tile_exponent(word);
         most = max(most, e);
         least = e == kNone ? least : min(least, e);
         mixed |= tile_mixed(word);
+        zeros |= tile_by_tokens(word);
     }
     __device__ __forceinline__ void add_mixed(int word) { mixed |= tile_mixed(word); }
     // Over the wave: whether no tile is mixed and all are within 2^-spread of the largest. most: uniform from here on.
@@ -121,6 +126,8 @@ struct Powers {
         most = over_wave((float)most);
         return !__any(mixed) && most - low <= spread;
     }
+    // For terms whose scale follows the largest: whether no tile is mixed, and none has zeros (tile_word) where tiles are of unlike size.
+    __device__ __forceinline__ bool even_terms() { return __any(zeros) ? even(kSpread) : !__any(mixed); }
 };
 
 // A tile's word, by a scalar load: it counts apart from the copies into LDS, which the compiler does not see and which a wait for a vector load would include.
@@ -131,7 +138,7 @@ struct PartsTensor {
     TokenStrides s;
     int heads, tokens, tiles, rows;            // rows: not keys but queries (their masks: rows of lse = -inf are left out)
     char *image;
-    int *exps, *each;                          // [N * heads][tiles], [N * heads][tiles][64] (written for mixed tiles)
+    int *exps, *each;                          // [N * heads][tiles], [N * heads][tiles][64] (written for mixed tiles and those with zeros)
     unsigned first_block;
 };
 struct PartsArgs {

@@ -31,6 +31,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
     floatx4 x[PER][4];
     const int tq = threadIdx.x >> 2 & 15;
     floatx4 most{0.f, 0.f, 0.f, 0.f};
+    int there = 0;                                         // of the four tokens: those that anything may see
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const int e = threadIdx.x + p * 256, dq = (e & 3) | (e >> 6) << 2;
@@ -42,6 +43,7 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
             if (on && !t.rows && a.docs) on = a.docs[(size_t)n * a.Sk + j] >= 0;
             x[p][i] = floatx4{0.f, 0.f, 0.f, 0.f};
             if (on) x[p][i] = load_quad<VEC>(a, t.s, token_at(t.p, t.s, n, j), head * a.D, dq * 4);
+            there |= on << i;
 #pragma unroll
             for (int d = 0; d < 4; ++d) most[i] = fmaxf(most[i], any_magnitude(x[p][i][d]));
         }
@@ -68,16 +70,18 @@ __global__ void __launch_bounds__(256) attn_make_parts(AttnArgs a, PartsArgs arg
     // (nothing but zeros: any power does for them)
     const int ex = parts_exponent(all);
     int own[4];
-    bool mixed = false;
+    bool mixed = false, zeros = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int y = parts_exponent(most[i]);
-        own[i] = most[i] == kInf ? kBad : most[i] == 0.f || y >= ex - kSpread ? ex : y;
-        mixed |= own[i] != ex;
+        own[i] = most[i] == kInf ? kBad : most[i] == 0.f ? y : y >= ex - kSpread ? ex : y;
+        mixed |= most[i] != 0.f && own[i] != ex;
+        zeros |= most[i] == 0.f && (there >> i & 1);
     }
     mixed = __any(mixed);
-    if (mixed && threadIdx.x < 64 && (threadIdx.x & 3) == 0) *reinterpret_cast<int4 *>(t.each + (size_t)id * 64 + tq * 4) = int4{own[0], own[1], own[2], own[3]};
-    if (threadIdx.x == 0) t.exps[id] = (all == 0.f ? kNone : ex) * 2 + mixed;
+    zeros = __any(zeros);
+    if ((mixed | zeros) && threadIdx.x < 64 && (threadIdx.x & 3) == 0) *reinterpret_cast<int4 *>(t.each + (size_t)id * 64 + tq * 4) = int4{own[0], own[1], own[2], own[3]};
+    if (threadIdx.x == 0) t.exps[id] = tile_word(all == 0.f ? kNone : ex, zeros, mixed);
 #pragma unroll
     for (int p = 0; p < PER; ++p) {
         const int e = threadIdx.x + p * 256, dq = (e & 3) | (e >> 6) << 2;
@@ -246,8 +250,8 @@ __global__ void __launch_bounds__(256, STEPS == 1 && MODE <= 2 ? 5 : STEPS <= 2 
             }
             sum = fmaf((part.x + part.y) + (part.z + part.w), ldexpf(1.f, -lift), sum);
             if (!EVEN) {
-                if (tile_mixed(v_word)) by_token(s, a.v_each + first_tile * 64 + j0 + 4 * g);
-                vs.apply(s, tile_mixed(v_word) ? 0 : v_now, o);
+                if (tile_by_tokens(v_word)) by_token(s, a.v_each + first_tile * 64 + j0 + 4 * g);
+                vs.apply(s, tile_by_tokens(v_word) ? 0 : v_now, o);
             }
             half8 p_hi[2], p_lo[2];
 #pragma unroll

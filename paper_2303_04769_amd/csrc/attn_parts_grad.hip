@@ -3,8 +3,8 @@
 // tiles of 32 rows of its query heads; where there are few key tiles, its rows are shared out over several workgroups, whose sums attn_grad_join adds.
 //
 // The tile that a wave holds comes straight from the images (a lane's operand is what the image has at its place), what it walks over through LDS.
-// P is at most 1 and is lifted to fp16's top. dS has no such bound worth having -- a long row's weights are small, and so are their gradients -- so it carries
-// a power of two for each column, set by the first tile and raised where a value would pass fp16's range; and so do dV's terms where dO's tiles are uneven.
+// P and dS have no size of their own -- a long row's weights are small, and so are their gradients, and a key may have small ones only -- so they carry
+// a power of two for each column, set by the first tile and raised where a value would pass fp16's range.
 //
 // Bound as the forward kernel is, by some forty vector instructions a pair in either walk, and by waits that three workgroups a compute unit (registers; two from 65
 // channels on) do not cover: vector ALU busy 46 % and 41 %, matrix pipe 19 % and 22 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
@@ -194,8 +194,13 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
     const int tiles = (a.Sk + 63) / 64;
     const size_t first_tile = ((size_t)n * kv + key_head) * tiles;
     const int *k_exps = a.k_exps + first_tile, *v_exps = a.v_exps + first_tile;
-    bool mixed = tile_mixed(q_word | d_word);
-    for (int x = begin / 64 + lane; x * 64 < end; x += 64) mixed |= tile_mixed(k_exps[x] | v_exps[x]);
+    Powers powers;
+    powers.add_mixed(q_word | d_word);
+    for (int x = begin / 64 + lane; x * 64 < end; x += 64) {
+        powers.add(k_exps[x]);
+        powers.add_mixed(v_exps[x]);
+    }
+    const bool even = powers.even_terms();
     const unsigned lds = lds_address(parts_lds);
     if (begin < end) {
         copy_image(a.k_tok + (first_tile + begin / 64) * IMAGE, IMAGE, lds);
@@ -305,8 +310,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
                 for (int b = 0; b < 4; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
-            if (MIXED && tile_mixed(k_word)) by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g);
-            cs.apply(s, MIXED && tile_mixed(k_word) ? 0 : tile_exponent(k_word), dq);
+            if (MIXED && tile_by_tokens(k_word)) by_token(s, a.k_each + first_tile * 64 + j0 + 4 * g);
+            cs.apply(s, MIXED && tile_by_tokens(k_word) ? 0 : tile_exponent(k_word), dq);
             half8 hi_[2], lo_[2];
 #pragma unroll
             for (int b = 0; b < 2; ++b) split_results(s[2 * b], s[2 * b + 1], hi_[b], lo_[b]);
@@ -325,8 +330,8 @@ __global__ void __launch_bounds__(256, STEPS <= 2 ? 3 : 2) attn_grad_rows_parts(
             __syncthreads();
             next_values(j0);
         }
-    else if (__any(mixed)) walk(std::true_type{});
-    else walk(std::false_type{});
+    else if (__builtin_expect(even, 1)) walk(std::false_type{});
+    else walk(std::true_type{});
     const AttnArgs z = late_args();
     if (sums) {
         __shared__ float ends[8];
@@ -414,18 +419,16 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
         begin = min(end, begin + row_part * per);
         end = min(end, begin + per);
     }
-    // The largest power of two that these rows' dO carry: all of dV's sums are kept at it, where no tile's is less than 2^-4 of it and no tile is mixed, these keys' included (even).
-    // Where not, each key's at its own.
-    Powers powers;
-    powers.add_mixed(k_word | v_word);
+    // Whether neither these keys nor the rows' queries and dO have powers of two by token that count.
+    Powers of_q, of_d;
+    of_q.add_mixed(k_word | v_word);
     for (int h = h0; h < h1; ++h)
         for (int x = begin / 64 + lane; x * 64 < end; x += 64) {
             const size_t at = ((size_t)n * a.heads + h) * a.row_tiles + x;
-            powers.add(a.do_exps[at]);
-            powers.add_mixed(a.q_exps[at]);
+            of_q.add(a.q_exps[at]);
+            of_d.add(a.do_exps[at]);
         }
-    const bool even = powers.even(4);
-    const int d_most = powers.most;
+    const bool even = of_q.even_terms() & of_d.even_terms();
 
     float *const bias_lds = reinterpret_cast<float *>(parts_lds + 4 * HALF);
     const unsigned lds = lds_address(parts_lds);
@@ -599,7 +602,6 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
                 }
                 if (!EVEN && tile_mixed(q_word)) bad_tokens<true>(s, a.q_each + first_tile * 64 + i0 + 4 * g);
                 if (!EVEN && tile_mixed(d_word)) bad_tokens<true>(s, a.do_each + first_tile * 64 + i0 + 4 * g);
-                const float lift = EVEN ? ldexpf(1.f, max(0, 14 + d_exp - d_most)) : 1.f;
 #pragma unroll
                 for (int b = 0; b < 2; ++b) {
                     const floatx4 d4 = *reinterpret_cast<const floatx4 *>(rows.delta + 16 * b + 4 * g);
@@ -610,7 +612,6 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
                     for (int e = 0; e < 4; ++e) {
                         const float p = s[b][e];
                         dp[b][e] = p == 0.f ? 0.f : p * fmaf(dp[b][e], dp_in, -d4[e]);
-                        s[b][e] = p * lift;
                     }
                 }
                 if (capped)
@@ -618,13 +619,12 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
                     for (int b = 0; b < 2; ++b)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) dp[b][e] *= fmaf(-core[b][e], core[b][e], 1.f);
-                const bool q_mixed = !EVEN && tile_mixed(q_word);
-                if (q_mixed) by_token(dp, a.q_each + first_tile * 64 + i0 + 4 * g);
-                cs.apply(dp, q_mixed ? 0 : q_exp, dk);
-                if (!EVEN) {
-                    if (tile_mixed(d_word)) by_token(s, a.do_each + first_tile * 64 + i0 + 4 * g);
-                    vs.apply(s, tile_mixed(d_word) ? 0 : d_exp, dv);
-                }
+                const bool q_by_tokens = !EVEN && tile_by_tokens(q_word);
+                if (q_by_tokens) by_token(dp, a.q_each + first_tile * 64 + i0 + 4 * g);
+                cs.apply(dp, q_by_tokens ? 0 : q_exp, dk);
+                const bool d_by_tokens = !EVEN && tile_by_tokens(d_word);
+                if (d_by_tokens) by_token(s, a.do_each + first_tile * 64 + i0 + 4 * g);
+                vs.apply(s, d_by_tokens ? 0 : d_exp, dv);
                 half8 p_hi, p_lo, s_hi, s_lo;
                 split_results(s[0], s[1], p_hi, p_lo);
                 split_results(dp[0], dp[1], s_hi, s_lo);
@@ -637,7 +637,7 @@ __global__ void __launch_bounds__(256, STEPS == 1 ? 4 : STEPS == 2 || (STEPS == 
     else walk(std::false_type{});
     const AttnArgs z = late_args();
     if (j_raw >= z.Sk) return;
-    const float dk_back = cs.back(z.scale), dv_back = even ? ldexpf(1.f, d_most - 14) : vs.back(1.f);
+    const float dk_back = cs.back(z.scale), dv_back = vs.back(1.f);
     if (z.splits > 1) {
         // [part][image, key head][key][dk, dv][D]
         float *to = z.part_o + ((((size_t)part * z.N + n) * kv + key_head) * z.Sk + j) * 2 * z.D;

@@ -72,8 +72,8 @@ int small_groupnorm_grad(const float *in, const float *gamma, const float *beta,
  *
  * Precision. Larger calls hold values as two fp16 numbers at a power of two of their token's largest channel: 22 bits of values down to 2^-12 of that, one less for every
  * halving below; their products are summed in fp32. So results are as near to 64 bits as those of fp32 products (which round every addition)
- * where the channels of a token are of like size, and a channel 2^-35 of its neighbours is lost. Weights are held to 2^-33 of a row's largest or better (2^-38 of one in dk
- * and dv): what only smaller ones contribute may come out as zero. Distances past 2^24 are rounded as fp32 does. (What a mask hides may decide which of two ways a value is rounded, no
+ * where the channels of a token are of like size, and a channel 2^-35 of its neighbours is lost. A row's weights are held to 2^-33 of its largest or better, and the
+ * terms of a gradient to 2^-33 of its largest: what only smaller ones contribute may come out as zero. Distances past 2^24 are rounded as fp32 does. (What a mask hides may decide which of two ways a value is rounded, no
  * more.) The gradients take their weights from lse, and so have the error of lse's rounding, 2^-24 of its size; with slopes, which make lse large, weights are scaled to sum
  * to one. Past scores of some 2^20 lse does not hold them apart any more, and gradients of rows that see such may be infinite or NaN.
  *

@@ -182,6 +182,39 @@ def test_large_values_in_hidden_places(shape, mask, big):
             raise AssertionError(f"{name}: {e}") from None
 
 
+@pytest.mark.parametrize("whole", [False, True], ids=["some", "tile"])
+@pytest.mark.parametrize("mask", [causal, documents], ids=["causal", "documents"])
+@pytest.mark.parametrize("shape", SHAPES)
+def test_zeros_beside_large_values_in_hidden_places(shape, mask, whole):
+    """Tokens of nothing but zeros, which rows see, beside large ones that these rows do not see, a few of each or a whole tile of 64: zeros have no size of their own to
+    go by."""
+    S = SHAPES[shape]["Sq"]
+    edge = S // 3 + 5
+    begin = edge // 64 * 64
+    low, high = list(range(begin, edge)), list(range(edge, min(begin + 64, S)))
+    rows = torch.arange(S)
+    for name in ("v", "k", "dout", "q"):
+        c = Case(**SHAPES[shape], **mask(S))
+        t = getattr(c, name)
+        # (of a causal mask's keys the late ones are hidden; of rows, and of documents here, the early ones)
+        large, zeros = (high, low) if mask is causal and name in "kv" else (low, high)
+        if not whole:
+            large, zeros = large[-1:], zeros[::7]
+        t[0, :, large] *= 1e20
+        t[0, :, zeros] = 0.0
+        where = None
+        if name in "kq":
+            good = rows >= edge if mask is documents else rows < large[0] if name == "k" else rows > large[-1]
+            none = torch.zeros(S, dtype=torch.bool)
+            out = good if name == "k" else torch.tensor([int(i) not in large for i in rows])
+            keys = good if mask is documents else none if name == "k" else good
+            where = {"out": out, "lse": out, "dq": out, "dk": keys, "dv": keys, "dtable": torch.tensor(False)}
+        try:
+            compare(c, everything(c), exact(c), where)
+        except AssertionError as e:
+            raise AssertionError(f"{name}: {e}") from None
+
+
 @pytest.mark.parametrize("step", [1.0, 20.0])
 @pytest.mark.parametrize("shape", ["parts", "parts, many rows", "parts, capped, buckets", "fp32"])
 def test_magnitudes_that_rise_along_a_sequence(shape, step):
