@@ -8,7 +8,7 @@
 //
 // Bound as the forward kernel is, by some forty vector instructions a pair in either walk, and by waits that three workgroups a compute unit (registers; two from 65
 // channels on) do not cover: vector ALU busy 46 % and 41 %, matrix pipe 19 % and 22 % for 2048 frames with a prefix, 8 heads of 64 on 2, capped, a bias by
-// buckets, 4 sequences. Measured there: rows 175 us, keys 191, and with the forward call and all else 446 to 455 (fp32
+// buckets, 4 sequences. Measured there: rows 175 to 182 us, keys 191 to 200, and with the forward call and all else 446 to 463 (fp32
 // instructions: 2123); 14 x 14 pixels, 8 heads of 32, a bias by offsets, 64 images: rows 67, keys 53.
 #include "attn_parts.h"
 
