@@ -15,7 +15,8 @@ LIB = os.path.join(HERE, "libsmall_hip.so")
 FASTCALL = os.path.join(HERE, f"_fastcall.{sysconfig.get_config_var('SOABI')}.torch-{torch.__version__}.so")
 PROBE_LIB = os.path.join(HERE, "libsmall_probe.so")       # the benchmark's matrix-rate probe, a library of its own
 SOURCES = ["elementwise.hip", "window.hip", "window_rows.hip", "window_dpp.hip", "window_dpp_u8.hip", "pool_dpp_u8.hip", "quant_ends.hip", "pool_dpp.hip", "conv.hip", "conv_same.hip", "conv_pw.hip", "conv_split.hip", "conv_split3.hip", "conv_split3_wide.hip", "dwpw.hip", "dwpw_run.hip", "dwpw_team.hip", "chain.hip", "resident.hip", "quant.hip", "conv_u8_tile.hip", "conv_u8_pw.hip", "layout_u8.hip", "resident_u8.hip", "table2.hip", "small_api.hip",
-           "groupnorm.hip", "attn.hip", "attn_token.hip", "attn_parts.hip", "attn_parts_grad.hip", "attn_grad.hip", "attn_api.hip"]
+           "groupnorm.hip", "attn.hip", "attn_token.hip", "attn_parts.hip", "attn_parts_grad.hip", "attn_grad.hip", "attn_api.hip",
+           "rotary.hip", "cache_store.hip", "cache_token.hip", "cache_api.hip"]
 # packed fp32 VALU ops are switched off for every device translation unit
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-fno-gpu-rdc", "-Wall", "-Wno-unused-function", "-Wno-pass-failed",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
@@ -67,13 +68,14 @@ def build_lib(force=False, verbose=False):
         force = True
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     headers = [os.path.join(CSRC, "small_internal.h"), os.path.join(HERE, "..", "include", "small.h")]
-    block = [os.path.join(CSRC, "attn_tile.h"), os.path.join(CSRC, "attn_row.h"), os.path.join(CSRC, "attn_parts.h"), os.path.join(HERE, "include", "small_attn.h")]
+    block = [os.path.join(CSRC, h) for h in ("attn_tile.h", "attn_row.h", "attn_parts.h", "attn_laid.h", "rotary.h", "cache.h")] + \
+            [os.path.join(HERE, "include", h) for h in ("small_attn.h", "small_cache.h")]
     objs, procs = [], []
     for src in SOURCES:
         s = os.path.join(CSRC, src)
         o = os.path.join(OBJ, src.replace(".hip", ".o"))
         objs.append(o)
-        if force or _stale(o, [s] + headers + (block if src.startswith(("attn", "groupnorm")) else [])):
+        if force or _stale(o, [s] + headers + (block if src.startswith(("attn", "groupnorm", "rotary", "cache")) else [])):
             cmd = [hipcc] + FLAGS + ["-c", s, "-o", o]
             if verbose:
                 print(" ".join(cmd), flush=True)
