@@ -61,6 +61,19 @@ def load():
     return _lib
 
 
+_fastcall = None
+
+
+def _fast():
+    """The extension's calls (binding._fast), told once what the plans' records are."""
+    global _fastcall
+    if _fastcall is None:
+        fast = A._fast()
+        fast.bind_cache(small_rotation, small_cache)
+        _fastcall = fast
+    return _fastcall
+
+
 def small_rotary_workspace(record):
     n = C.c_size_t(0)
     B._check(load().small_rotary_workspace(C.byref(record), C.byref(n)), "small_rotary_workspace")
@@ -140,6 +153,10 @@ class Rotary:
 
     def run(self, q, k, freq, q_out=None, k_out=None, first=None, positions=None, stream=None):
         """Turns q and k (either may be None) into q_out and k_out, or in place where these are None."""
+        if stream is None:
+            rc = _fast().rotary(self.record, q, k, freq, positions, first, q_out, k_out, None)
+            if rc is not None:
+                return B._check(rc, "small_rotary")
         self._fill(freq, first, positions)
         pq, pk = self._pair(q, k, ("q", "k"))
         po, pko = self._pair(q if q_out is None else q_out, k if k_out is None else k_out, ("q_out", "k_out"))
@@ -149,11 +166,16 @@ class Rotary:
         """Turns the gradients of run's outputs back into those of its inputs (in place where dq and dk are None). With dfreq, [freq_heads][axes][pairs], the frequencies'
         gradient too, from q and k: run's outputs, or its inputs."""
         r = self.record
+        if dfreq is not None and self._workspace is None:
+            self._fill(freq, first, positions)
+            self._workspace = torch.empty(small_rotary_workspace(r), dtype=torch.uint8, device=self.device)
+        if stream is None:
+            rc = _fast().rotary_grad(r, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, None if dfreq is None else self._workspace, None)
+            if rc is not None:
+                return B._check(rc, "small_rotary_grad")
         self._fill(freq, first, positions)
         if dfreq is not None:
             A._floats(dfreq, (r.freq_heads, r.axes, r.pairs))
-            if self._workspace is None:
-                self._workspace = torch.empty(small_rotary_workspace(r), dtype=torch.uint8, device=self.device)
         pq, pk = self._pair(q, k, ("q", "k"))
         pdo, pdko = self._pair(dq_out, dk_out, ("q_out", "k_out"))
         pd, pdk = self._pair(dq_out if dq is None else dq, dk_out if dk is None else dk, ("dq", "dk"))
@@ -199,6 +221,10 @@ class PagedCache:
     def write(self, k, v, pages, first=None, counts=None, rotary=None, freq=None, positions=None, q=None, q_out=None, stream=None):
         """Tokens i < counts[n] of k and v into the cache at positions first[n] + i of stream n. With a Rotary plan of these sizes (and its freq) keys are turned on the way,
         and queries q into q_out (in place where it is None)."""
+        if stream is None:
+            rc = _fast().cache_write(self.record, k, v, pages, first, counts, None if rotary is None else rotary.record, freq, positions, q, q_out, None)
+            if rc is not None:
+                return B._check(rc, "small_cache_write")
         span, pk, pv = self._span(k, v, pages, first, counts)
         if rotary is None:
             if q is not None:
@@ -211,6 +237,10 @@ class PagedCache:
 
     def read(self, k, v, pages, first=None, counts=None, stream=None):
         """The same tokens from the cache into k and v; what is no token of a stream's is left as it was."""
+        if stream is None:
+            rc = _fast().cache_read(self.record, k, v, pages, first, counts, None)
+            if rc is not None:
+                return B._check(rc, "small_cache_read")
         span, pk, pv = self._span(k, v, pages, first, counts)
         small_cache_read(self.record, span, pk, pv, stream)
 
@@ -233,6 +263,10 @@ class CacheAttention:
         """q, out: [N][blocks][Sq][Cb]; pages: the streams' table; lengths: tokens that each stream has in the cache, with the new ones; first: position of the first new one
         (None: the last Sq)."""
         r = self.record
+        if stream is None:
+            rc = _fast().cache_attention(self.cache.record, r, q, out, lse, self.workspace, pages, lengths, first, slopes, table, bucket, None)
+            if rc is not None:
+                return B._check(rc, "small_cache_attention")
         if pages.shape[1] != self.per_stream:
             raise TypeError(f"expected a table of {self.per_stream} pages a stream, got {list(pages.shape)}")
         self.cache._table(pages, r.N)

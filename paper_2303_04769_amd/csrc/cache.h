@@ -10,6 +10,9 @@ struct CacheArgs {
     float *key_scales, *value_scales;
     int kind, pages, shift, kv_heads, D, Dk, per_stream;      // shift: log2 of a page's tokens
     const int *table;
+    int workgroups, least_rounds;                             // attention: at most so many, with so many rounds each at least
+    int2 *units;                                              // the first and last workgroup that has a part of a unit; null: none is split
+    FastDiv by_rows;
 };
 
 __host__ __device__ constexpr int cache_bytes(int kind) { return kind == SMALL_CACHE_F32 ? 4 : kind == SMALL_CACHE_BF16 ? 2 : 1; }
@@ -50,6 +53,8 @@ struct StoreArgs {
 };
 hipError_t launch_cache_write(const StoreArgs &a, bool vec, bool halves, hipStream_t s);                   // cache_store.hip
 hipError_t launch_cache_read(const StoreArgs &a, bool vec, hipStream_t s);
-hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool vec, hipStream_t s);             // cache_token.hip
+struct TokenShape { int rows, keys, per_cu; };               // rows of a tile, keys of a round, workgroups that a compute unit runs at a time
+TokenShape token_shape(int kind, int D, int rows);                                                          // cache_token.hip
+hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool joined, hipStream_t s);
 
 }  // namespace small

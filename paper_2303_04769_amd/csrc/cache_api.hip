@@ -211,7 +211,7 @@ CacheArgs cache_args(const small_cache &c)
 {
     const int size = cache_bytes(c.kind), fill = 16 / size;
     return CacheArgs{(char *)c.keys, (char *)c.values, c.key_scales, c.value_scales, c.kind, c.pages, log2_of(c.page), c.kv_heads, c.D, (c.D + fill - 1) / fill * fill,
-                     c.per_stream, c.table};
+                     c.per_stream, c.table, 0, 1, nullptr, {}};
 }
 struct CacheRanges { Range r[4]; };
 CacheRanges cache_ranges(const small_cache &c)
@@ -252,34 +252,41 @@ int token_check(const small_cache &c, const small_attn &a)
     if (a.N != c.N || a.kv_heads != c.kv_heads || a.D != c.D || a.width != 1 || a.prefix || a.docs) return SMALL_ERR_SHAPE;
     if ((double)a.N * a.heads * a.Sq > INT_MAX || !isfinite(a.scale) || !(a.cap >= 0.f) || isinf(a.cap)) return SMALL_ERR_SHAPE;
     if (!a.table != !a.bucket) return SMALL_ERR_NULL;
-    if (a.table && (a.reach < 0 || a.reach > kFar || a.buckets < 1)) return SMALL_ERR_SHAPE;
+    if (a.table && (a.reach < 0 || a.reach > kFar || a.buckets < 1 || (double)a.heads * a.buckets > 1 << 30)) return SMALL_ERR_SHAPE;
     return SMALL_OK;
 }
+// How the calls of these sizes share out their work (cache_token.hip): tiles of rows, workgroups, and places of parts: one for each pair of a workgroup and a
+// unit (a tile of rows of a key head of a stream) that it has a part of, of which there are fewer than workgroups and units together.
 struct TokenPlan {
-    int rows, row_tiles, splits;
-    size_t ml_at, bytes;
+    int rows, row_tiles, workgroups;
+    bool joined;
+    double rounds;
+    size_t ml_at, units_at, bytes;
 };
+constexpr int kLeastRounds = 1;
 TokenPlan plan_token(const small_cache &c, const small_attn &a)
 {
     TokenPlan p{};
     p.rows = a.heads / a.kv_heads * a.Sq;
-    p.row_tiles = (p.rows + 15) / 16;
-    const long base = (long)a.N * a.kv_heads * p.row_tiles, cus = device_cus(), most = ((long)c.per_stream * c.page + 255) / 256;
-    const long want = base < cus / 2 ? cus / base : (4 * cus + base - 1) / base;
-    p.splits = (int)(want < most ? want : most);
-    if (p.splits < 1) p.splits = 1;
+    const TokenShape shape = token_shape(c.kind, c.D, p.rows);
+    p.row_tiles = (p.rows + shape.rows - 1) / shape.rows;
+    const long of_unit = ((long)c.per_stream * c.page + shape.keys - 1) / shape.keys;
+    const double units = (double)a.N * a.kv_heads * p.row_tiles;
+    p.rounds = units * of_unit;
+    p.workgroups = (int)fmin(p.rounds, (double)shape.per_cu * device_cus());
+    p.joined = of_unit > 1;
     const auto up = [](size_t bytes) { return (bytes + 255) / 256 * 256; };
-    if (p.splits > 1) {
-        const size_t pieces = (size_t)a.N * a.kv_heads * p.rows * p.splits;
+    if (p.joined) {
+        const size_t pieces = (size_t)(units + p.workgroups) * shape.rows;
         p.ml_at = up(pieces * a.D * sizeof(float));
-        p.bytes = up(p.ml_at + pieces * sizeof(float2));
+        p.units_at = up(p.ml_at + pieces * sizeof(float2));
+        p.bytes = up(p.units_at + (size_t)units * sizeof(int2));
     }
     return p;
 }
 bool token_launches(const small_attn &a, const TokenPlan &p)
 {
-    const double workgroups = (double)a.N * a.kv_heads * p.row_tiles * p.splits;
-    return workgroups < INT_MAX && launches(workgroups, 512);
+    return p.rounds < INT_MAX && launches((double)a.N * a.kv_heads * p.rows, 256);
 }
 
 }  // namespace
@@ -417,15 +424,18 @@ int small_cache_attention(const small_cache *c, const small_attn *a, const float
     x.scale = a->scale; x.cap = a->cap;
     x.causal = 1; x.width = 1; x.reach = a->reach; x.buckets = a->buckets;
     x.lengths = a->lengths; x.first = a->first; x.slopes = a->slopes; x.table = a->table; x.bucket = a->bucket;
-    x.pack = 1; x.head_sets = a->kv_heads; x.rows = p.rows; x.row_tiles = p.row_tiles; x.splits = p.splits;
+    x.pack = 1; x.head_sets = a->kv_heads; x.rows = p.rows; x.row_tiles = p.row_tiles;
     x.by_Cb = make_fastdiv(a->Cb); x.by_Sq = make_fastdiv(a->Sq); x.by_width = make_fastdiv(1); x.by_group = make_fastdiv(x.group);
-    x.by_tiles = make_fastdiv(p.row_tiles); x.by_sets = make_fastdiv(a->kv_heads); x.by_splits = make_fastdiv(p.splits);
+    x.by_sets = make_fastdiv(a->kv_heads);
     x.part_o = (float *)workspace;
     x.part_ml = (float2 *)((char *)workspace + p.ml_at);
-    const hipStream_t s = (hipStream_t)stream;
-    hipError_t e = launch_cache_token(x, cache_args(*c), quads(a->D, a->Cb, {&a->q, &a->out}, {q, out}), s);
-    if (e == hipSuccess && p.splits > 1) e = launch_attn_join(x, s);
-    return from_hip(e);
+    x.vec = quads(a->D, a->Cb, {&a->q, &a->out}, {q, out});
+    CacheArgs held_args = cache_args(*c);
+    held_args.workgroups = p.workgroups;
+    held_args.least_rounds = kLeastRounds;
+    held_args.units = p.joined ? (int2 *)((char *)workspace + p.units_at) : nullptr;
+    held_args.by_rows = make_fastdiv(p.rows);
+    return from_hip(launch_cache_token(x, held_args, p.joined, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -124,23 +124,36 @@ __global__ void __launch_bounds__(1024) cache_write(StoreArgs a)
     QuadTurns<HALVES> turns;
     int turns_of = -1;
     const int i = max(0, min(at.i, a.S - 1));
-    const float *const qt = q_items ? token_at(a.r.q, a.r.qs, at.n, i) : nullptr, *const kt = token_at(a.k, a.ks, at.n, i), *const vt = token_at(a.v, a.vs, at.n, i);
-    const auto fetch = [&](int item) {
-        const bool is_q = item < q_items, is_k = item < q_items + a.c.kv_heads;
-        const int head = is_q ? item : is_k ? item - q_items : item - q_items - a.c.kv_heads;
-        return quad_of<VEC>(a.r.by_Cb, D, is_q ? a.r.qs : is_k ? a.ks : a.vs, is_q ? qt : is_k ? kt : vt, head * D, at.d);
+    // An item's tensor, by its values: a choice between the arguments' own places would put them all into scratch memory.
+    struct Source { const float *token; TokenStrides s; int head; bool is_q, is_k; };
+    const auto source = [&](int item) {
+        Source x;
+        x.is_q = item < q_items;
+        x.is_k = !x.is_q && item < q_items + a.c.kv_heads;
+        x.head = x.is_q ? item : x.is_k ? item - q_items : item - q_items - a.c.kv_heads;
+        x.s.image = x.is_q ? a.r.qs.image : x.is_k ? a.ks.image : a.vs.image;
+        x.s.block = x.is_q ? a.r.qs.block : x.is_k ? a.ks.block : a.vs.block;
+        x.s.token = x.is_q ? a.r.qs.token : x.is_k ? a.ks.token : a.vs.token;
+        x.token = token_at(x.is_q ? a.r.q : x.is_k ? a.k : a.v, x.s, at.n, i);
+        return x;
     };
-    floatx4 next = fetch(lo_item);
+    const auto fetch = [&](const Source &x) { return quad_of<VEC>(a.r.by_Cb, D, x.s, x.token, x.head * D, at.d); };
+    Source coming = source(lo_item);
+    floatx4 next = fetch(coming);
     for (int item = lo_item; item < hi_item; ++item) {
         floatx4 x = next;
-        if (item + 1 < hi_item) next = fetch(item + 1);
-        const bool is_q = item < q_items, is_k = !is_q && item < q_items + a.c.kv_heads;
-        const int head = is_q ? item : is_k ? item - q_items : item - q_items - a.c.kv_heads;
+        const Source now = coming;
+        if (item + 1 < hi_item) {
+            coming = source(item + 1);
+            next = fetch(coming);
+        }
+        const bool is_q = now.is_q, is_k = now.is_k;
+        const int head = now.head;
         if (a.turns && (is_q || is_k) && at.d < 2 * a.r.pairs) {
             const int f = a.r.freq_heads == 1 ? 0 : is_q ? a.by_per_q.div(head) : head;
             if (f != turns_of) turns.set(a.r, place, f, at.d);
             turns_of = f;
-            x = turns.template turned<VEC>(a.r, is_q ? a.r.qs : a.ks, is_q ? qt : kt, head * D, at.d, x);
+            x = turns.template turned<VEC>(a.r, now.s, now.token, head * D, at.d, x);
         }
         if (is_q) {
             if (token) put_quad<VEC>(a.r.by_Cb, D, a.r.qos, const_cast<float *>(token_at(a.r.qo, a.r.qos, at.n, i)), head * D, at.d, x);

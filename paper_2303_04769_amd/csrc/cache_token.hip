@@ -11,6 +11,8 @@
 #include "attn_tile.h"
 #include "cache.h"
 
+#include <initializer_list>
+
 namespace small {
 
 namespace {
@@ -26,10 +28,11 @@ __device__ __forceinline__ floatx4 mfma_bf16(uintx4 a, uintx4 b, floatx4 c)
 }
 // The upper halves of two words.
 __device__ __forceinline__ unsigned upper(unsigned lo, unsigned hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
-// Eight codes as bfloat16 numbers.
+// Eight codes as bfloat16 numbers. (Taken apart here: behind the load, where the compiler would do it, it is a wait for the load, and four registers for every one.)
 __device__ __forceinline__ uintx4 widened(unsigned lo, unsigned hi)
 {
     uintx4 r;
+    asm volatile("" : "+v"(lo), "+v"(hi));
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const unsigned w = i < 2 ? lo : hi, at = 16 * (i & 1);
@@ -37,13 +40,13 @@ __device__ __forceinline__ uintx4 widened(unsigned lo, unsigned hi)
     }
     return r;
 }
-// Eight floats in three parts of eight bits each, cut off, not rounded: their sum is the float.
-struct Parts3 { uintx4 p[3]; };
-__device__ __forceinline__ Parts3 parts_of(const float (&x)[8])
+// Four floats in three parts of eight bits each, cut off, not rounded: their sum is the float.
+struct Parts3 { unsigned p[3][2]; };
+__device__ __forceinline__ Parts3 parts_of(floatx4 x)
 {
     Parts3 r;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
         unsigned h[2], m[2], l[2];
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
@@ -59,6 +62,11 @@ __device__ __forceinline__ Parts3 parts_of(const float (&x)[8])
     }
     return r;
 }
+__device__ __forceinline__ uintx4 words(const unsigned (&lo)[2], const unsigned (&hi)[2]) { return uintx4{lo[0], lo[1], hi[0], hi[1]}; }
+
+// What stands so many bytes behind a place that all lanes share: below 2^32, so that an address takes one register.
+template <typename T>
+__device__ __forceinline__ T at_bytes(const T *base, unsigned bytes) { return *reinterpret_cast<const T *>(reinterpret_cast<const char *>(base) + bytes); }
 
 // One row by one wave, key by key, for rows whose sums came out as NaN: in a product of tiles a key of weight zero contributes 0 * v, which is NaN where a token that
 // the row does not see holds an infinite or NaN value. Slow, and reached only by caches that hold such values.
@@ -113,73 +121,226 @@ __device__ void attend_cached_row(const AttnArgs &a, const CacheArgs &c, const R
     sum = total;
 }
 
-template <int KIND, int DT, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) cache_token(AttnArgs a, CacheArgs c)
+// The kernel's second argument likewise (late_args).
+__device__ __forceinline__ CacheArgs late_cache_args()
+{
+    static_assert(sizeof(AttnArgs) % 8 == 0 && alignof(CacheArgs) <= 8, "one behind the other");
+    auto at = (const __attribute__((address_space(4))) unsigned *)__builtin_amdgcn_kernarg_segment_ptr() + sizeof(AttnArgs) / 4;
+    asm volatile("" : "+s"(at));
+    unsigned words[sizeof(CacheArgs) / 4];
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(CacheArgs) / 4; ++i) words[i] = at[i];
+    return __builtin_bit_cast(CacheArgs, words);
+}
+
+// Waves a SIMD that the registers are to leave room for, and waves of a workgroup: as many workgroups run at a time.
+constexpr int least_waves(int kind, int DT, int SP)
+{
+    return kind == SMALL_CACHE_I8 ? (DT <= 4 && SP == 4 ? 3 : DT <= 5 || (DT <= 8 && SP > 1) ? 2 : 1) : DT <= 1 ? 5 : DT <= 3 ? 4 : DT == 4 ? 3 : DT <= 8 ? 2 : 1;
+}
+constexpr int group_waves(int DT) { return DT > 8 ? 2 : 4; }      // (their results fit 64 KB of LDS together)
+
+// Who does what: a round is a tile for each wave of a workgroup, a stream's tokens are R rounds (one at least) of each tile of rows of each key head, and the rounds
+// of all streams one behind the other are shared out evenly: streams differ in length, workgroups do not (64 streams of 2048 to 16384 tokens, 8 bits, in equal parts of each
+// stream: 86 us; in pieces of equal length: 93; evenly: 75). Known only on the device, where each workgroup sums up the lengths.
+struct Rounds {
+    int *prefix;                  // LDS: rounds in front of each of the chunk's streams; their sum, [threads]; the waves' sums, 4; what was found
+    int threads, units, all = 0, chunk = 0, before = 0, workgroups, each, more;
+    __device__ __forceinline__ static int of(const AttnArgs &a, int n, int keys) { return max(1, (max(0, min(a.lengths[n], a.Sk)) + keys - 1) / keys); }
+    // Sums of the streams from `first` on, a thread each.
+    __device__ __forceinline__ int scan(const AttnArgs &a, int first, int keys)
+    {
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));                         // (or what only this needs is computed once and kept in registers throughout)
+        const int lane = tid & 63, wave = tid >> 6, n = first + tid;
+        const int mine = n < a.N ? of(a, n, keys) * units : 0;
+        int sum = mine;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int below = __shfl_up(sum, d);
+            sum += lane >= d ? below : 0;
+        }
+        __syncthreads();
+        if (lane == 63) prefix[threads + 1 + wave] = sum;
+        __syncthreads();
+        int total = 0, under = 0;
+        for (int w = 0; w < threads >> 6; ++w) {
+            const int x = prefix[threads + 1 + w];
+            under += w < wave ? x : 0;
+            total += x;
+        }
+        prefix[tid] = under + sum - mine;
+        if (tid == 0) prefix[threads] = total;
+        __syncthreads();
+        return __builtin_amdgcn_readfirstlane(total);
+    }
+    __device__ __forceinline__ Rounds(const AttnArgs &a, const CacheArgs &c, int keys, int *lds) : prefix(lds), threads(blockDim.x), units(a.head_sets * a.row_tiles)
+    {
+        for (int n = 0; n < a.N; n += threads) all += scan(a, n, keys);
+        workgroups = max(1, min(c.workgroups, all / c.least_rounds));
+        each = all / workgroups;
+        more = all - each * workgroups;                       // the first so many have one more
+    }
+    __device__ __forceinline__ int begin(int w) const { return w * each + min(w, more); }
+    __device__ __forceinline__ int owner(int x) const
+    {
+        const int longer = more * (each + 1);
+        return x < longer ? x / (each + 1) : more + (x - longer) / each;
+    }
+    // The stream that has round x, and the first round of its first unit.
+    __device__ __forceinline__ int stream(const AttnArgs &a, int keys, int x, int *start)
+    {
+        if (a.N > threads) {
+            if (x < before) { chunk = 0; before = 0; }
+            int here = scan(a, chunk, keys);
+            while (x >= before + here) {
+                before += here;
+                chunk += threads;
+                here = scan(a, chunk, keys);
+            }
+        }
+        const int y = x - before;
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        if (prefix[tid] <= y && y < prefix[tid + 1]) prefix[threads + 5] = tid;
+        __syncthreads();
+        const int found = __builtin_amdgcn_readfirstlane(prefix[threads + 5]);
+        *start = before + __builtin_amdgcn_readfirstlane(prefix[found]);
+        return chunk + found;
+    }
+};
+constexpr int rounds_ints(int threads) { return threads + 6; }
+
+// SP: into how many columns a row's keys of a tile are shared out, where there are at most 16 / SP rows. Column m then has row m mod (16 / SP), and of the tile's results only
+// those of its share, m / (16 / SP): as if it were a row of its own, with a maximum, a sum and a result of its own, joined as those of the waves are. So the 16 columns
+// of single tokens' products are not mostly empty lanes in all that lies between the products.
+template <int KIND, int DT, int SP, bool ONE>
+__global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_waves_per_eu(least_waves(KIND, DT, SP)))) cache_token(AttnArgs args, CacheArgs cache_args)
 {
     constexpr int B = cache_bytes(KIND), E = 16 / B, NB = E / 4, KT = 4 * E, NS = (16 * DT + KT - 1) / KT, DP = 16 * DT, H = E / 8 > 0 ? E / 8 : 1;
-    const int wave = threadIdx.x >> 6, waves = blockDim.x >> 6, lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
-    const unsigned id = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int by_split = a.by_splits.div((int)id), split = (int)id - by_split * a.splits;
-    const int by_tile = a.by_tiles.div(by_split), r0 = 16 * (by_split - by_tile * a.row_tiles);
-    const int n = a.by_sets.div(by_tile), key_head = by_tile - n * a.head_sets, rows = min(16, a.rows - r0);
-    const int r = r0 + min(m, rows - 1), hh = a.by_Sq.div(r), i = r - hh * a.Sq, head = key_head * a.group + hh;
+    constexpr int NV = NB / SP, R = 16 / SP;                   // results of a lane that count, rows
+    constexpr int waves = group_waves(DT), KR = waves * KT;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    __shared__ int rounds_lds[rounds_ints(64 * waves)];
+    Rounds rounds(args, cache_args, KR, rounds_lds);
+    // (neighbours on one XCD: they have the tiles of rows that read the same keys)
+    const int w_id = (int)xcd_contiguous(blockIdx.x, gridDim.x);
+    if (w_id >= rounds.workgroups) return;
+    int stream_start = 0, stream_rounds = 0, of_unit = 1, n = 0;
+    for (int round = rounds.begin(w_id), stop = rounds.begin(w_id + 1); round < stop;) {
+    const AttnArgs a = late_args();                            // (anew for every unit: what the compiler would compute of them once and keep does not fit the registers)
+    const CacheArgs c = late_cache_args();
+    int lane = threadIdx.x & 63;
+    asm volatile("" : "+v"(lane));
+    const int tid = 64 * wave + lane, m = lane & 15, g = lane >> 4;
+    if (round >= stream_start + stream_rounds) {
+        n = rounds.stream(a, KR, round, &stream_start);
+        of_unit = __builtin_amdgcn_readfirstlane(Rounds::of(a, n, KR));
+        stream_rounds = of_unit * rounds.units;
+    }
+    const int unit = (round - stream_start) / of_unit, lo_round = round - stream_start - unit * of_unit, hi_round = min(of_unit, lo_round + stop - round);
+    const int key_head = unit / a.row_tiles, tile = unit - key_head * a.row_tiles;
+    const bool whole = lo_round == 0 && hi_round == of_unit;
+    round += hi_round - lo_round;
+    const int r0 = R * tile, rows = min(R, a.rows - r0), share = m / R;
+    const int r = r0 + min(m % R, rows - 1), hh = a.by_Sq.div(r), i = r - hh * a.Sq, head = key_head * a.group + hh;
     ImageMask im(a, n);
-    if (!a.first) im.first = im.len - a.Sq;
+    im.len = __builtin_amdgcn_readfirstlane(im.len);           // (the same for all lanes, which only scalar loads would tell the compiler: what follows from them is scalar)
+    im.prefix = 0;
+    im.first = a.first ? __builtin_amdgcn_readfirstlane(im.first) : im.len - a.Sq;
     const RowState row(a, im, n, i, head);
-    // keys up to the last one that a row of the tile can see, this workgroup's share of them in whole tiles
+    // keys up to the last one that a row of the tile can see, of these rounds
     const int last = a.by_Sq.div(r0) == a.by_Sq.div(r0 + rows - 1) ? r0 + rows - 1 - a.by_Sq.div(r0) * a.Sq : a.Sq - 1;
     const int hi = max(0, min(im.len, im.position(last) + 1));
-    const int per = ((hi + KT - 1) / KT + a.splits - 1) / a.splits * KT, begin = min(hi, split * per), end = min(hi, begin + per);
-
+    const int begin = min(hi, lo_round * KR), end = min(hi, hi_round * KR);
     const int step = waves * KT, first = begin + wave * KT;
     int left = first < end ? (end - first + step - 1) / step : 0;
     const int stride = a.slopes ? -step : step;
     int j0 = first + (a.slopes ? (left - 1) * step : 0);
 
     uintx4 kx[NB][NS], vx[DT];
-    floatx4 ksc[NB], vsc[NB];                                  // scales of codes
-    // Pages of a lane's keys and of its values' keys: of tile j0, -1 where there is none.
-    int k_page, v_page, k_next = -1, v_next = -1;
-    const auto pages_at = [&](int j, int &kp, int &vp) {
-        kp = page_of(c, n, min(j + E * (m >> 2), end - 1));    // (a chunk behind the last key: its page; its keys are hidden)
-        vp = page_of(c, n, min(j + E * g, end - 1));
+    floatx4 ksc[NV], vsc[NV];                                  // scales of codes, of the keys of a lane's share
+    // Pages of a lane's keys and of its values' keys: of tile j0, -1 where there is none. Their numbers come by scalar loads: these have a counter of their own, so that waiting
+    // for them is not waiting for all keys and values asked for before. ONE: pages hold whole tiles, so that a tile's place is the same for all lanes, and a lane's offset
+    // from it the same for all tiles; else a tile is in up to four pages.
+    constexpr int NP = KT / 16;
+    const auto *const table = (const __attribute__((address_space(4))) int *)(c.table + (size_t)n * c.per_stream);
+    const int k_in = E * (m >> 2) >> c.shift, v_in = E * g >> c.shift, last_page = (end - 1) >> c.shift;
+    int k_page = -1, v_page = -1, page0 = -1, page1 = -1, page2 = -1, page3 = -1;
+    const auto ask_pages = [&](int j) {
+        const int at = j >> c.shift;
+        page0 = table[min(at, last_page)];
+        if constexpr (!ONE && NP > 1) page1 = table[min(at + 1, last_page)];
+        if constexpr (!ONE && NP > 2) {
+            page2 = table[min(at + 2, last_page)];
+            page3 = table[min(at + 3, last_page)];
+        }
     };
+    const auto page_in = [&](int in) {
+        int page = page0;
+        if constexpr (!ONE && NP > 1) page = in == 1 ? page1 : page;
+        if constexpr (!ONE && NP > 2) page = in == 2 ? page2 : in == 3 ? page3 : page;
+        return (unsigned)page < (unsigned)c.pages ? page : -1;
+    };
+    const auto at_lane = [](const void *base, unsigned bytes) { return *reinterpret_cast<const uintx4 *>(static_cast<const char *>(base) + bytes); };
     const auto fetch_k = [&](int j) {
-        const int chunk = min(j + E * (m >> 2), (end - 1) & -E), place = chunk & ((1 << c.shift) - 1);
-        const size_t at = place_at(c, max(0, k_page), key_head, place + (m & 3));
+        if constexpr (ONE) {
+            const size_t at = place_at(c, max(0, v_page), key_head, j & ((1 << c.shift) - 1));
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int s = 0; s < NS; ++s) kx[b][s] = *reinterpret_cast<const uintx4 *>(c.keys + ((at + 4 * b) * c.Dk + min(E * g + KT * s, c.Dk - E)) * B);
-        if constexpr (KIND == SMALL_CACHE_I8) {
-            const int vplace = min(j + E * g, (end - 1) & -E) & ((1 << c.shift) - 1);
-            const float *from = c.key_scales + place_at(c, max(0, v_page), key_head, vplace);
+                for (int s = 0; s < NS; ++s)
+                    kx[b][s] = at_lane(c.keys + (at + 4 * b) * (size_t)(c.Dk * B), (unsigned)(((E * (m >> 2) + (m & 3)) * c.Dk + min(E * g + KT * s, c.Dk - E)) * B));
+            if constexpr (KIND == SMALL_CACHE_I8) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) ksc[b] = *reinterpret_cast<const floatx4 *>(from + 4 * b);
+                for (int b = 0; b < NV; ++b) ksc[b] = __builtin_bit_cast(floatx4, at_lane(c.key_scales + at, 4u * (unsigned)(E * g + 4 * (share * NV + b))));
+            }
+        } else {
+            const int chunk = min(j + E * (m >> 2), (end - 1) & -E), place = chunk & ((1 << c.shift) - 1);
+            const size_t at = place_at(c, max(0, k_page), key_head, place + (m & 3));
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int s = 0; s < NS; ++s) kx[b][s] = *reinterpret_cast<const uintx4 *>(c.keys + ((at + 4 * b) * c.Dk + min(E * g + KT * s, c.Dk - E)) * B);
+            if constexpr (KIND == SMALL_CACHE_I8) {
+                const int vplace = min(j + E * g, (end - 1) & -E) & ((1 << c.shift) - 1);
+                const float *from = c.key_scales + place_at(c, max(0, v_page), key_head, vplace);
+#pragma unroll
+                for (int b = 0; b < NV; ++b) ksc[b] = *reinterpret_cast<const floatx4 *>(from + 4 * (share * NV + b));
+            }
         }
     };
     const auto fetch_v = [&](int j) {
-        const int place = min(j + E * g, (end - 1) & -E) & ((1 << c.shift) - 1);
+        const int place = (ONE ? j : min(j + E * g, (end - 1) & -E)) & ((1 << c.shift) - 1);
         const size_t page_row = place_at(c, max(0, v_page), key_head, 0);
         const char *from = c.values + (page_row * c.D + place) * B;
+        if constexpr (ONE) {
 #pragma unroll
-        for (int d = 0; d < DT; ++d) vx[d] = *reinterpret_cast<const uintx4 *>(from + ((size_t)min(16 * d + m, c.D - 1) << c.shift) * B);
+            for (int d = 0; d < DT; ++d) vx[d] = at_lane(from, (unsigned)(((min(16 * d + m, c.D - 1) << c.shift) + E * g) * B));
+        } else {
+#pragma unroll
+            for (int d = 0; d < DT; ++d) vx[d] = *reinterpret_cast<const uintx4 *>(from + ((size_t)min(16 * d + m, c.D - 1) << c.shift) * B);
+        }
         if constexpr (KIND == SMALL_CACHE_I8) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b) vsc[b] = *reinterpret_cast<const floatx4 *>(c.value_scales + page_row + place + 4 * b);
+            for (int b = 0; b < NV; ++b)
+                vsc[b] = ONE ? __builtin_bit_cast(floatx4, at_lane(c.value_scales + page_row + place, 4u * (unsigned)(E * g + 4 * (share * NV + b))))
+                             : *reinterpret_cast<const floatx4 *>(c.value_scales + page_row + place + 4 * (share * NV + b));
         }
     };
     if (left) {
-        pages_at(j0, k_page, v_page);
+        ask_pages(j0);
+        k_page = page_in(k_in);
+        v_page = page_in(v_in);
         fetch_k(j0);
         fetch_v(j0);
     }
-    // queries: floats, or their parts
+    // queries, times what makes their products scores (or, with a cap, what the tanh is taken of): floats, or their parts
     floatx4 qf[KIND == SMALL_CACHE_F32 ? DT : 1];
-    Parts3 qp[KIND == SMALL_CACHE_F32 ? 1 : NS * H];
+    Parts3 qp[KIND == SMALL_CACHE_F32 ? 1 : 2 * NS * H];
     {
         const float *token = token_at(a.q, a.qs, n, i);
-        const auto quad = [&](int d) { return a.vec ? load_quad<true>(a, a.qs, token, head * a.D, d) : load_quad<false>(a, a.qs, token, head * a.D, d); };
+        const float in = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
+        const auto quad = [&](int d) { return (a.vec ? load_quad<true>(a, a.qs, token, head * a.D, d) : load_quad<false>(a, a.qs, token, head * a.D, d)) * in; };
         if constexpr (KIND == SMALL_CACHE_F32) {
 #pragma unroll
             for (int s = 0; s < DT; ++s) qf[s] = quad(16 * s + 4 * g);
@@ -187,111 +348,115 @@ __global__ void __launch_bounds__(64 * WAVES) cache_token(AttnArgs a, CacheArgs 
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int h = 0; h < H; ++h) {
-                    float x[8];
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const floatx4 f = quad(KT * s + E * g + 8 * h + 4 * e);
-#pragma unroll
-                        for (int y = 0; y < 4; ++y) x[4 * e + y] = f[y];
-                    }
-                    qp[s * H + h] = parts_of(x);
-                }
+                for (int h = 0; h < 2 * H; ++h) qp[2 * H * s + h] = parts_of(quad(KT * s + E * g + 4 * h));
         }
     }
     const float far_lo = a.table ? bias_gather(a, head, 0) : 0.f, far_hi = a.table ? bias_gather(a, head, 2 * a.reach) : 0.f;
     floatx4 o[DT] = {};
     Reference top(a, row, begin, end);
     float sum = 0.f;
-    if (left > 1) pages_at(j0 + stride, k_next, v_next);
+    if (left > 1) ask_pages(j0 + stride);
     for (; left; --left, j0 += stride) {
-        const int key0 = j0 + E * g;                           // of this lane's scores: key0 + 4 b + e
+        const int value0 = j0 + E * g, key0 = value0 + 4 * NV * share;        // of this lane's values, and of its scores: key0 + 4 b + e
         const bool no_page = v_page < 0;
         // a learned bias: all buckets are asked for, then all biases -- unless the tile's keys are all at one end of the reach, as most of a long cache is
         bool near = false;
-        float far = 0.f, bias[NB][4];
+        float far = 0.f, bias[NV][4];
         if (a.table) {
             const bool all_lo = __all(j0 + KT - 1 - row.code <= -a.reach), all_hi = __all(j0 - row.code >= a.reach);
             near = !all_lo && !all_hi;
             far = all_lo ? far_lo : all_hi ? far_hi : 0.f;
             if (near) {
-                int bucket[NB][4];
+                int bucket[NV][4];
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int b = 0; b < NV; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) bucket[b][e] = a.bucket[offset_at(a, key0 + 4 * b + e, row.code)];
+                    for (int e = 0; e < 4; ++e) bucket[b][e] = at_bytes(a.bucket, 4u * (unsigned)offset_at(a, key0 + 4 * b + e, row.code));
 #pragma unroll
-                for (int b = 0; b < NB; ++b)
+                for (int b = 0; b < NV; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) bias[b][e] = a.table[(size_t)head * a.buckets + max(0, min(bucket[b][e], a.buckets - 1))];
+                    for (int e = 0; e < 4; ++e) bias[b][e] = at_bytes(a.table, 4u * (unsigned)(head * a.buckets + max(0, min(bucket[b][e], a.buckets - 1))));
             }
         }
-        floatx4 s[NB] = {};
+        floatx4 all[NB] = {};
 #pragma unroll
         for (int x = 0; x < NS; ++x)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if constexpr (KIND == SMALL_CACHE_F32) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) s[b] = mfma(__uint_as_float(kx[b][x][e]), qf[x][e], s[b]);
-                } else if constexpr (KIND == SMALL_CACHE_BF16) {
-#pragma unroll
-                    for (int p = 2; p >= 0; --p) s[b] = mfma_bf16(kx[b][x], qp[x].p[p], s[b]);
+                    for (int e = 0; e < 4; ++e) all[b] = mfma(__uint_as_float(kx[b][x][e]), qf[x][e], all[b]);
                 } else {
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uintx4 k = widened(kx[b][x][2 * h], kx[b][x][2 * h + 1]);
+                    for (int h = 0; h < H; ++h) {
+                        uintx4 k = kx[b][x];
+                        if constexpr (KIND == SMALL_CACHE_I8) k = widened(kx[b][x][2 * h], kx[b][x][2 * h + 1]);
+                        const Parts3 &q0 = qp[2 * (H * x + h)], &q1 = qp[2 * (H * x + h) + 1];
 #pragma unroll
-                        for (int p = 2; p >= 0; --p) s[b] = mfma_bf16(k, qp[2 * x + h].p[p], s[b]);
+                        for (int p = 2; p >= 0; --p) all[b] = mfma_bf16(k, words(q0.p[p], q1.p[p]), all[b]);
                     }
                 }
             }
-        if constexpr (KIND == SMALL_CACHE_I8) {
+        floatx4 s[NV];
 #pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] *= ksc[b];
+        for (int b = 0; b < NV; ++b) {
+            s[b] = all[b];
+#pragma unroll
+            for (int x = 1; x < SP; ++x) s[b] = share == x ? all[x * NV + b] : s[b];
+            if constexpr (KIND == SMALL_CACHE_I8) s[b] *= ksc[b];
         }
         if (left > 1) {
             const int v_now = v_page;
-            k_page = k_next; v_page = v_next;                  // (v_page too: key scales stand at the values' keys)
+            k_page = page_in(k_in);
+            v_page = page_in(v_in);                            // (key scales stand at the values' keys)
             fetch_k(j0 + stride);
             v_page = v_now;
         }
         const float base = far - top.at;
-        float in = a.scale * kLog2e;
         if (a.cap > 0.f) {
-#pragma unroll
-            for (int b = 0; b < NB; ++b) s[b] *= a.scale / a.cap;
             tanh_all(s);
-            in = a.cap * kLog2e;
+            const float out = a.cap * kLog2e;
+#pragma unroll
+            for (int b = 0; b < NV; ++b) s[b] *= out;
         }
+        if (a.slopes) {
+            const float from = (float)(row.p - key0);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NV; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) s[b][e] = fmaf(s[b][e], in, a.slopes ? fmaf(-row.slope, fabsf((float)(row.p - (key0 + 4 * b + e))), base) : base);
+                for (int e = 0; e < 4; ++e) s[b][e] += fmaf(-row.slope, fabsf(from - (float)(4 * b + e)), base);
+        } else {
+#pragma unroll
+            for (int b = 0; b < NV; ++b) s[b] += base;
+        }
         if (near)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NV; ++b)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[b][e] += bias_log2(bias[b][e]);
         const int bound = min(row.bound, end);
         if (!__all((j0 + KT <= bound) & !no_page)) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
+            for (int b = 0; b < NV; ++b)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] = ((key0 + 4 * b + e < bound) & !no_page) ? s[b][e] : -kInf;
+                for (int e = 0; e < 4; ++e) {
+                    const bool seen = (key0 + 4 * b + e < bound) & !no_page;
+                    s[b][e] = seen ? s[b][e] : -kInf;
+                    if constexpr (KIND == SMALL_CACHE_I8) vsc[b][e] = seen ? vsc[b][e] : 0.f;              // (the scale of a hidden token may be anything)
+                }
         }
         if (KIND != SMALL_CACHE_I8 && (j0 + KT > end || __any(no_page))) {       // what stands behind the last key, or in no page of the stream's, becomes zeros
 #pragma unroll
             for (int d = 0; d < DT; ++d)
 #pragma unroll
                 for (int x = 0; x < 4; ++x) {
-                    if constexpr (KIND == SMALL_CACHE_F32) vx[d][x] = ((key0 + x < end) & !no_page) ? vx[d][x] : 0u;
-                    else vx[d][x] &= no_page ? 0u : key0 + 2 * x + 1 < end ? 0xffffffffu : key0 + 2 * x < end ? 0xffffu : 0u;
+                    if constexpr (KIND == SMALL_CACHE_F32) vx[d][x] = ((value0 + x < end) & !no_page) ? vx[d][x] : 0u;
+                    else vx[d][x] &= no_page ? 0u : value0 + 2 * x + 1 < end ? 0xffffffffu : value0 + 2 * x < end ? 0xffffu : 0u;
                 }
         }
         raise_top(s, top, sum, o);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NV; ++b)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
@@ -303,129 +468,206 @@ __global__ void __launch_bounds__(64 * WAVES) cache_token(AttnArgs a, CacheArgs 
 #pragma unroll
                 for (int d = 0; d < DT; ++d) o[d] = mfma(__uint_as_float(vx[d][e]), s[0][e], o[d]);
         } else {
+            Parts3 w[NV];
+#pragma unroll
+            for (int b = 0; b < NV; ++b) {
+                if constexpr (KIND == SMALL_CACHE_I8) s[b] *= vsc[b];
+                w[b] = parts_of(s[b]);
+            }
 #pragma unroll
             for (int h = 0; h < H; ++h) {
-                float w[8];
+                uintx4 p[3];                                   // (zeros at the other shares' keys)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float p = s[2 * h + e / 4][e & 3];
-                    if constexpr (KIND == SMALL_CACHE_I8) w[e] = p == 0.f ? 0.f : p * vsc[2 * h + e / 4][e & 3];      // (the scale of a hidden token may be anything)
-                    else w[e] = p;
-                }
-                const Parts3 p = parts_of(w);
+                for (int x = 0; x < 3; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        const int b = 2 * h + y / 2;
+                        p[x][y] = SP == 1 || share == b / NV ? w[b % NV].p[x][y & 1] : 0u;
+                    }
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    uintx4 v;
+                    uintx4 v = vx[d];
                     if constexpr (KIND == SMALL_CACHE_I8) v = widened(vx[d][2 * h], vx[d][2 * h + 1]);
-                    else v = vx[d];
 #pragma unroll
-                    for (int x = 2; x >= 0; --x) o[d] = mfma_bf16(v, p.p[x], o[d]);
+                    for (int x = 2; x >= 0; --x) o[d] = mfma_bf16(v, p[x], o[d]);
                 }
             }
         }
         if (left > 1) {
-            v_page = v_next;
+            v_page = page_in(v_in);
             fetch_v(j0 + stride);
-            if (left > 2) pages_at(j0 + 2 * stride, k_next, v_next);
+            if (left > 2) ask_pages(j0 + 2 * stride);
         }
     }
     sum = column_sum(sum);
 
-    // join the waves: [wave][row][DP] and [wave][row] (maximum, sum)
+    // join the waves' shares: [wave][share][row][DP] and [wave][share][row] (maximum, sum)
+    const AttnArgs z = late_args();
+    const CacheArgs zc = late_cache_args();
+    const size_t all_units = (size_t)n * rounds.units + unit, part = (w_id + all_units) * R;       // (workgroups and units both only grow: a place of its own for each pair)
+    if (zc.units && lo_round == 0 && tid == 0) zc.units[all_units] = int2{w_id, rounds.owner(round - (hi_round - lo_round) + of_unit - 1)};      // who has parts of it, for the join
     float *const lo_ = token_lds;
-    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * rows * DP);
-    int *const flags = reinterpret_cast<int *>(ml + waves * rows);
-    if (m < rows) {
+    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * SP * rows * DP);
+    int *const flags = reinterpret_cast<int *>(ml + waves * SP * rows);
+    if (m % R < rows) {
+        const int mine = (wave * SP + share) * rows + m % R;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + (wave * rows + m) * DP + 16 * d + 4 * g) = o[d];
-        if (g == 0) ml[wave * rows + m] = float2{top.maximum(), sum};
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + mine * DP + 16 * d + 4 * g) = o[d];
+        if (g == 0) ml[mine] = float2{top.maximum(), sum};
     }
-    if (threadIdx.x < 16) flags[threadIdx.x] = 0;
+    if (tid < 16) flags[tid] = 0;
     __syncthreads();
     constexpr int QD = DP / 4;
-    for (int e = threadIdx.x; e < rows * QD; e += blockDim.x) {
+    for (int e = tid; e < rows * QD; e += 64 * waves) {
         const int rr = e / QD, d = (e - rr * QD) * 4;
         float all = -kInf, total = 0.f;
 #pragma unroll 4
-        for (int w = 0; w < waves; ++w) all = fmaxf(all, ml[w * rows + rr].x);
+        for (int w = 0; w < waves * SP; ++w) all = fmaxf(all, ml[w * rows + rr].x);
         const float ref = all == -kInf ? 0.f : all;
         floatx4 y = {};
 #pragma unroll 4
-        for (int w = 0; w < waves; ++w) {
+        for (int w = 0; w < waves * SP; ++w) {
             const float2 p = ml[w * rows + rr];
-            const floatx4 z = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * DP + d);
+            const floatx4 w4 = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * DP + d);
             const float f = __builtin_amdgcn_exp2f(p.x - ref);
             total += p.y == 0.f ? 0.f : f * p.y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * z[x];       // (a wave that saw no key)
+            for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * w4[x];       // (a share that saw no key)
         }
-        if (d < a.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = 1;
-        const int h2 = a.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * a.Sq, head2 = key_head * a.group + h2;
-        const size_t part = (((size_t)n * a.head_sets + key_head) * a.rows + r0 + rr) * a.splits + split;
-        if (a.splits > 1) {
+        if (d < z.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = 1;
+        const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
+        if (!whole) {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
-                if (d + x < a.D) a.part_o[part * a.D + d + x] = y[x];
-            if (d == 0) a.part_ml[part] = float2{all, total};
+                if (d + x < z.D) z.part_o[(part + rr) * z.D + d + x] = y[x];
+            if (d == 0) z.part_ml[part + rr] = float2{all, total};
         } else {
-            const floatx4 z = total == 0.f ? floatx4{} : y * (1.f / total);
-            float *token = const_cast<float *>(token_at(a.o, a.os, n, i2));
-            if (a.vec) store_quad<true>(a, a.os, token, head2 * a.D, d, z);
-            else store_quad<false>(a, a.os, token, head2 * a.D, d, z);
-            if (a.lse && d == 0) a.lse[((size_t)n * a.heads + head2) * a.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
+            const floatx4 all_of = total == 0.f ? floatx4{} : y * (1.f / total);
+            float *token = const_cast<float *>(token_at(z.o, z.os, n, i2));
+            if (z.vec) store_quad<true>(z, z.os, token, head2 * z.D, d, all_of);
+            else store_quad<false>(z, z.os, token, head2 * z.D, d, all_of);
+            if (z.lse && d == 0) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
         }
     }
     __syncthreads();
     for (int rr = wave; rr < rows; rr += waves) {
         if (!flags[rr]) continue;
-        const int h2 = a.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * a.Sq, head2 = key_head * a.group + h2;
-        const RowState again(a, im, n, i2, head2);
+        const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
+        const RowState again(z, im, n, i2, head2);
         float y[4], most, total;
-        attend_cached_row<KIND>(a, c, again, n, i2, key_head, begin, end, y, most, total);
-        const size_t part = (((size_t)n * a.head_sets + key_head) * a.rows + r0 + rr) * a.splits + split;
+        attend_cached_row<KIND>(z, zc, again, n, i2, key_head, begin, end, y, most, total);
         const float inv = total == 0.f ? 0.f : 1.f / total;
         for (int x = 0; x < 4; ++x) {
             const int d = lane + 64 * x;
-            if (d >= a.D) continue;
-            if (a.splits > 1) a.part_o[part * a.D + d] = y[x];
-            else const_cast<float *>(token_at(a.o, a.os, n, i2))[channel_at(a, a.os, head2 * a.D + d)] = total == 0.f ? 0.f : y[x] * inv;
+            if (d >= z.D) continue;
+            if (!whole) z.part_o[(part + rr) * z.D + d] = y[x];
+            else const_cast<float *>(token_at(z.o, z.os, n, i2))[channel_at(z, z.os, head2 * z.D + d)] = total == 0.f ? 0.f : y[x] * inv;
         }
         if (lane) continue;
-        if (a.splits > 1) a.part_ml[part] = float2{most, total};
-        else if (a.lse) a.lse[((size_t)n * a.heads + head2) * a.Sq + i2] = total == 0.f ? -kInf : (most + __builtin_amdgcn_logf(total)) * kLn2;
+        if (!whole) z.part_ml[part + rr] = float2{most, total};
+        else if (z.lse) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (most + __builtin_amdgcn_logf(total)) * kLn2;
+    }    __syncthreads();                                           // (what the join read is free)
     }
 }
 
-template <int KIND>
-hipError_t token_kind(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
+// Rows whose rounds more than one workgroup had: their parts joined, a workgroup for each row. (Who had them stands in the workspace: summing up the lengths again took it
+// 7.0 us instead of 5.9, 64 streams of 16 heads.)
+__global__ void __launch_bounds__(256) cache_token_join(AttnArgs a, CacheArgs c, int most_rows)
 {
-    const unsigned grid = (unsigned)((long)a.N * a.head_sets * a.row_tiles * a.splits);
-    const int rows = a.rows < 16 ? a.rows : 16, keys = 64 / cache_bytes(KIND);
-    // waves of a workgroup: as many as have a tile to do each, as far as their results fit 64 KB of LDS together
-#define TOKEN(dt, most) \
-    if (a.D <= 16 * dt) { \
-        const int need = ((a.Sk + keys - 1) / keys + a.splits - 1) / a.splits; \
-        int w = 1; \
-        while (w < most && w < need && 2 * w * rows * (16 * dt + 2) * 4 + 64 <= 65536) w *= 2; \
-        hipLaunchKernelGGL((cache_token<KIND, dt, most>), dim3(grid), dim3(64 * w), (size_t)w * rows * (16 * dt + 2) * 4 + 64, s, a, c); \
-        return hipGetLastError(); \
+    __shared__ float sums[4][256], all[4];
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int by_head = c.by_rows.div((int)blockIdx.x), r = (int)blockIdx.x - by_head * a.rows, n = a.by_sets.div(by_head), key_head = by_head - n * a.head_sets;
+    const int tile = r / most_rows;
+    const size_t unit = (size_t)by_head * a.row_tiles + tile;
+    const int from = c.units[unit].x, to = c.units[unit].y;
+    if (from == to) return;
+    const size_t step = most_rows, first = (from + unit) * most_rows + (r - tile * most_rows);
+    float top = -kInf, sum = 0.f, o[4] = {};
+#pragma unroll 4
+    for (int s = lane; s <= to - from; s += 64) top = fmaxf(top, a.part_ml[first + s * step].x);
+    for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float ref = top == -kInf ? 0.f : top;
+#pragma unroll 4
+    for (int s = wave; s <= to - from; s += 4) {
+        const float2 w = a.part_ml[first + s * step];
+        const float x = w.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.x - ref);      // (a part that saw no key)
+        sum = fmaf(x, w.y, sum);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (lane + 64 * k < a.D) {
+                const float y = a.part_o[(first + s * step) * a.D + lane + 64 * k];
+                o[k] += w.y == 0.f ? 0.f : x * y;
+            }
     }
-    TOKEN(1, 8) TOKEN(2, 8) TOKEN(3, 8) TOKEN(4, 8) TOKEN(5, 8) TOKEN(6, 8) TOKEN(8, 8) TOKEN(16, 4)
+#pragma unroll
+    for (int k = 0; k < 4; ++k) sums[wave][lane + 64 * k] = o[k];
+    if (lane == 0) all[wave] = sum;
+    __syncthreads();
+    const int d = threadIdx.x;
+    sum = (all[0] + all[1]) + (all[2] + all[3]);
+    const int hh = a.by_Sq.div(r), i = r - hh * a.Sq, head = key_head * a.group + hh;
+    if (d < a.D) {
+        const float y = (sums[0][d] + sums[1][d]) + (sums[2][d] + sums[3][d]);
+        const_cast<float *>(token_at(a.o, a.os, n, i))[channel_at(a, a.os, head * a.D + d)] = sum == 0.f ? 0.f : y * (1.f / sum);
+    }
+    if (a.lse && d == 0) a.lse[((size_t)n * a.heads + head) * a.Sq + i] = sum == 0.f ? -kInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// Rows of a tile: as many as leave each a column of its own, or fewer that share the columns out.
+constexpr int token_shares(int kind, int rows)
+{
+    return kind == SMALL_CACHE_I8 ? (rows <= 4 ? 4 : rows <= 8 ? 2 : 1) : kind == SMALL_CACHE_BF16 && rows <= 8 ? 2 : 1;
+}
+int token_tiles(int D)
+{
+    for (const int dt : {1, 2, 3, 4, 5, 6, 8})
+        if (D <= 16 * dt) return dt;
+    return 16;
+}
+
+template <int KIND, int SP, bool ONE>
+hipError_t token_form(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
+{
+    const int rows = a.rows < 16 / SP ? a.rows : 16 / SP;
+    switch (token_tiles(a.D)) {
+#define TOKEN(dt) \
+    case dt: \
+        hipLaunchKernelGGL((cache_token<KIND, dt, SP, ONE>), dim3((unsigned)c.workgroups), dim3(64 * group_waves(dt)), (size_t)group_waves(dt) * SP * rows * (16 * dt + 2) * 4 + 64, s, a, c); \
+        break;
+        TOKEN(1) TOKEN(2) TOKEN(3) TOKEN(4) TOKEN(5) TOKEN(6) TOKEN(8) TOKEN(16)
 #undef TOKEN
-    return hipErrorInvalidValue;
+    }
+    return hipGetLastError();
+}
+template <int KIND, int SP>
+hipError_t token_pages(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
+{
+    if constexpr (KIND != SMALL_CACHE_F32)
+        if ((1 << c.shift) < 64 / cache_bytes(KIND)) return token_form<KIND, SP, false>(a, c, s);
+    return token_form<KIND, SP, true>(a, c, s);
 }
 
 }  // namespace
 
-hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool vec, hipStream_t s)
+TokenShape token_shape(int kind, int D, int rows)
 {
-    AttnArgs x = a;
-    x.vec = vec;
+    const int shares = token_shares(kind, rows), dt = token_tiles(D), waves = group_waves(dt);
+    return TokenShape{16 / shares, waves * 64 / cache_bytes(kind), least_waves(kind, dt, shares) * 4 / waves};
+}
+
+hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool joined, hipStream_t s)
+{
+    const int shares = token_shares(c.kind, a.rows);
+    hipError_t e;
     switch (c.kind) {
-    case SMALL_CACHE_F32: return token_kind<SMALL_CACHE_F32>(x, c, s);
-    case SMALL_CACHE_BF16: return token_kind<SMALL_CACHE_BF16>(x, c, s);
-    default: return token_kind<SMALL_CACHE_I8>(x, c, s);
+    case SMALL_CACHE_F32: e = token_pages<SMALL_CACHE_F32, 1>(a, c, s); break;
+    case SMALL_CACHE_BF16: e = shares == 2 ? token_pages<SMALL_CACHE_BF16, 2>(a, c, s) : token_pages<SMALL_CACHE_BF16, 1>(a, c, s); break;
+    default: e = shares == 4 ? token_pages<SMALL_CACHE_I8, 4>(a, c, s) : shares == 2 ? token_pages<SMALL_CACHE_I8, 2>(a, c, s) : token_pages<SMALL_CACHE_I8, 1>(a, c, s);
     }
+    if (e != hipSuccess || !joined) return e;
+    const TokenShape shape = token_shape(c.kind, a.D, a.rows);
+    hipLaunchKernelGGL(cache_token_join, dim3((unsigned)((long)a.N * a.head_sets * a.rows)), dim3(256), 0, s, a, c, shape.rows);
+    return hipGetLastError();
 }
 
 }  // namespace small

@@ -1,4 +1,4 @@
-// The single-layer calls of binding.py, and the calls of attn.py, from Python, without ctypes: a call of a few microseconds on the GPU is bound by its
+// The single-layer calls of binding.py, and the calls of attn.py and cache.py, from Python, without ctypes: a call of a few microseconds on the GPU is bound by its
 // host time, and of that the launch itself takes 3.0 us; attribute reads, argument conversion and the foreign-function
 // interface took another 1.6 (ReLU) to 3 (convolution), here some 0.4.
 //
@@ -12,23 +12,26 @@
 #include <c10/hip/HIPStream.h>
 
 #include <dlfcn.h>
+#include <limits.h>
 #include <stddef.h>
 #include <string.h>
 
 #include <initializer_list>
 
 #include "../../include/small.h"
-#include "../include/small_attn.h"
+#include "../include/small_cache.h"
 
 namespace {
 
 PyTypeObject *quant_type = nullptr;        // binding.small_quant
 PyTypeObject *attn_type = nullptr;         // attn.small_attn
+PyTypeObject *rotation_type = nullptr, *cache_type = nullptr;      // cache.small_rotation, cache.small_cache
 
 #define SMALL_FUNCTIONS(X)                                                                                                        \
     X(small_pack) X(small_unpack) X(small_conv2d) X(small_dwconv2d) X(small_pool2d) X(small_relu) X(small_add) X(small_dense)     \
     X(small_pack_u8) X(small_unpack_u8) X(small_conv2d_u8) X(small_dwconv2d_u8) X(small_dense_u8) X(small_pool2d_u8) X(small_relu_u8) \
-    X(small_groupnorm) X(small_groupnorm_grad) X(small_attention) X(small_attention_grad)
+    X(small_groupnorm) X(small_groupnorm_grad) X(small_attention) X(small_attention_grad)                                         \
+    X(small_rotary) X(small_rotary_grad) X(small_cache_write) X(small_cache_read) X(small_cache_attention)
 struct Library {
 #define X(f) decltype(&::f) f = nullptr;
     SMALL_FUNCTIONS(X)
@@ -120,22 +123,76 @@ struct Reader {
         memcpy(&r, quant.buf, sizeof r);
         return r;
     }
-    // An activation [N][blocks][S][Cb] that may be a view, of at least `channels` channels.
-    float *view(int k, const small_attn &r, int S, long channels, small_tokens *strides)
+    // A record of a plan of cache.py, copied.
+    template <typename T>
+    T record(int k, PyTypeObject *type)
     {
-        if (!plain || error) return nullptr;
+        T r = {};
+        Py_buffer b = {};
+        if (!plain) return r;
+        if (!type || Py_TYPE(a[k]) != type || PyObject_GetBuffer(a[k], &b, PyBUF_SIMPLE) != 0) {
+            PyErr_Clear();
+            plain = false;
+            return r;
+        }
+        if (b.len == (Py_ssize_t)sizeof r) memcpy(&r, b.buf, sizeof r);
+        else plain = false;
+        PyBuffer_Release(&b);
+        return r;
+    }
+    // An activation [N][blocks][S][Cb] that may be a view, of at least `channels` channels.
+    float *view(int k, const small_attn &r, int S, long channels, small_tokens *strides) { return view(k, r.N, S, r.Cb, channels, strides); }
+    float *view(int k, long N, long S, long Cb, long channels, small_tokens *strides, bool optional = false)
+    {
+        if (!plain || error || (optional && a[k] == Py_None)) return nullptr;
         if (!THPVariable_CheckExact(a[k])) {
             plain = false;
             return nullptr;
         }
         const at::Tensor &t = THPVariable_Unpack(a[k]);
-        if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 4 || t.size(0) != r.N || t.size(2) != S || t.size(3) != r.Cb ||
-            (r.Cb > 1 && t.stride(3) != 1) || t.size(1) * r.Cb < channels) {
+        if (!t.is_cuda() || t.scalar_type() != at::kFloat || t.dim() != 4 || t.size(0) != N || t.size(2) != S || t.size(3) != Cb ||
+            (Cb > 1 && t.stride(3) != 1) || t.size(1) * Cb < channels) {
             plain = false;                               // (the binding says what is wrong with it)
             return nullptr;
         }
         *strides = small_tokens{(size_t)t.stride(0), (size_t)t.stride(1), (size_t)t.stride(2)};
         return static_cast<float *>(t.data_ptr());
+    }
+    // Sizes [N][..][S][Cb] of an activation.
+    bool sizes(int k, int *N, int *S, int *Cb)
+    {
+        if (plain && !THPVariable_CheckExact(a[k])) plain = false;
+        if (!plain || error) return false;
+        const at::Tensor &t = THPVariable_Unpack(a[k]);
+        if (t.dim() != 4 || t.size(0) > INT_MAX || t.size(2) > INT_MAX || t.size(3) > INT_MAX) return plain = false;
+        *N = (int)t.size(0);
+        *S = (int)t.size(2);
+        *Cb = (int)t.size(3);
+        return true;
+    }
+    // A table of pages [N][..], with its place in the cache's record.
+    void pages(int k, int N, small_cache &c)
+    {
+        if (plain && !THPVariable_CheckExact(a[k])) plain = false;
+        if (!plain || error) return;
+        const at::Tensor &t = THPVariable_Unpack(a[k]);
+        if (!t.is_cuda() || t.scalar_type() != at::kInt || !t.is_contiguous() || t.dim() != 2 || t.size(0) != N || t.size(1) > INT_MAX) {
+            plain = false;
+            return;
+        }
+        c.N = N;
+        c.per_stream = (int)t.size(1);
+        c.table = static_cast<const int *>(t.data_ptr());
+    }
+    // A rotation's frequencies and places, from arguments k and k + 1.
+    void places(int k, small_rotation &r)
+    {
+        r.freq = of<float>(k, at::kFloat, {r.freq_heads, r.axes, r.pairs});
+        r.positions = of<int>(k + 1, at::kInt, {r.N, r.S, r.axes});
+        if (a[k] == Py_None) plain = false;
+        if (!r.positions)
+            for (int x = 1; x < r.axes && x < 4; ++x)
+                if (r.extent[x] < 1) plain = false;
     }
     // A contiguous tensor of these sizes, or null for None.
     template <typename T>
@@ -292,6 +349,74 @@ ENTRY(attention_grad, 20, small_attn rec = r.record(0); const long cq = (long)re
       auto *dt = r.of<float>(10, at::kFloat, {rec.heads, rec.buckets});
       return r.call([&](void *s) { return lib.small_attention_grad(&rec, q, k, v, o, l, d, dq, dk, dv, dt, ws, size, s); });)
 
+// (record, q, k, freq, positions, first, q_out, k_out, stream): q_out, k_out None: in place
+ENTRY(rotary, 9, small_rotation rec = r.record<small_rotation>(0, rotation_type); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
+      r.places(3, rec); rec.first = r.of<int>(5, at::kInt, {rec.N});
+      auto *q = r.view(1, rec.N, rec.S, rec.Cb, cq, &rec.q, true); auto *k = r.view(2, rec.N, rec.S, rec.Cb, ck, &rec.k, true);
+      auto *qo = r.view(args[6] == Py_None ? 1 : 6, rec.N, rec.S, rec.Cb, cq, &rec.q_out, true);
+      auto *ko = r.view(args[7] == Py_None ? 2 : 7, rec.N, rec.S, rec.Cb, ck, &rec.k_out, true);
+      return r.call([&](void *s) { return lib.small_rotary(&rec, q, k, qo, ko, s); });)
+// (record, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, workspace, stream)
+ENTRY(rotary_grad, 13, small_rotation rec = r.record<small_rotation>(0, rotation_type); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
+      size_t size; void *ws = r.bytes(11, &size);
+      r.places(3, rec); rec.first = r.of<int>(5, at::kInt, {rec.N});
+      auto *dqo = r.view(1, rec.N, rec.S, rec.Cb, cq, &rec.q_out, true); auto *dko = r.view(2, rec.N, rec.S, rec.Cb, ck, &rec.k_out, true);
+      auto *dq = r.view(args[6] == Py_None ? 1 : 6, rec.N, rec.S, rec.Cb, cq, &rec.dq, true);
+      auto *dk = r.view(args[7] == Py_None ? 2 : 7, rec.N, rec.S, rec.Cb, ck, &rec.dk, true);
+      auto *q = r.view(8, rec.N, rec.S, rec.Cb, cq, &rec.q, true); auto *k = r.view(9, rec.N, rec.S, rec.Cb, ck, &rec.k, true);
+      auto *df = r.of<float>(10, at::kFloat, {rec.freq_heads, rec.axes, rec.pairs});
+      return r.call([&](void *s) { return lib.small_rotary_grad(&rec, dqo, dko, q, k, dq, dk, df, ws, size, s); });)
+// (cache, k, v, pages, first, counts, rotation or None, freq, positions, q, q_out, stream)
+ENTRY(cache_write, 12, small_cache c = r.record<small_cache>(0, cache_type); small_span sp = {}; int N = 0;
+      r.sizes(1, &N, &sp.S, &sp.Cb); r.pages(3, N, c);
+      sp.first = r.of<int>(4, at::kInt, {N}); sp.counts = r.of<int>(5, at::kInt, {N});
+      const long ck = (long)c.kv_heads * c.D; const bool turn = r.plain && args[6] != Py_None;
+      auto *k = r.view(1, N, sp.S, sp.Cb, ck, &sp.k); auto *v = r.view(2, N, sp.S, sp.Cb, ck, &sp.v);
+      small_rotation rec = {}; float *q = nullptr, *qo = nullptr;
+      if (turn) {
+          rec = r.record<small_rotation>(6, rotation_type);
+          r.places(7, rec);
+          rec.first = nullptr;
+          rec.k = rec.k_out = small_tokens{};
+          q = r.view(9, rec.N, rec.S, rec.Cb, (long)rec.heads * rec.D, &rec.q, true);
+          qo = r.view(args[10] == Py_None ? 9 : 10, rec.N, rec.S, rec.Cb, (long)rec.heads * rec.D, &rec.q_out, true);
+      } else if (r.plain && args[9] != Py_None) {
+          r.plain = false;
+      }
+      return r.call([&](void *s) { return lib.small_cache_write(&c, &sp, k, v, turn ? &rec : nullptr, q, qo, s); });)
+// (cache, k, v, pages, first, counts, stream)
+ENTRY(cache_read, 7, small_cache c = r.record<small_cache>(0, cache_type); small_span sp = {}; int N = 0;
+      r.sizes(1, &N, &sp.S, &sp.Cb); r.pages(3, N, c);
+      sp.first = r.of<int>(4, at::kInt, {N}); sp.counts = r.of<int>(5, at::kInt, {N});
+      const long ck = (long)c.kv_heads * c.D;
+      auto *k = r.view(1, N, sp.S, sp.Cb, ck, &sp.k); auto *v = r.view(2, N, sp.S, sp.Cb, ck, &sp.v);
+      return r.call([&](void *s) { return lib.small_cache_read(&c, &sp, k, v, s); });)
+// (cache, record, q, out, lse, workspace, pages, lengths, first, slopes, table, bucket, stream)
+ENTRY(cache_attention, 13, small_cache c = r.record<small_cache>(0, cache_type); small_attn rec = r.record<small_attn>(1, attn_type); const long cq = (long)rec.heads * rec.D;
+      size_t size; void *ws = r.bytes(5, &size);
+      r.pages(6, rec.N, c);
+      if (r.plain && (long)c.per_stream * c.page != rec.Sk) r.plain = false;
+      rec.lengths = r.of<int>(7, at::kInt, {rec.N}); rec.first = r.of<int>(8, at::kInt, {rec.N}); rec.slopes = r.of<float>(9, at::kFloat, {rec.heads});
+      rec.table = r.of<float>(10, at::kFloat, {rec.heads, rec.buckets}); rec.bucket = r.of<int>(11, at::kInt, {2L * rec.reach + 1});
+      rec.prefix = rec.docs = nullptr;
+      auto *q = r.view(2, rec, rec.Sq, cq, &rec.q); auto *o = r.view(3, rec, rec.Sq, cq, &rec.out);
+      auto *l = r.of<float>(4, at::kFloat, {rec.N, rec.heads, rec.Sq});
+      return r.call([&](void *s) { return lib.small_cache_attention(&c, &rec, q, o, l, ws, size, s); });)
+
+// bind_cache(cache's small_rotation and small_cache)
+PyObject *bind_cache(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 2 || !PyType_Check(args[0]) || !PyType_Check(args[1])) {
+        PyErr_SetString(PyExc_TypeError, "bind_cache(small_rotation, small_cache)");
+        return nullptr;
+    }
+    Py_INCREF(args[0]);                    // (kept for the module's life)
+    Py_INCREF(args[1]);
+    rotation_type = reinterpret_cast<PyTypeObject *>(args[0]);
+    cache_type = reinterpret_cast<PyTypeObject *>(args[1]);
+    Py_RETURN_NONE;
+}
+
 // bind_attention(attn's small_attn)
 PyObject *bind_attention(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
@@ -331,7 +456,8 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n)
 PyMethodDef methods[] = {METHOD(bind), METHOD(pack), METHOD(unpack), METHOD(pack_u8), METHOD(unpack_u8), METHOD(conv2d), METHOD(conv2d_u8),
                          METHOD(dwconv2d), METHOD(dwconv2d_u8), METHOD(pool2d), METHOD(pool2d_u8), METHOD(relu), METHOD(relu_u8), METHOD(add),
                          METHOD(dense), METHOD(dense_u8), METHOD(groupnorm), METHOD(groupnorm_grad), METHOD(attention), METHOD(attention_grad),
-                         METHOD(bind_attention), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(bind_attention), METHOD(rotary), METHOD(rotary_grad), METHOD(cache_write), METHOD(cache_read), METHOD(cache_attention),
+                         METHOD(bind_cache), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
