@@ -47,6 +47,8 @@ struct StoreArgs {
     const float *k, *v;
     float *k_out, *v_out;                    // read
     TokenStrides ks, vs;
+    int fast;                                // RotaryArgs' FAST, of these tensors
+    long long q_step, qo_step, k_step, v_step;
     int turns, N, S, lanes_log2, tile, tiles, items, parts;      // tile: tokens of a workgroup, 16 or 1
     const int *first, *counts;
     FastDiv by_parts, by_tiles, by_per_q, by_per_k;              // by_per: heads of one set of frequencies

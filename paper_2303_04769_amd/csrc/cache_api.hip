@@ -131,11 +131,19 @@ void place(RotaryArgs &x, const TurnPlan &p, bool grad)
 {
     x.run = p.run; x.runs = p.units / p.run; x.parts = p.parts; x.chunks = p.chunks; x.per_chunk = p.per_chunk;
     x.by_run = make_fastdiv(p.run); x.by_runs = make_fastdiv(x.runs); x.by_parts = make_fastdiv(p.parts); x.by_chunks = make_fastdiv(p.chunks);
-    x.turn_threads = grad ? 0u : (unsigned)((double)x.N * x.S * p.units * x.freq_heads * p.parts);
+    x.turn_threads = grad ? 0u : (unsigned)((double)x.N * x.S * p.units);          // (for every set of heads)
+    x.by_sets = make_fastdiv(x.freq_heads * p.parts);
     const int copied = (x.q && x.q != x.qo ? x.heads : 0) + (x.k && x.k != x.ko ? x.kv_heads : 0);
     x.copy_run = p.copy_run; x.copy_runs = p.copies ? p.copies / p.copy_run : 1;
     x.by_copy_run = make_fastdiv(p.copy_run); x.by_copy_runs = make_fastdiv(x.copy_runs); x.by_copy_heads = make_fastdiv(copied ? copied : 1);
     x.copy_threads = (unsigned)((double)x.N * x.S * p.copies * copied);
+}
+
+// Floats from a head to the next, if they are the same from each to the next and the tensor is small enough for offsets of 32 bits in bytes; else 0.
+long long head_step(const Laid &t, int heads, int D)
+{
+    if (t.floats() >= (size_t)1 << 30) return 0;
+    return D % t.Cb == 0 ? (long long)(D / t.Cb * t.s.block) : (size_t)heads * D <= t.Cb ? D : 0;
 }
 
 // The rotation's own inputs, which nothing that is written may meet.
@@ -184,6 +192,15 @@ int rotary(const small_rotation &r, const float *q, const float *k, float *q_out
     x.qs = strides(qs); x.ks = strides(ks); x.qos = strides(qos); x.kos = strides(kos);
     x.yq = yq; x.yk = yk; x.yqs = strides(r.q); x.yks = strides(r.k);
     x.partial = (double *)workspace;
+    x.fast = vec;
+    const auto step = [&](const Laid &t, int heads) {
+        const long long floats = t.p ? head_step(t, heads, r.D) : 0;
+        if (t.p && !floats) x.fast = 0;
+        return floats;
+    };
+    x.q_step = step(in[0], r.heads); x.k_step = step(in[1], r.kv_heads);
+    x.qo_step = step(out[0], r.heads); x.ko_step = step(out[1], r.kv_heads);
+    x.yq_step = step(saved[0], r.heads); x.yk_step = step(saved[1], r.kv_heads);
     if (back) x.sign = -1.f;
     place(x, p, dfreq != nullptr);
     return from_hip(dfreq ? launch_rotary_grad(x, vec, r.halves != 0, dfreq, stream) : launch_rotary(x, vec, r.halves != 0, stream));
@@ -362,6 +379,13 @@ int small_cache_write(const small_cache *c, const small_span *s, const float *k,
         if (q) vec = vec && quads(c->D, s->Cb, {&r->q, &r->q_out}, {q, q_out});
         x.by_per_q = make_fastdiv(r->heads / r->freq_heads);
     }
+    x.k_step = head_step(in[0], c->kv_heads, c->D); x.v_step = head_step(in[1], c->kv_heads, c->D);
+    x.fast = vec && x.k_step && x.v_step;
+    if (q) {
+        x.q_step = head_step(laid(c->N, s->S, r->heads, c->D, s->Cb, q, r->q), r->heads, c->D);
+        x.qo_step = head_step(laid(c->N, s->S, r->heads, c->D, s->Cb, q_out, r->q_out), r->heads, c->D);
+        x.fast = x.fast && x.q_step && x.qo_step;
+    }
     return from_hip(launch_cache_write(x, vec, r && r->halves, (hipStream_t)stream));
 }
 
@@ -384,7 +408,10 @@ int small_cache_read(const small_cache *c, const small_span *s, float *k, float 
     if (const int rc = plan_store(x, *c, *s, 0, true)) return rc;
     x.k_out = k; x.v_out = v;
     x.ks = strides(s->k); x.vs = strides(s->v);
-    return from_hip(launch_cache_read(x, quads(c->D, s->Cb, {&s->k, &s->v}, {k, v}), (hipStream_t)stream));
+    const bool vec = quads(c->D, s->Cb, {&s->k, &s->v}, {k, v});
+    x.k_step = head_step(out[0], c->kv_heads, c->D); x.v_step = head_step(out[1], c->kv_heads, c->D);
+    x.fast = vec && x.k_step && x.v_step;
+    return from_hip(launch_cache_read(x, vec, (hipStream_t)stream));
 }
 
 int small_cache_attention_workspace(const small_cache *c, const small_attn *a, size_t *bytes)

@@ -44,6 +44,37 @@ struct Pairs {
             token[channel_of(a.by_Cb, s, c0 + (HALVES ? a.pairs + u : 2 * u + 1))] = x[1];
         }
     }
+    // FAST: two offsets of a lane in a tensor (the second with HALVES), and quads at them from a head's place on
+    struct Offsets {
+        unsigned at[HALVES ? 2 : 1];
+        __device__ __forceinline__ Offsets(const RotaryArgs &a, const TokenStrides &s, int n, int i, int u)
+        {
+            const long long token = n * s.image + i * s.token;
+            at[0] = 4u * (unsigned)(token + channel_of(a.by_Cb, s, 4 * u));
+            if constexpr (HALVES) at[1] = 4u * (unsigned)(token + channel_of(a.by_Cb, s, a.pairs + 4 * u));
+        }
+    };
+    __device__ __forceinline__ void load_at(const float *head, const Offsets &o)
+    {
+        if constexpr (VEC && HALVES) {
+            const floatx4 p = quad_at(head, o.at[0]), q = quad_at(head, o.at[1]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { x[2 * i] = p[i]; x[2 * i + 1] = q[i]; }
+        } else if constexpr (VEC) {
+            const floatx4 p = quad_at(head, o.at[0]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = p[i];
+        }
+    }
+    __device__ __forceinline__ void store_at(float *head, const Offsets &o) const
+    {
+        if constexpr (VEC && HALVES) {
+            put_quad_at(head, o.at[0], floatx4{x[0], x[2], x[4], x[6]});
+            put_quad_at(head, o.at[1], floatx4{x[1], x[3], x[5], x[7]});
+        } else if constexpr (VEC) {
+            put_quad_at(head, o.at[0], floatx4{x[0], x[1], x[2], x[3]});
+        }
+    }
     __device__ __forceinline__ void turn(const Turn (&t)[kCount])
     {
 #pragma unroll
@@ -89,51 +120,69 @@ __device__ __forceinline__ void copy_rest(const RotaryArgs &a, unsigned idx)
     else *to = *from;
 }
 
-template <bool VEC, bool HALVES>
+// A workgroup has one set of heads (part of those of one set of frequencies), a thread a unit of a token.
+template <bool VEC, bool HALVES, bool FAST>
 __global__ void __launch_bounds__(256) rotary_turn(RotaryArgs a)
 {
     using Unit = Pairs<VEC, HALVES>;
-    const unsigned idx = blockIdx.x * 256u + threadIdx.x;
-    const unsigned turning = (a.turn_threads + 255u) & ~255u;
-    if (idx >= turning) return copy_rest<VEC>(a, idx - turning);
+    constexpr int G = HALVES ? 4 : 8;                                // heads at a time
+    const unsigned sets = (unsigned)(a.freq_heads * a.parts), turning = (a.turn_threads + 255u) / 256u * sets;
+    if (blockIdx.x >= turning) return copy_rest<VEC>(a, (blockIdx.x - turning) * 256u + threadIdx.x);
+    const int group = a.by_sets.div((int)blockIdx.x), set = (int)blockIdx.x - group * (int)sets, f = a.by_parts.div(set), part = set - f * a.parts;
+    const unsigned idx = (unsigned)group * 256u + threadIdx.x;
     if (idx >= a.turn_threads) return;
     int rest = a.by_run.div((int)idx);
     const int uq = (int)idx - rest * a.run, above = a.by_S.div(rest), i = rest - above * a.S;
-    rest = a.by_runs.div(above);
-    const int u = (above - rest * a.runs) * a.run + uq, by_part = a.by_parts.div(rest), part = rest - by_part * a.parts;
-    const int n = a.by_freq_heads.div(by_part), f = by_part - n * a.freq_heads;
-    int place[4];
-    place_of(a, n, i, a.first ? a.first[n] : 0, place);
-    Turn t[Unit::kCount];
-#pragma unroll
-    for (int p = 0; p < Unit::kCount; ++p) t[p] = turn_of(a, place, f, Unit::kCount * u + p);
+    const int n = a.by_runs.div(above), u = (above - n * a.runs) * a.run + uq;
     const Heads heads(a, f, part);
-    for (int j0 = heads.lo; j0 < heads.hi; j0 += 4) {
-        Unit x[4];
+    int place[4];
+    Turn t[Unit::kCount];
+    const auto turns = [&] {
+        place_of(a, n, i, a.first ? a.first[n] : 0, place);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int j = min(j0 + b, heads.hi - 1);
-            const bool is_q = heads.is_q(j);
-            x[b].load(a, is_q ? a.qs : a.ks, token_at(is_q ? a.q : a.k, is_q ? a.qs : a.ks, n, i), heads.head(j) * a.D, u);
-        }
+        for (int p = 0; p < Unit::kCount; ++p) t[p] = turn_of(a, place, f, Unit::kCount * u + p);
+    };
+    bool turned = false;
+    // queries, then keys
 #pragma unroll
-        for (int b = 0; b < 4; ++b) {
-            const int j = j0 + b;
-            if (j >= heads.hi) break;
-            const bool is_q = heads.is_q(j);
-            x[b].turn(t);
-            x[b].store(a, is_q ? a.qos : a.kos, const_cast<float *>(token_at(is_q ? a.qo : a.ko, is_q ? a.qos : a.kos, n, i)), heads.head(j) * a.D, u);
+    for (int tensor = 0; tensor < 2; ++tensor) {
+        const int lo = tensor ? max(heads.lo, heads.per_q) : heads.lo, hi = tensor ? heads.hi : min(heads.hi, heads.per_q);
+        if (lo >= hi) continue;
+        const float *const from = tensor ? a.k : a.q;
+        float *const to = tensor ? a.ko : a.qo;
+        const TokenStrides &fs = tensor ? a.ks : a.qs, &ts = tensor ? a.kos : a.qos;
+        const typename Unit::Offsets fo(a, fs, n, i, u), so(a, ts, n, i, u);
+        const float *const token = token_at(from, fs, n, i);
+        float *const token_out = const_cast<float *>(token_at(to, ts, n, i));
+        for (int j0 = lo; j0 < hi; j0 += G) {
+            Unit x[G];
+#pragma unroll
+            for (int b = 0; b < G; ++b) {
+                const int h = heads.head(min(j0 + b, hi - 1));
+                if constexpr (FAST) x[b].load_at(from + h * (tensor ? a.k_step : a.q_step), fo);
+                else x[b].load(a, fs, token, h * a.D, u);
+            }
+            if (!turned) turns();                                    // (the first loads are on their way)
+            turned = true;
+#pragma unroll
+            for (int b = 0; b < G; ++b) {
+                if (j0 + b >= hi) break;
+                const int h = heads.head(j0 + b);
+                x[b].turn(t);
+                if constexpr (FAST) x[b].store_at(to + h * (tensor ? a.ko_step : a.qo_step), so);
+                else x[b].store(a, ts, token_out, h * a.D, u);
+            }
         }
     }
 }
 
 // The turn back, with the sums over a chunk of tokens for the frequencies' gradient. A workgroup has one run of units of one set of frequencies; run is a power of two.
-template <bool VEC, bool HALVES>
+template <bool VEC, bool HALVES, bool FAST>
 __global__ void __launch_bounds__(256) rotary_grad(RotaryArgs a)
 {
     using Unit = Pairs<VEC, HALVES>;
-    constexpr int P = Unit::kCount;
-    __shared__ double sums[4][64];
+    constexpr int P = Unit::kCount, G = HALVES ? 2 : 4;
+    __shared__ double sums[4][4 * P][64];
     const unsigned summing = (unsigned)(a.freq_heads * a.parts * a.runs * a.chunks);
     if (blockIdx.x >= summing) return copy_rest<VEC>(a, (blockIdx.x - summing) * 256u + threadIdx.x);
     const int rest = a.by_chunks.div((int)blockIdx.x);
@@ -146,39 +195,58 @@ __global__ void __launch_bounds__(256) rotary_grad(RotaryArgs a)
     for (int at = chunk * a.per_chunk + (int)threadIdx.x / a.run; at < end; at += tokens) {
         const int n = a.by_S.div(at), i = at - n * a.S;
         int place[4];
-        place_of(a, n, i, a.first ? a.first[n] : 0, place);
         Turn t[P];
-#pragma unroll
-        for (int p = 0; p < P; ++p) t[p] = turn_of(a, place, f, P * u + p);
         double g[P] = {};
-        for (int j0 = heads.lo; j0 < heads.hi; j0 += 2) {
-            Unit x[2], y[2];
+        bool turned = false;
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int j = min(j0 + b, heads.hi - 1), c0 = heads.head(j) * a.D;
-                const bool is_q = heads.is_q(j);
-                x[b].load(a, is_q ? a.qs : a.ks, token_at(is_q ? a.q : a.k, is_q ? a.qs : a.ks, n, i), c0, u);
-                y[b].load(a, is_q ? a.yqs : a.yks, token_at(is_q ? a.yq : a.yk, is_q ? a.yqs : a.yks, n, i), c0, u);
-            }
+        for (int tensor = 0; tensor < 2; ++tensor) {
+            const int lo = tensor ? max(heads.lo, heads.per_q) : heads.lo, hi = tensor ? heads.hi : min(heads.hi, heads.per_q);
+            if (lo >= hi) continue;
+            const float *const from = tensor ? a.k : a.q, *const saved = tensor ? a.yk : a.yq;
+            float *const to = tensor ? a.ko : a.qo;
+            const TokenStrides &fs = tensor ? a.ks : a.qs, &ts = tensor ? a.kos : a.qos, &ss = tensor ? a.yks : a.yqs;
+            const typename Unit::Offsets fo(a, fs, n, i, u), to_at(a, ts, n, i, u), so(a, ss, n, i, u);
+            const float *const token = token_at(from, fs, n, i), *const token_saved = token_at(saved, ss, n, i);
+            float *const token_out = const_cast<float *>(token_at(to, ts, n, i));
+            for (int j0 = lo; j0 < hi; j0 += G) {
+                Unit x[G], y[G];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
-                const int j = j0 + b;
-                if (j >= heads.hi) break;
-                const bool is_q = heads.is_q(j);
+                for (int b = 0; b < G; ++b) {
+                    const int h = heads.head(min(j0 + b, hi - 1));
+                    if constexpr (FAST) {
+                        x[b].load_at(from + h * (tensor ? a.k_step : a.q_step), fo);
+                        y[b].load_at(saved + h * (tensor ? a.yk_step : a.yq_step), so);
+                    } else {
+                        x[b].load(a, fs, token, h * a.D, u);
+                        y[b].load(a, ss, token_saved, h * a.D, u);
+                    }
+                }
+                if (!turned) {
+                    place_of(a, n, i, a.first ? a.first[n] : 0, place);
 #pragma unroll
-                for (int p = 0; p < P; ++p)
-                    g[p] += __builtin_fma((double)x[b].x[2 * p + 1], (double)y[b].x[2 * p], -((double)x[b].x[2 * p] * (double)y[b].x[2 * p + 1]));
-                x[b].turn(t);
-                x[b].store(a, is_q ? a.qos : a.kos, const_cast<float *>(token_at(is_q ? a.qo : a.ko, is_q ? a.qos : a.kos, n, i)), heads.head(j) * a.D, u);
+                    for (int p = 0; p < P; ++p) t[p] = turn_of(a, place, f, P * u + p);
+                    turned = true;
+                }
+#pragma unroll
+                for (int b = 0; b < G; ++b) {
+                    if (j0 + b >= hi) break;
+                    const int h = heads.head(j0 + b);
+#pragma unroll
+                    for (int p = 0; p < P; ++p)
+                        g[p] += __builtin_fma((double)x[b].x[2 * p + 1], (double)y[b].x[2 * p], -((double)x[b].x[2 * p] * (double)y[b].x[2 * p + 1]));
+                    x[b].turn(t);
+                    if constexpr (FAST) x[b].store_at(to + h * (tensor ? a.ko_step : a.qo_step), to_at);
+                    else x[b].store(a, ts, token_out, h * a.D, u);
+                }
             }
         }
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-            for (int x = 0; x < 4; ++x) acc[p][x] = __builtin_fma((double)place[x], g[p], acc[p][x]);
+            for (int x4 = 0; x4 < 4; ++x4) acc[p][x4] = __builtin_fma((double)place[x4], g[p], acc[p][x4]);
     }
+    // the lanes of a unit, the four waves
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const size_t row = ((size_t)f * a.chunks + chunk) * a.parts + part;
 #pragma unroll
     for (int p = 0; p < P; ++p)
 #pragma unroll
@@ -186,11 +254,15 @@ __global__ void __launch_bounds__(256) rotary_grad(RotaryArgs a)
             if (x >= a.axes) break;
             double v = acc[p][x];
             for (int d = 32; d >= a.run; d >>= 1) v += __shfl_xor(v, d);
-            __syncthreads();
-            sums[wave][lane] = v;
-            __syncthreads();
-            if ((int)threadIdx.x < a.run) a.partial[(row * a.axes + x) * a.pairs + P * u + p] = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+            if (lane < a.run) sums[wave][p * 4 + x][lane] = v;
         }
+    __syncthreads();
+    const size_t row = ((size_t)f * a.chunks + chunk) * a.parts + part;
+    for (int e = threadIdx.x; e < P * 4 * a.run; e += 256) {
+        const int v = e / a.run, at = e - v * a.run, p = v >> 2, x = v & 3;
+        if (x < a.axes)
+            a.partial[(row * a.axes + x) * a.pairs + P * (ub * a.run + at) + p] = (sums[0][v][at] + sums[1][v][at]) + (sums[2][v][at] + sums[3][v][at]);
+    }
 }
 
 // One wave for each frequency: its sums over all chunks.
@@ -206,19 +278,21 @@ __global__ void __launch_bounds__(256) rotary_grad_join(const double *partial, f
     if (lane == 0) dfreq[at] = (float)v;
 }
 
-#define BY_FORM(kernel, grid, vec, halves, s, a)                                                       \
-    do {                                                                                               \
-        if (vec && halves) hipLaunchKernelGGL((kernel<true, true>), dim3(grid), dim3(256), 0, s, a);   \
-        else if (vec) hipLaunchKernelGGL((kernel<true, false>), dim3(grid), dim3(256), 0, s, a);       \
-        else if (halves) hipLaunchKernelGGL((kernel<false, true>), dim3(grid), dim3(256), 0, s, a);    \
-        else hipLaunchKernelGGL((kernel<false, false>), dim3(grid), dim3(256), 0, s, a);               \
+#define BY_FORM(kernel, grid, vec, halves, s, a)                                                                            \
+    do {                                                                                                                    \
+        if (vec && halves && a.fast) hipLaunchKernelGGL((kernel<true, true, true>), dim3(grid), dim3(256), 0, s, a);        \
+        else if (vec && a.fast) hipLaunchKernelGGL((kernel<true, false, true>), dim3(grid), dim3(256), 0, s, a);            \
+        else if (vec && halves) hipLaunchKernelGGL((kernel<true, true, false>), dim3(grid), dim3(256), 0, s, a);            \
+        else if (vec) hipLaunchKernelGGL((kernel<true, false, false>), dim3(grid), dim3(256), 0, s, a);                     \
+        else if (halves) hipLaunchKernelGGL((kernel<false, true, false>), dim3(grid), dim3(256), 0, s, a);                  \
+        else hipLaunchKernelGGL((kernel<false, false, false>), dim3(grid), dim3(256), 0, s, a);                             \
     } while (0)
 
 }  // namespace
 
 hipError_t launch_rotary(const RotaryArgs &a, bool vec, bool halves, hipStream_t s)
 {
-    const unsigned grid = (a.turn_threads + 255u) / 256u + (a.copy_threads + 255u) / 256u;
+    const unsigned grid = (a.turn_threads + 255u) / 256u * (unsigned)(a.freq_heads * a.parts) + (a.copy_threads + 255u) / 256u;
     BY_FORM(rotary_turn, grid, vec, halves, s, a);
     return hipGetLastError();
 }
