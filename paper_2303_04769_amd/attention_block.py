@@ -2,12 +2,14 @@
 
     out = in + conv1x1(attention(q, k, v)),   (q, k, v) = conv1x1(silu(groupnorm(in)))
 
-ImageBlock runs it over the pixels of feature maps with a learned bias for every offset of rows and columns, and takes the gradients of its input,
-gamma, beta and the bias table through frozen filters (the data gradient of a 1x1 convolution is a 1x1 convolution with the transposed filter).
+ImageBlock runs it over the pixels of feature maps with a learned bias for every offset of rows and columns, or rotary positions of rows and columns, or both, and takes
+the gradients of its input, gamma, beta, the bias table and the rotary frequencies through frozen filters (the data gradient of a 1x1 convolution is a 1x1 convolution
+with the transposed filter).
 FrameBlock runs it over the frames of sequences, causally and with a bias over distances: a whole sequence at once, or frame by frame
 on a cache of the keys and values that were seen.
+StreamBlock runs it over streams that come and go, each of an age of its own, with rotary positions, on a paged cache that they share: the next frames of each, one or many.
 
-    python -m paper_2303_04769_amd.attention_block        trains the first for a few steps, compares both ways through the second
+    python -m paper_2303_04769_amd.attention_block        trains the first for a few steps, compares both ways through the second and the third
 
 Everything is enqueued on torch's current stream; tensors are float32, activations channel-blocked. No arithmetic of the layers happens here.
 """
@@ -17,6 +19,7 @@ import torch
 
 from . import attn as A
 from . import binding as B
+from . import cache as K
 
 
 def _packed(weight, Cib, Cob):
@@ -37,9 +40,10 @@ def _conv1x1(inp, filt, out, N, Ci, Co, H, W, Cib, Cob):
 
 
 class ImageBlock:
-    """The block over N images of H x W pixels and Cc channels. w_in: [(heads + 2 kv_heads) D][Cc], w_out: [Cc][heads D], frozen."""
+    """The block over N images of H x W pixels and Cc channels. w_in: [(heads + 2 kv_heads) D][Cc], w_out: [Cc][heads D], frozen. halves: how rotary
+    positions pair channels (cache.Rotary)."""
 
-    def __init__(self, w_in, w_out, N, Cc, H, W, G, heads, kv_heads, D, cap=0.0, Cb=16):
+    def __init__(self, w_in, w_out, N, Cc, H, W, G, heads, kv_heads, D, cap=0.0, Cb=16, halves=False):
         self.N, self.C, self.H, self.W, self.Cb = N, Cc, H, W, Cb
         self.Cq, self.Ck = heads * D, kv_heads * D
         self.Cqkv = self.Cq + 2 * self.Ck
@@ -52,6 +56,8 @@ class ImageBlock:
         self.bucket, self.buckets = bucket.to(dev), buckets
         self.norm = A.GroupNorm(N, Cc, H, W, G, act="silu", Cb=Cb, device=dev)
         self.attention = A.Attention(N, H * W, H * W, heads, kv_heads, D, Cb=Cb, cap=cap, width=width, reach=reach, buckets=buckets, device=dev)
+        self._turns, self._turn_sizes = {}, (N, H * W, heads, kv_heads, D)
+        self.halves = halves
         self.stats = torch.empty(N, G, 2, device=dev)
         self.lse = torch.empty(N, heads, H * W, device=dev)
         self.h, self.qkv, self.ctx = self._empty(Cc), self._empty(self.Cqkv), self._empty(self.Cq)
@@ -68,28 +74,44 @@ class ImageBlock:
     def _conv(self, inp, filt, out):
         _conv1x1(inp, filt, out, self.N, inp.shape[1] * self.Cb, out.shape[1] * self.Cb, self.H, self.W, self.Cb, self.Cb)
 
-    def forward(self, inp, gamma, beta, table):
-        """inp: [N][C/Cb][H*W][Cb]; table: [heads][buckets]. Returns the output; what grad needs stays in the block."""
+    def _turn(self, freq):
+        """The plan of rotary positions with frequencies of this shape."""
+        F, axes, pairs = freq.shape
+        if (F, axes, pairs) not in self._turns:
+            if axes != 2:
+                raise ValueError(f"expected frequencies [1 or key heads][2][pairs] for rows and columns, got {list(freq.shape)}")
+            self._turns[F, axes, pairs] = K.Rotary(*self._turn_sizes, axes=2, pairs=pairs, halves=self.halves, extent=(self.W,), freq_heads=F, Cb=self.Cb, device=self.w_in.device)
+        return self._turns[F, axes, pairs]
+
+    def forward(self, inp, gamma, beta, table=None, freq=None):
+        """inp: [N][C/Cb][H*W][Cb]; table: [heads][buckets]; freq: [1 or kv_heads][2][pairs], rotary positions of rows and columns. Returns the output; what grad
+        needs stays in the block."""
         _shaped(inp, (self.N, self.C // self.Cb, self.H * self.W, self.Cb))
         out = torch.empty_like(inp)
         self.norm.run(inp, gamma, beta, self.h, self.stats)
         self._conv(self.h, self.w_in, self.qkv)
-        self.attention.run(*self._parts(self.qkv), self.ctx, lse=self.lse, table=table, bucket=self.bucket)
+        if freq is not None:
+            self._turn(freq).run(*self._parts(self.qkv)[:2], freq)
+        self.attention.run(*self._parts(self.qkv), self.ctx, lse=self.lse, table=table, bucket=None if table is None else self.bucket)
         self._conv(self.ctx, self.w_out, out)
         B.small_add(out, inp, out, out.numel())
         return out
 
-    def grad(self, inp, gamma, beta, table, dout):
-        """Gradients (inp, gamma, beta, table) of the last forward call, which had the same arguments."""
+    def grad(self, inp, gamma, beta, table, dout, freq=None):
+        """Gradients (inp, gamma, beta, table) of the last forward call, which had the same arguments, and that of freq behind them if there is one (None for a table of None)."""
         _shaped(dout, (self.N, self.C // self.Cb, self.H * self.W, self.Cb))
-        din, dgamma, dbeta, dtable = (torch.empty_like(t) for t in (inp, gamma, beta, table))
+        din, dgamma, dbeta, dtable, dfreq = (None if t is None else torch.empty_like(t) for t in (inp, gamma, beta, table, freq))
         self._conv(dout, self.w_out_t, self.dctx)
         self.attention.grad(*self._parts(self.qkv), self.ctx, self.lse, self.dctx, *self._parts(self.dqkv), dtable=dtable, table=table,
-                            bucket=self.bucket)
+                            bucket=None if table is None else self.bucket)
+        if freq is not None:
+            q, k, _ = self._parts(self.qkv)
+            dq, dk, _ = self._parts(self.dqkv)
+            self._turn(freq).grad(dq, dk, freq, q=q, k=k, dfreq=dfreq)
         self._conv(self.dqkv, self.w_in_t, self.dh)
         self.norm.grad(inp, gamma, beta, self.stats, self.dh, din, dgamma, dbeta)
         B.small_add(din, dout, din, din.numel())
-        return din, dgamma, dbeta, dtable
+        return (din, dgamma, dbeta, dtable) if freq is None else (din, dgamma, dbeta, dtable, dfreq)
 
 
 KEPT_PLANS = 4
@@ -161,6 +183,106 @@ class FrameBlock:
         return out
 
 
+ROWS_ON_CACHE = 64
+
+
+class StreamBlock:
+    """The block over up to N streams, channels last, with rotary positions (freq: [1 or kv_heads][1][pairs]) and a paged cache of `pages` pages of `page` tokens for all of them,
+    `per_stream` of them at most for one; kind: what the cache holds (cache.PagedCache). Each call brings the next frames of some or all streams; a stream that ends gives its
+    pages back. Few new frames attend to the cache itself, many to what is read back from it: the same keys and values, whichever way a stream's frames come in."""
+
+    def __init__(self, w_in, w_out, gamma, beta, freq, N, pages, page, per_stream, Cc, G, heads, kv_heads, D, kind="int8", cap=0.0, halves=True, Cb=16):
+        dev = w_in.device
+        self.N, self.C, self.G, self.heads, self.kv_heads, self.D, self.cap, self.halves, self.Cb = N, Cc, G, heads, kv_heads, D, cap, halves, Cb
+        self.Cq, self.Ck = heads * D, kv_heads * D
+        _shaped(w_in, (self.Cq + 2 * self.Ck, Cc))
+        _shaped(w_out, (Cc, self.Cq))
+        _shaped(gamma, (Cc,))
+        _shaped(beta, (Cc,))
+        if freq.dim() != 3 or freq.shape[1] != 1:
+            raise ValueError(f"expected frequencies [1 or key heads][1][pairs], got {list(freq.shape)}")
+        self.w_in, self.w_out = _packed(w_in, Cb, Cb), _packed(w_out, Cb, Cb)
+        self.gamma, self.beta, self.freq = gamma, beta, freq
+        self.cache = K.PagedCache(pages, page, kv_heads, D, kind=kind, device=dev)
+        self.page, self.per_stream = page, per_stream
+        self.free, self.held = list(range(pages))[::-1], [[] for _ in range(N)]
+        self.lengths = [0] * N
+        self.table = torch.full((N, per_stream), -1, dtype=torch.int32, device=dev)
+        self._first, self._length = (torch.zeros(N, dtype=torch.int32, device=dev) for _ in range(2))
+        self._plans = {}
+
+    def _plan(self, S, Sk):
+        """What calls of S new frames need; Sk: tokens that are read back, 0 where the cache is attended to. The last few are kept."""
+        plan = self._plans.pop((S, Sk), None)
+        if plan is None:
+            dev, tokens = self.w_in.device, self.N * S
+            e = lambda *shape: torch.empty(*shape, device=dev)  # noqa: E731
+            F, _, pairs = self.freq.shape
+            attention = A.Attention(self.N, S, Sk, self.heads, self.kv_heads, self.D, Cb=self.D, cap=self.cap, causal=True, device=dev) if Sk else \
+                K.CacheAttention(self.cache, self.N, S, self.heads, self.per_stream, Cb=self.D, cap=self.cap, device=dev)
+            plan = (A.GroupNorm(tokens, self.C, 1, 1, self.G, act="silu", Cb=self.C, device=dev),
+                    K.Rotary(self.N, S, self.heads, self.kv_heads, self.D, pairs=pairs, halves=self.halves, freq_heads=F, Cb=self.D, device=dev), attention,
+                    e(tokens, self.C), e(tokens, self.Cq + 2 * self.Ck), e(tokens, self.Cq),
+                    (e(self.N, self.kv_heads, Sk, self.D), e(self.N, self.kv_heads, Sk, self.D)) if Sk else None)
+            while len(self._plans) >= KEPT_PLANS:
+                del self._plans[next(iter(self._plans))]                   # (the one that was not used for longest)
+        self._plans[S, Sk] = plan
+        return plan
+
+    def _take(self, counts):
+        """Pages for so many more frames of each stream, all or none."""
+        need = [-(-(held + more) // self.page) - len(pages) for held, more, pages in zip(self.lengths, counts, self.held)]
+        for n, (held, more) in enumerate(zip(self.lengths, counts)):
+            if held + more > self.per_stream * self.page:
+                raise ValueError(f"stream {n}: {held} frames and {more} more do not fit {self.per_stream} pages of {self.page}")
+        if sum(need) > len(self.free):
+            raise ValueError(f"{sum(need)} pages are needed and {len(self.free)} free")
+        for n, more in enumerate(need):
+            if more:
+                new = [self.free.pop() for _ in range(more)]
+                at = len(self.held[n])
+                self.held[n] += new
+                self.table[n, at:at + more] = torch.tensor(new, dtype=torch.int32)
+
+    def release(self, n):
+        """Stream n ends: its pages are free, its place is empty for another."""
+        self.free += self.held[n][::-1]
+        self.held[n] = []
+        self.lengths[n] = 0
+        self._length[n] = 0
+        self.table[n] = -1
+
+    def forward(self, frames, counts=None):
+        """The next frames [N][S][Cc], of which stream n has counts[n] (a list; None: S each): their outputs. What stands behind a stream's frames, in and out, is of no
+        meaning."""
+        S = frames.shape[1]
+        _shaped(frames, (self.N, S, self.C))
+        if counts is not None and (len(counts) != self.N or not all(0 <= c <= S for c in counts)):
+            raise ValueError(f"expected {self.N} numbers of frames in 0 .. {S}, got {counts}")
+        more = [S] * self.N if counts is None else [int(c) for c in counts]
+        self._take(more)
+        here = None if counts is None else torch.tensor(more, dtype=torch.int32).to(frames.device)
+        self._first.copy_(self._length)
+        self._length.add_(S if here is None else here)
+        self.lengths = [a + b for a, b in zip(self.lengths, more)]
+        few = S * (self.heads // self.kv_heads) <= ROWS_ON_CACHE
+        norm, rotary, attention, h, qkv, ctx, read = self._plan(S, 0 if few else -(-max(self.lengths) // self.page) * self.page)
+        out = torch.empty_like(frames)
+        norm.run(frames, self.gamma, self.beta, h)
+        _conv1x1(h, self.w_in, qkv, self.N * S, self.C, self.Cq + 2 * self.Ck, 1, 1, self.Cb, self.Cb)
+        heads = lambda t, first, n: t.as_strided((self.N, n, S, self.D), (S * t.shape[1], self.D, t.shape[1], 1), first)  # noqa: E731
+        q, k, v = heads(qkv, 0, self.heads), heads(qkv, self.Cq, self.kv_heads), heads(qkv, self.Cq + self.Ck, self.kv_heads)
+        self.cache.write(k, v, self.table, self._first, counts=here, rotary=rotary, freq=self.freq, q=q)
+        if few:
+            attention.run(q, heads(ctx, 0, self.heads), self.table, self._length, first=self._first)
+        else:
+            self.cache.read(*read, self.table, counts=self._length)
+            attention.run(q, *read, heads(ctx, 0, self.heads), lengths=self._length, first=self._first)
+        _conv1x1(ctx, self.w_out, out, self.N * S, self.Cq, self.C, 1, 1, self.Cb, self.Cb)
+        B.small_add(out, frames, out, out.numel())
+        return out
+
+
 def _uniform(gen, *shape, of=1.0):
     return (torch.rand(*shape, generator=gen) * (2 * of) - of).cuda()
 
@@ -192,6 +314,12 @@ def main(steps=20):
     at_once = whole.forward(frames)
     in_turn = torch.cat([single.forward(frames[:, :S].contiguous())] + [single.forward(frames[:, i:i + 1].contiguous()) for i in range(S, room)], 1)
     print(f"{room} frames at once, and {S} and then one by one: outputs differ by {float((at_once - in_turn).abs().max()):.1e} at most")
+
+    freq = K.axis_frequencies(D // 2).cuda()
+    whole, single = (StreamBlock(w_in, w_out, params[0], params[1], freq, 2, 24, 16, 12, Cc, G, heads, kv_heads, D, cap=20.0) for _ in range(2))
+    at_once = whole.forward(frames)
+    in_turn = torch.cat([single.forward(frames[:, :S].contiguous())] + [single.forward(frames[:, i:i + 1].contiguous()) for i in range(S, room)], 1)
+    print(f"the same on 8-bit pages: outputs differ by {float((at_once - in_turn).abs().max()):.1e} at most")
 
 
 if __name__ == "__main__":

@@ -1,0 +1,186 @@
+"""The attention block with rotary positions: images with the gradients of their frequencies, streams of different ages on a paged cache, against 64 bits."""
+import pytest
+import torch
+
+import paper_2303_04769_amd as S
+from paper_2303_04769_amd import attention_block as AB
+
+pytestmark = pytest.mark.gpu
+TOL = 1.1e-3           # of the block's layers in fp32 against 64 bits (test_gpu_attention_block.py: 1e-4 (sqrt(K) max + 1) of two convolutions of up to 96 channels)
+
+
+def uniform(gen, *shape, of=1.0):
+    return ((torch.rand(*shape, generator=gen, dtype=torch.float64) * 2 - 1) * of).float().double()
+
+
+def norm64(x, gamma, beta, G):
+    """[..][pixels][C] -> normalized in G groups over the last two, then SiLU"""
+    N, P, C = x.shape
+    c = x.transpose(1, 2).reshape(N, G, -1)
+    c = (c - c.mean(2, keepdim=True)) / torch.sqrt(c.var(2, unbiased=False, keepdim=True) + 1e-5)
+    z = c.reshape(N, C, P).transpose(1, 2) * gamma + beta
+    return z * torch.sigmoid(z)
+
+
+def turn64(x, place, freq, halves):
+    """x [N][S][heads][D], place [S][axes] or [N][S][axes], freq [F][axes][pairs]"""
+    F, axes, P = freq.shape
+    heads = x.shape[2]
+    angle = torch.einsum("...sa,fap->...sfp", place, freq).repeat_interleave(heads // F, -2)
+    a, b = (slice(0, P), slice(P, 2 * P)) if halves else (slice(0, 2 * P, 2), slice(1, 2 * P, 2))
+    first = x[..., a] * torch.cos(angle) - x[..., b] * torch.sin(angle)
+    second = x[..., a] * torch.sin(angle) + x[..., b] * torch.cos(angle)
+    rest = x[..., 2 * P:]
+    turned = torch.cat((first, second), -1) if halves else torch.stack((first, second), -1).flatten(-2)
+    return torch.cat((turned, rest), -1)
+
+
+def attention64(q, k, v, bias, cap, seen=None):
+    """[N][S][heads][D] -> [N][S][heads * D]"""
+    N, Sq, heads, D = q.shape
+    k, v = (t.repeat_interleave(heads // k.shape[2], 2) for t in (k, v))
+    s = torch.einsum("nihd,njhd->nhij", q, k) / D ** 0.5
+    s = cap * torch.tanh(s / cap) if cap else s
+    s = s if bias is None else s + bias
+    s = s if seen is None else s.masked_fill(~seen, -torch.inf)
+    return torch.einsum("nhij,njhd->nihd", torch.softmax(s, -1), v).reshape(N, Sq, heads * D)
+
+
+def close(got, want, what, tol=TOL):
+    off = float((got - want).abs().max())
+    assert off <= tol * (1 + float(want.abs().max())), (what, off)
+
+
+@pytest.mark.parametrize("N,Cc,H,W,G,heads,kv_heads,D,F,pairs,halves,with_table,Cb", [(2, 32, 5, 3, 4, 2, 1, 16, 1, 8, False, True, 16), (3, 48, 4, 4, 3, 3, 3, 16, 3, 8, True, False, 16),
+                                                                                     (1, 96, 9, 7, 8, 4, 2, 24, 2, 10, False, False, 8)])
+def test_image_block_with_rotary_positions(N, Cc, H, W, G, heads, kv_heads, D, F, pairs, halves, with_table, Cb):
+    gen = torch.Generator().manual_seed(Cc + H)
+    w_in, w_out = uniform(gen, (heads + 2 * kv_heads) * D, Cc, of=Cc ** -0.5), uniform(gen, Cc, heads * D, of=(heads * D) ** -0.5)
+    block = AB.ImageBlock(w_in.float().cuda(), w_out.float().cuda(), N, Cc, H, W, G, heads, kv_heads, D, cap=4.0, Cb=Cb, halves=halves)
+    args = [uniform(gen, N, H * W, Cc), 1 + uniform(gen, Cc, of=0.3).float().double(), uniform(gen, Cc, of=0.3), uniform(gen, heads, block.buckets), uniform(gen, F, 2, pairs)]
+    dout = uniform(gen, N, H * W, Cc)
+    place = torch.stack((torch.arange(H * W) // W, torch.arange(H * W) % W), 1).double()
+    rows, cols = place[:, 0].long(), place[:, 1].long()
+    at = (rows[None] - rows[:, None]) * (2 * W - 1) + cols[None] - cols[:, None] + block.attention.record.reach
+    Cq, Ck = heads * D, kv_heads * D
+
+    def run(x, gamma, beta, table, freq):
+        qkv = norm64(x, gamma, beta, G) @ w_in.t()
+        q, k, v = (t.reshape(N, H * W, -1, D) for t in qkv.split((Cq, Ck, Ck), 2))
+        q, k = turn64(q, place, freq, halves), turn64(k, place, freq, halves)
+        return x + attention64(q, k, v, table[:, at] if with_table else None, 4.0) @ w_out.t()
+
+    blocked = lambda t: t.float().reshape(N, H * W, Cc // Cb, Cb).transpose(1, 2).contiguous().cuda()  # noqa: E731
+    plain = lambda t: t.transpose(1, 2).reshape(N, H * W, Cc).cpu().double()  # noqa: E731
+    on = [blocked(args[0])] + [t.float().cuda() for t in args[1:]]
+    table = on[3] if with_table else None
+    close(plain(block.forward(*on[:3], table, on[4])), run(*args), "out")
+    grads = block.grad(*on[:3], table, blocked(dout), on[4])
+    assert len(grads) == 5 and (grads[3] is not None) == with_table
+    leaves = [t.clone().requires_grad_() for t in args]
+    run(*leaves).backward(dout)
+    for i, (g, leaf) in enumerate(zip(grads, leaves)):
+        if g is None:
+            continue
+        g = plain(g) if i == 0 else g.cpu().double()
+        # (gradients are sums over what the output's error is the error of: relative to the sums of their terms' sizes)
+        scale = float(leaf.grad.abs().max())
+        assert float((g - leaf.grad).abs().max()) <= TOL * (1 + scale), ("inp", "gamma", "beta", "table", "freq")[i]
+    # without rotary positions the block is what it was
+    if with_table:
+        assert len(block.grad(*on[:3], table, blocked(dout))) == 4
+
+
+def stream_block(gen, N, Cc, G, heads, kv_heads, D, kind, pages, page, per, halves=True, F=1, pairs=None):
+    w_in, w_out = uniform(gen, (heads + 2 * kv_heads) * D, Cc, of=Cc ** -0.5), uniform(gen, Cc, heads * D, of=(heads * D) ** -0.5)
+    gamma, beta, freq = 1 + uniform(gen, Cc, of=0.3).float().double(), uniform(gen, Cc, of=0.3), uniform(gen, F, 1, pairs or D // 2)
+    on = [t.float().cuda() for t in (w_in, w_out, gamma, beta, freq)]
+    make = lambda: AB.StreamBlock(*on, N, pages, page, per, Cc, G, heads, kv_heads, D, kind=kind, cap=6.0, halves=halves)  # noqa: E731
+
+    def run(x):
+        """One stream's frames [S][Cc], whole"""
+        S_, place = x.shape[0], torch.arange(x.shape[0], dtype=torch.float64)[:, None]
+        qkv = norm64(x.view(S_, 1, Cc), gamma, beta, G).view(1, S_, Cc) @ w_in.t()
+        q, k, v = (t.reshape(1, S_, -1, D) for t in qkv.split((heads * D, kv_heads * D, kv_heads * D), 2))
+        q, k = turn64(q, place, freq, halves), turn64(k, place, freq, halves)
+        seen = torch.arange(S_)[None] <= torch.arange(S_)[:, None]
+        return (x + (attention64(q, k, v, None, 6.0, seen) @ w_out.t())[0])
+    return make, run
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "int8"])
+def test_streams_that_come_and_go(kind):
+    """Three places: prompts of unequal length in one padded batch, single frames of some, a few frames at once, a stream that ends and another in its place, a long piece behind
+    all that. Each stream's outputs are those of its frames at once, in 64 bits (float32), or nearly (fewer bits: what rounding keys and values to 2^-9 of them, or 2^-8 of their
+    largest, can move a result by, which is a mean of values of up to 2 through a filter of 64 rows: 0.1)."""
+    gen = torch.Generator().manual_seed(5)
+    N, Cc, G, heads, kv_heads, D, page, per = 3, 48, 4, 4, 2, 16, 16, 12
+    make, run = stream_block(gen, N, Cc, G, heads, kv_heads, D, kind, 26, page, per, F=2)
+    block = make()
+    streams = [uniform(gen, 150, Cc) for _ in range(4)]
+    at, who, got = [0, 0, 0], [0, 1, 2], {0: [], 1: [], 2: [], 3: []}
+
+    def bring(counts, width):
+        frames = torch.full((N, width, Cc), 7.0, dtype=torch.float64)
+        for n, c in enumerate(counts):
+            frames[n, :c] = streams[who[n]][at[n]:at[n] + c]
+        out = block.forward(frames.float().cuda(), counts).cpu().double()
+        for n, c in enumerate(counts):
+            got[who[n]].append(out[n, :c])
+            at[n] += c
+        assert len(block._plans) <= AB.KEPT_PLANS
+    bring([40, 7, 33], 40)
+    for _ in range(3):
+        bring([1, 1, 1], 1)
+    bring([0, 1, 1], 1)
+    bring([5, 0, 3], 5)
+    block.release(1)
+    assert block.lengths[1] == 0 and len(block.free) == 26 - sum(-(-a // page) for a in (at[0], at[2]))
+    who[1], at[1] = 3, 0
+    bring([2, 60, 50], 60)
+    bring([1, 1, 1], 1)
+    assert sorted(block.free + sum(block.held, [])) == list(range(26))
+    for k, pieces in got.items():
+        out = torch.cat(pieces)
+        want = run(streams[k][:len(out)])
+        close(out, want, k, TOL if kind == "float32" else 0.1 / (1 + float(want.abs().max())))
+
+
+@pytest.mark.parametrize("kind", ["float32", "int8"])
+def test_frames_one_by_one_and_at_once(kind):
+    """The same keys and values whichever way they come in: outputs differ by fp32 sums in another order alone."""
+    gen = torch.Generator().manual_seed(9)
+    make, _ = stream_block(gen, 2, 64, 8, 4, 2, 32, kind, 20, 16, 9, halves=False)
+    frames = uniform(gen, 2, 140, 64).float().cuda()
+    whole, single = make(), make()
+    a = whole.forward(frames)
+    b = torch.cat([single.forward(frames[:, :100].contiguous())] + [single.forward(frames[:, i:i + 1].contiguous()) for i in range(100, 140)], 1)
+    close(b.cpu().double(), a.cpu().double(), kind, 2 * TOL)
+    if kind == "int8":
+        assert torch.equal(whole.cache.keys[whole.table.long()[whole.table.long() >= 0]], single.cache.keys[single.table.long()[single.table.long() >= 0]])
+
+
+def test_no_pages_left():
+    """All or nothing: a call that does not fit changes no length, no table and no list of free pages."""
+    gen = torch.Generator().manual_seed(3)
+    make, _ = stream_block(gen, 2, 32, 4, 2, 1, 16, "int8", 5, 16, 4)
+    block = make()
+    frames = torch.zeros(2, 33, 32, device="cuda")
+    block.forward(frames[:, :17].contiguous())
+    before = (block.lengths[:], block.table.clone(), block.free[:], [h[:] for h in block.held])
+    for counts in (None, [33, 1], [33, 33]):
+        with pytest.raises(ValueError):
+            block.forward(frames, counts)
+        assert block.lengths == before[0] and torch.equal(block.table, before[1]) and block.free == before[2] and block.held == before[3]
+    with pytest.raises(ValueError):
+        block.forward(frames[:, :2].contiguous(), [1, 3])
+    with pytest.raises(ValueError):
+        block.forward(frames[:, :2].contiguous(), [1])
+    block.release(0)
+    block.forward(frames, [33, 0])
+    assert block.lengths == [33, 17]
+
+
+def test_the_example_runs(capsys):
+    AB.main(steps=2)
+    assert "8-bit pages" in capsys.readouterr().out
