@@ -10,7 +10,7 @@ struct CacheArgs {
     float *key_scales, *value_scales;
     int kind, pages, shift, kv_heads, D, Dk, per_stream;      // shift: log2 of a page's tokens
     const int *table;
-    int workgroups, least_rounds;                             // attention: at most so many, with so many rounds each at least
+    int workgroups;                                           // attention: at most so many
     int2 *units;                                              // the first and last workgroup that has a part of a unit; null: none is split
     FastDiv by_rows;
 };

@@ -228,7 +228,7 @@ CacheArgs cache_args(const small_cache &c)
 {
     const int size = cache_bytes(c.kind), fill = 16 / size;
     return CacheArgs{(char *)c.keys, (char *)c.values, c.key_scales, c.value_scales, c.kind, c.pages, log2_of(c.page), c.kv_heads, c.D, (c.D + fill - 1) / fill * fill,
-                     c.per_stream, c.table, 0, 1, nullptr, {}};
+                     c.per_stream, c.table, 0, nullptr, {}};
 }
 struct CacheRanges { Range r[4]; };
 CacheRanges cache_ranges(const small_cache &c)
@@ -280,7 +280,6 @@ struct TokenPlan {
     double rounds;
     size_t ml_at, units_at, bytes;
 };
-constexpr int kLeastRounds = 1;
 TokenPlan plan_token(const small_cache &c, const small_attn &a)
 {
     TokenPlan p{};
@@ -459,7 +458,6 @@ int small_cache_attention(const small_cache *c, const small_attn *a, const float
     x.vec = quads(a->D, a->Cb, {&a->q, &a->out}, {q, out});
     CacheArgs held_args = cache_args(*c);
     held_args.workgroups = p.workgroups;
-    held_args.least_rounds = kLeastRounds;
     held_args.units = p.joined ? (int2 *)((char *)workspace + p.units_at) : nullptr;
     held_args.by_rows = make_fastdiv(p.rows);
     return from_hip(launch_cache_token(x, held_args, p.joined, (hipStream_t)stream));

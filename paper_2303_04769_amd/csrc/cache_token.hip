@@ -159,9 +159,9 @@ struct Rounds {
             const int below = __shfl_up(sum, d);
             sum += lane >= d ? below : 0;
         }
-        __syncthreads();
+        lds_barrier();
         if (lane == 63) prefix[threads + 1 + wave] = sum;
-        __syncthreads();
+        lds_barrier();
         int total = 0, under = 0;
         for (int w = 0; w < threads >> 6; ++w) {
             const int x = prefix[threads + 1 + w];
@@ -170,13 +170,14 @@ struct Rounds {
         }
         prefix[tid] = under + sum - mine;
         if (tid == 0) prefix[threads] = total;
-        __syncthreads();
+        lds_barrier();
         return __builtin_amdgcn_readfirstlane(total);
     }
     __device__ __forceinline__ Rounds(const AttnArgs &a, const CacheArgs &c, int keys, int *lds) : prefix(lds), threads(blockDim.x), units(a.head_sets * a.row_tiles)
     {
         for (int n = 0; n < a.N; n += threads) all += scan(a, n, keys);
-        workgroups = max(1, min(c.workgroups, all / c.least_rounds));
+        const int most = (all + c.workgroups - 1) / c.workgroups;      // rounds of the longest: no more workgroups than that takes, for the fewest parts
+        workgroups = (all + most - 1) / most;
         each = all / workgroups;
         more = all - each * workgroups;                       // the first so many have one more
     }
@@ -202,7 +203,7 @@ struct Rounds {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         if (prefix[tid] <= y && y < prefix[tid + 1]) prefix[threads + 5] = tid;
-        __syncthreads();
+        lds_barrier();
         const int found = __builtin_amdgcn_readfirstlane(prefix[threads + 5]);
         *start = before + __builtin_amdgcn_readfirstlane(prefix[found]);
         return chunk + found;
@@ -211,7 +212,7 @@ struct Rounds {
 constexpr int rounds_ints(int threads) { return threads + 6; }
 
 // SP: into how many columns a row's keys of a tile are shared out, where there are at most 16 / SP rows. Column m then has row m mod (16 / SP), and of the tile's results only
-// those of its share, m / (16 / SP): as if it were a row of its own, with a maximum, a sum and a result of its own, joined as those of the waves are. So the 16 columns
+// those of its share, m / (16 / SP): as if it were a row of its own, with a maximum, a sum and a result of its own, joined in the end. So the 16 columns
 // of single tokens' products are not mostly empty lanes in all that lies between the products.
 template <int KIND, int DT, int SP, bool ONE>
 __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_waves_per_eu(least_waves(KIND, DT, SP)))) cache_token(AttnArgs args, CacheArgs cache_args)
@@ -500,43 +501,66 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
         }
     }
     sum = column_sum(sum);
+    float most = top.maximum();
+    if constexpr (SP > 1) {                                    // a row's shares: columns 16 / SP apart, in the same sixteen lanes
+        float all = most;
+        all = fmaxf(all, __int_as_float(dpp_of<0x128>(__float_as_int(all))));            // row_ror:8
+        if constexpr (SP == 4) all = fmaxf(all, __int_as_float(dpp_of<0x124>(__float_as_int(all))));
+        const float w = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(most - all);            // (a share that saw no key)
+        const auto over = [&](float x) {
+            x = sum == 0.f ? 0.f : x * w;
+            x += __int_as_float(dpp_of<0x128>(__float_as_int(x)));
+            if constexpr (SP == 4) x += __int_as_float(dpp_of<0x124>(__float_as_int(x)));
+            return x;
+        };
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[d][e] = over(o[d][e]);
+        sum = over(sum);
+        most = all;
+    }
 
-    // join the waves' shares: [wave][share][row][DP] and [wave][share][row] (maximum, sum)
+    // join the waves: [wave][row][DP] and [wave][row] (maximum, sum)
     const AttnArgs z = late_args();
     const CacheArgs zc = late_cache_args();
     const size_t all_units = (size_t)n * rounds.units + unit, part = (w_id + all_units) * R;       // (workgroups and units both only grow: a place of its own for each pair)
     if (zc.units && lo_round == 0 && tid == 0) zc.units[all_units] = int2{w_id, rounds.owner(round - (hi_round - lo_round) + of_unit - 1)};      // who has parts of it, for the join
+    constexpr int LP = DP + 4;                                 // (rows of lanes that write at a time in different banks)
     float *const lo_ = token_lds;
-    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * SP * rows * DP);
-    int *const flags = reinterpret_cast<int *>(ml + waves * SP * rows);
-    if (m % R < rows) {
-        const int mine = (wave * SP + share) * rows + m % R;
+    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * rows * LP);
+    int *const flags = reinterpret_cast<int *>(ml + waves * rows);
+    if (m < rows) {
+        const int mine = wave * rows + m;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + mine * DP + 16 * d + 4 * g) = o[d];
-        if (g == 0) ml[mine] = float2{top.maximum(), sum};
+        for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + mine * LP + 16 * d + 4 * g) = o[d];
+        if (g == 0) ml[mine] = float2{most, sum};
     }
-    if (tid < 16) flags[tid] = 0;
-    __syncthreads();
+    if (tid < 17) flags[tid] = 0;                             // of rows, and of any
+    lds_barrier();
     constexpr int QD = DP / 4;
     for (int e = tid; e < rows * QD; e += 64 * waves) {
         const int rr = e / QD, d = (e - rr * QD) * 4;
         float all = -kInf, total = 0.f;
 #pragma unroll 4
-        for (int w = 0; w < waves * SP; ++w) all = fmaxf(all, ml[w * rows + rr].x);
+        for (int w = 0; w < waves; ++w) all = fmaxf(all, ml[w * rows + rr].x);
         const float ref = all == -kInf ? 0.f : all;
         floatx4 y = {};
 #pragma unroll 4
-        for (int w = 0; w < waves * SP; ++w) {
+        for (int w = 0; w < waves; ++w) {
             const float2 p = ml[w * rows + rr];
-            const floatx4 w4 = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * DP + d);
+            const floatx4 w4 = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * LP + d);
             const float f = __builtin_amdgcn_exp2f(p.x - ref);
             total += p.y == 0.f ? 0.f : f * p.y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * w4[x];       // (a share that saw no key)
+            for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * w4[x];       // (a wave that saw no key)
         }
-        if (d < z.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = 1;
+        if (d < z.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = flags[16] = 1;
         const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
-        if (!whole) {
+        if (!whole && z.D % 4 == 0) {
+            if (d < z.D) *reinterpret_cast<floatx4 *>(z.part_o + (part + rr) * z.D + d) = y;
+            if (d == 0) z.part_ml[part + rr] = float2{all, total};
+        } else if (!whole) {
 #pragma unroll
             for (int x = 0; x < 4; ++x)
                 if (d + x < z.D) z.part_o[(part + rr) * z.D + d + x] = y[x];
@@ -549,7 +573,12 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
             if (z.lse && d == 0) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
         }
     }
-    __syncthreads();
+    lds_barrier();
+    if (!__builtin_amdgcn_readfirstlane(flags[16])) {
+        lds_barrier();                                         // (what the join read is free)
+        continue;
+    }
+    __syncthreads();                                           // (stores of these rows have come to pass)
     for (int rr = wave; rr < rows; rr += waves) {
         if (!flags[rr]) continue;
         const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
@@ -632,7 +661,7 @@ hipError_t token_form(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
     switch (token_tiles(a.D)) {
 #define TOKEN(dt) \
     case dt: \
-        hipLaunchKernelGGL((cache_token<KIND, dt, SP, ONE>), dim3((unsigned)c.workgroups), dim3(64 * group_waves(dt)), (size_t)group_waves(dt) * SP * rows * (16 * dt + 2) * 4 + 64, s, a, c); \
+        hipLaunchKernelGGL((cache_token<KIND, dt, SP, ONE>), dim3((unsigned)c.workgroups), dim3(64 * group_waves(dt)), (size_t)group_waves(dt) * rows * (16 * dt + 6) * 4 + 80, s, a, c); \
         break;
         TOKEN(1) TOKEN(2) TOKEN(3) TOKEN(4) TOKEN(5) TOKEN(6) TOKEN(8) TOKEN(16)
 #undef TOKEN
