@@ -302,7 +302,7 @@ TokenPlan plan_token(const small_cache &c, const small_attn &a)
 }
 bool token_launches(const small_attn &a, const TokenPlan &p)
 {
-    return p.rounds < INT_MAX && launches((double)a.N * a.kv_heads * p.rows, 256);
+    return p.rounds < 1 << 30 && launches((double)a.N * a.kv_heads * p.rows, 256);
 }
 
 }  // namespace

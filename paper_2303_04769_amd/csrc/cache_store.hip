@@ -128,14 +128,15 @@ __global__ void __launch_bounds__(1024) cache_write(StoreArgs a)
     const bool kept = at.tok >= at.lo && at.tok < at.hi && at.page >= 0;
     const int lo_item = a.by_parts.div(at.part * a.items), hi_item = a.by_parts.div((at.part + 1) * a.items);
     const int q_items = a.items - 2 * a.c.kv_heads, D = a.c.D;
-    int place[4];
-    if (a.turns) place_of(a.r, at.n, at.i, at.first, place);
     QuadTurns<HALVES> turns;
     int turns_of = -1;
     const int i = max(0, min(at.i, a.S - 1)), other = max(0, at.d < a.r.pairs ? at.d + a.r.pairs : at.d - a.r.pairs), P = 1 << a.c.shift;
     const bool turning = a.turns && at.d < 2 * a.r.pairs;
-    // Heads of queries, of keys, of values, each kind with code of its own (a choice between the arguments' places, at run time, puts them all into scratch memory). A head's quad is
-    // on its way, with HALVES with the other channels of its pairs, while the one before is done.
+    int place[4];
+    if (a.turns) place_of(a.r, at.n, i, at.first, place);      // (of a token that there is: the tile's others have places, and positions, of none)
+    // Heads of queries, of keys, of values, each kind with code of its own (a choice between the arguments' places, at run time, puts them all into scratch memory). The quads of
+    // some heads, with HALVES with the other channels of their pairs, are on their way together.
+    constexpr int G = 4;
     const auto heads = [&](auto kind) {
         constexpr int W = decltype(kind)::value;
         const int before = W == 0 ? 0 : W == 1 ? q_items : q_items + a.c.kv_heads, all = W == 0 ? q_items : a.c.kv_heads;
@@ -157,16 +158,20 @@ __global__ void __launch_bounds__(1024) cache_write(StoreArgs a)
             }
             return r;
         };
-        Source next = fetch(lo);
-        for (int head = lo; head < hi; ++head) {
-            const Source now = next;
-            if (head + 1 < hi) next = fetch(head + 1);
-            floatx4 x = now.x;
+        for (int first = lo; first < hi; first += G) {
+        Source now[G];
+#pragma unroll
+        for (int b = 0; b < G; ++b) now[b] = fetch(min(first + b, hi - 1));
+#pragma unroll
+        for (int b = 0; b < G; ++b) {
+            const int head = first + b;
+            if (head >= hi) break;
+            floatx4 x = now[b].x;
             if (W < 2 && turning) {
                 const int f = a.r.freq_heads == 1 ? 0 : W == 0 ? a.by_per_q.div(head) : head;
                 if (f != turns_of) turns.set(a.r, place, f, at.d);
                 turns_of = f;
-                x = turns.turned(a.r, at.d, x, now.y);
+                x = turns.turned(a.r, at.d, x, now[b].y);
             }
             if constexpr (W == 0) {
                 if constexpr (FAST) {
@@ -221,6 +226,7 @@ __global__ void __launch_bounds__(1024) cache_write(StoreArgs a)
                     }
                 }
             }
+        }
         }
     };
     heads(std::integral_constant<int, 0>{});

@@ -582,6 +582,11 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
     for (int rr = wave; rr < rows; rr += waves) {
         if (!flags[rr]) continue;
         const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
+        // (a query that is not finite itself has no other result, and may be padding)
+        const float *query = token_at(z.q, z.qs, n, i2);
+        bool fine = true;
+        for (int d = lane; d < z.D; d += 64) fine &= fabsf(query[channel_at(z, z.qs, head2 * z.D + d)]) < kInf;
+        if (!__all(fine)) continue;
         const RowState again(z, im, n, i2, head2);
         float y[4], most, total;
         attend_cached_row<KIND>(z, zc, again, n, i2, key_head, begin, end, y, most, total);
@@ -595,7 +600,8 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
         if (lane) continue;
         if (!whole) z.part_ml[part + rr] = float2{most, total};
         else if (z.lse) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (most + __builtin_amdgcn_logf(total)) * kLn2;
-    }    __syncthreads();                                           // (what the join read is free)
+    }
+    __syncthreads();                                           // (what the join read is free)
     }
 }
 

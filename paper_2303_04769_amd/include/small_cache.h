@@ -24,7 +24,8 @@ extern "C" {
  * of one axis have zeros for the others; learned frequencies may turn by all of them.
  * A token's place is positions[n][i][axis] (int32 [N][S][axes]), or, where positions is NULL, that of number first[n] + i (first NULL: i, of at most 2^28 either
  * way) in rows of extent[axes - 1] places, planes of extent[axes - 2] rows and so on: extent[0] is not read, the first axis has no end.
- * Angles and turns are computed in 64 bits and rounded once, so results are within half a step of fp32 (and 2^-50 of the pair's larger channel).
+ * Angles and turns are computed in 64 bits and rounded once, so results are within half a step of fp32, and 2^-50 of the pair's larger channel times one and the size of the
+ * angle.
  *
  * small_rotary turns q ([N] images of `heads` heads, to q_out) and k (`kv_heads` heads, to k_out); q and q_out, or k and k_out, may both be NULL. An output may equal
  * its input exactly (in place); then channels that do not turn are not touched. Other overlaps are refused.
@@ -69,7 +70,7 @@ int small_rotary_grad(const small_rotation *r, const float *dq_out, const float 
  * its k, k_out, dq, dk are not read. Streams may share pages that are read; one place that a call writes twice holds one of the two.
  * small_cache_read: the same tokens from the cache to k and v; tokens that are none and those from counts[n] on are left as they were.
  * k, v: [N][blocks][S][Cb] views as in small_attn.h. Limits: of the launch's threads -- a quarter of D, filled up to a power of two
- * and to 4 at least, for each of N * (S + 31) tokens -- there are fewer than 2^32; per_stream * page <= 2^28. */
+ * and to 4 at least, for each of N * (S + 31) tokens; where S <= 4, at least 64 for each -- there are fewer than 2^32; per_stream * page <= 2^28. */
 enum { SMALL_CACHE_F32 = 0, SMALL_CACHE_BF16 = 1, SMALL_CACHE_I8 = 2 };
 typedef struct {
     int kind, pages, page, kv_heads, D;
@@ -90,7 +91,9 @@ int small_cache_read(const small_cache *c, const small_span *s, float *k, float 
 /* ---- attention of new tokens over the cache: small_attention with the keys and values of each stream's first lengths[n] tokens, causal. Of *a are read
  * N, Sq, heads, D, Cb, q, out, scale, cap, reach, buckets, lengths (not NULL; at most per_stream * page count), first (NULL: lengths[n] - Sq, the last tokens),
  * slopes, table (the bias's) and bucket; width must be 1, prefix and docs NULL, kv_heads and D the cache's. A stream of length zero is an empty place: out = 0,
- * lse = -inf. Meant for one token, or a few, a stream: sixteen rows (tokens times the query heads of a key head) read the cache once.
+ * lse = -inf. Meant for one token, or a few, a stream: sixteen rows (tokens times the query heads of a key head) read the cache once. The streams' work is shared out by all of
+ * their lengths: where a row's sums are split, and so how they are rounded, depends on the other streams' too. heads * buckets <= 2^30, and of tiles of sixteen rows and at least
+ * 32 keys there are fewer than 2^30.
  * What a row does not see, and what is behind a stream's length in its last page, does not reach it, however large, infinite or NaN.
  * small_cache_attention_workspace (host only) looks at sizes alone. */
 int small_cache_attention_workspace(const small_cache *c, const small_attn *a, size_t *bytes);

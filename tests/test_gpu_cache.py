@@ -386,6 +386,45 @@ def test_large_and_small_tokens_beside_each_other(kind):
     assert float((tokens_of(out, 1).double() - ref).abs().max()) <= 2.0 ** -17 * max(others, float(ref.abs().max()))
 
 
+@pytest.mark.parametrize("kind,N,D", [("float32", 300, 8), ("int8", 700, 16), ("bfloat16", 150, 136), ("int8", 257, 256)])
+def test_many_streams(kind, N, D):
+    """More streams than a workgroup has threads, of all lengths from none on."""
+    heads, kv, page, per = 2, 1, 16, 10
+    lengths = [(37 * n) % 161 for n in range(N)]
+    pages = sum(-(-x // page) for x in lengths) + 1
+    cache = S.PagedCache(pages, page, kv, D, kind=kind)
+    garbage(cache)
+    k, v, q = rand(1, N, kv, per * page, D), rand(2, N, kv, per * page, D), rand(3, N, heads, 1, D)
+    table, at = torch.full((N, per), -1, dtype=torch.int32), 0
+    for n, x in enumerate(lengths):
+        table[n, :-(-x // page)] = torch.arange(at, at + -(-x // page))
+        at += -(-x // page)
+    table = table.to(DEV)
+    cache.write(k.to(DEV), v.to(DEV), table, counts=ints(lengths))
+    out, lse = torch.full((N, heads, 1, D), math.nan, device=DEV), torch.full((N, heads, 1), math.nan, device=DEV)
+    S.CacheAttention(cache, N, 1, heads, per, Cb=D).run(q.to(DEV), out, table, ints(lengths), lse=lse)
+    kh, vh = held(tokens_of(k, kv), kind), held(tokens_of(v, kv), kind)
+    ref, ref_lse, size = attend(tokens_of(q, heads), kh, vh, lengths, None, D ** -0.5)
+    check_attention(tokens_of(out, heads), lse, ref, ref_lse, size, D, per * page, v)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_queries_that_are_not_finite(kind):
+    """... have no result but NaN, and the rows beside them theirs."""
+    form = (2, 2, 4, 2, 32, 32, 16, 6, [90, 70], None, "none", 0.0)
+    N, Sq, heads, kv, D, Cb, page, per, lengths, *_ = form
+    cache, table, q, k, v, more, reach, plan = attention_setup(form, kind)
+    out = torch.empty(q.shape, device=DEV)
+    plan.run(q.to(DEV), out, table, ints(lengths))
+    clean = tokens_of(out, heads)
+    q[0, 1, 0, 3], q[1, 2, 1, 0] = math.nan, math.inf
+    plan.run(q.to(DEV), out, table, ints(lengths))
+    got = tokens_of(out, heads)
+    hit = torch.zeros(N, Sq, heads, dtype=torch.bool)
+    hit[0, 0, 1] = hit[1, 1, 2] = True
+    assert torch.isnan(got[hit]).all() and torch.equal(got[~hit], clean[~hit])
+
+
 def test_captured_beside_eager_calls_and_another_stream():
     """A step of serving -- turn, write, attend -- captured once and replayed with new tokens, lengths and tables; every replay against the eager calls on another cache."""
     N, heads, kv, D, page, per = 3, 4, 2, 32, 16, 8
