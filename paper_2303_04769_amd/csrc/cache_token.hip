@@ -142,18 +142,19 @@ constexpr int group_waves(int DT) { return DT > 8 ? 2 : 4; }      // (their resu
 
 // Who does what: a round is a tile for each wave of a workgroup, a stream's tokens are R rounds (one at least) of each tile of rows of each key head, and the rounds
 // of all streams one behind the other are shared out evenly: streams differ in length, workgroups do not (64 streams of 2048 to 16384 tokens, 8 bits, in equal parts of each
-// stream: 86 us; in pieces of equal length: 93; evenly: 75). Known only on the device, where each workgroup sums up the lengths.
+// stream: 86 us; in pieces of equal length: 93; evenly: 73). Known only on the device, where each workgroup sums up the lengths.
 struct Rounds {
     int *prefix;                  // LDS: rounds in front of each of the chunk's streams; their sum, [threads]; the waves' sums, 4; what was found
+    int keys;                     // of a round, or of a piece of several
     int threads, units, all = 0, chunk = 0, before = 0, workgroups, each, more;
-    __device__ __forceinline__ static int of(const AttnArgs &a, int n, int keys) { return max(1, (max(0, min(a.lengths[n], a.Sk)) + keys - 1) / keys); }
+    __device__ __forceinline__ int of(const AttnArgs &a, int n) const { return max(1, (max(0, min(a.lengths[n], a.Sk)) + keys - 1) / keys); }
     // Sums of the streams from `first` on, a thread each.
-    __device__ __forceinline__ int scan(const AttnArgs &a, int first, int keys)
+    __device__ __forceinline__ int scan(const AttnArgs &a, int first)
     {
         int tid = threadIdx.x;
         asm volatile("" : "+v"(tid));                         // (or what only this needs is computed once and kept in registers throughout)
         const int lane = tid & 63, wave = tid >> 6, n = first + tid;
-        const int mine = n < a.N ? of(a, n, keys) * units : 0;
+        const int mine = n < a.N ? of(a, n) * units : 0;
         int sum = mine;
         for (int d = 1; d < 64; d <<= 1) {
             const int below = __shfl_up(sum, d);
@@ -173,10 +174,23 @@ struct Rounds {
         lds_barrier();
         return __builtin_amdgcn_readfirstlane(total);
     }
-    __device__ __forceinline__ Rounds(const AttnArgs &a, const CacheArgs &c, int keys, int *lds) : prefix(lds), threads(blockDim.x), units(a.head_sets * a.row_tiles)
+    __device__ __forceinline__ Rounds(const AttnArgs &a, const CacheArgs &c, int round, int *lds) : prefix(lds), keys(round), threads(blockDim.x), units(a.head_sets * a.row_tiles)
     {
-        for (int n = 0; n < a.N; n += threads) all += scan(a, n, keys);
-        const int most = (all + c.workgroups - 1) / c.workgroups;      // rounds of the longest: no more workgroups than that takes, for the fewest parts
+        for (int n = 0; n < a.N; n += threads) all += scan(a, n);
+        int most = (all + c.workgroups - 1) / c.workgroups;      // rounds of the longest: no more workgroups than that takes, for the fewest parts
+        // Few rounds each: in pieces of so many, if these are no more than the workgroups, so that none has to begin anew with another unit's queries and pages (16 streams of
+        // two key heads, 3001 tokens at most: 24.0 us instead of 26.4). Looking for it costs the time of one more sum, 1 us, which for longer shares it does not bring in.
+        if (most > 1 && most <= 4 && a.N <= threads && a.N * units <= c.workgroups) {
+            keys = round * most;
+            const int pieces = scan(a, 0);
+            if (pieces <= c.workgroups) {
+                all = pieces;
+                most = 1;
+            } else {
+                keys = round;
+                scan(a, 0);
+            }
+        }
         workgroups = (all + most - 1) / most;
         each = all / workgroups;
         more = all - each * workgroups;                       // the first so many have one more
@@ -188,15 +202,15 @@ struct Rounds {
         return x < longer ? x / (each + 1) : more + (x - longer) / each;
     }
     // The stream that has round x, and the first round of its first unit.
-    __device__ __forceinline__ int stream(const AttnArgs &a, int keys, int x, int *start)
+    __device__ __forceinline__ int stream(const AttnArgs &a, int x, int *start)
     {
         if (a.N > threads) {
             if (x < before) { chunk = 0; before = 0; }
-            int here = scan(a, chunk, keys);
+            int here = scan(a, chunk);
             while (x >= before + here) {
                 before += here;
                 chunk += threads;
-                here = scan(a, chunk, keys);
+                here = scan(a, chunk);
             }
         }
         const int y = x - before;
@@ -234,8 +248,8 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
     asm volatile("" : "+v"(lane));
     const int tid = 64 * wave + lane, m = lane & 15, g = lane >> 4;
     if (round >= stream_start + stream_rounds) {
-        n = rounds.stream(a, KR, round, &stream_start);
-        of_unit = __builtin_amdgcn_readfirstlane(Rounds::of(a, n, KR));
+        n = rounds.stream(a, round, &stream_start);
+        of_unit = __builtin_amdgcn_readfirstlane(rounds.of(a, n));
         stream_rounds = of_unit * rounds.units;
     }
     const int unit = (round - stream_start) / of_unit, lo_round = round - stream_start - unit * of_unit, hi_round = min(of_unit, lo_round + stop - round);
@@ -252,7 +266,7 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
     // keys up to the last one that a row of the tile can see, of these rounds
     const int last = a.by_Sq.div(r0) == a.by_Sq.div(r0 + rows - 1) ? r0 + rows - 1 - a.by_Sq.div(r0) * a.Sq : a.Sq - 1;
     const int hi = max(0, min(im.len, im.position(last) + 1));
-    const int begin = min(hi, lo_round * KR), end = min(hi, hi_round * KR);
+    const int begin = min(hi, lo_round * rounds.keys), end = min(hi, hi_round * rounds.keys);
     const int step = waves * KT, first = begin + wave * KT;
     int left = first < end ? (end - first + step - 1) / step : 0;
     const int stride = a.slopes ? -step : step;

@@ -408,6 +408,32 @@ def test_many_streams(kind, N, D):
     check_attention(tokens_of(out, heads), lse, ref, ref_lse, size, D, per * page, v)
 
 
+@pytest.mark.parametrize("kind,rounds,keys", [("float32", 100, 64), ("float32", 160, 64), ("bfloat16", 70, 128), ("bfloat16", 140, 128), ("int8", 70, 256)])
+def test_shares_of_a_few_rounds(kind, rounds, keys):
+    """Streams whose tokens are two to four times what all workgroups take at once: shared out in pieces that end with a stream's, or -- 140 -- in equal shares that do not."""
+    N, Sq, heads, kv, D, page = 12, 3, 2, 2, 128, 64
+    per = rounds * keys // page
+    lengths = [min(rounds * keys, x) for x in [0, 1, rounds * keys, keys + 1] + [rounds * keys * (n + 2) // 10 - 7 * n for n in range(8)]]
+    pages = sum(-(-x // page) for x in lengths) + 1
+    cache = S.PagedCache(pages, page, kv, D, kind=kind)
+    garbage(cache)
+    k, v, q = rand(1, N, kv, per * page, D), rand(2, N, kv, per * page, D), rand(3, N, heads, Sq, D)
+    table, at = torch.full((N, per), -1, dtype=torch.int32), 0
+    for n, x in enumerate(lengths):
+        table[n, :-(-x // page)] = torch.arange(at, at + -(-x // page)).flip(0)
+        at += -(-x // page)
+    table = table.to(DEV)
+    cache.write(k.to(DEV), v.to(DEV), table, counts=ints(lengths))
+    out, lse = torch.full((N, heads, Sq, D), math.nan, device=DEV), torch.full((N, heads, Sq), math.nan, device=DEV)
+    plan = S.CacheAttention(cache, N, Sq, heads, per, Cb=D)
+    plan.run(q.to(DEV), out, table, ints(lengths), lse=lse)
+    ref, ref_lse, size = attend(tokens_of(q, heads), held(tokens_of(k, kv), kind), held(tokens_of(v, kv), kind), lengths, None, D ** -0.5)
+    check_attention(tokens_of(out, heads), lse, ref, ref_lse, size, D, per * page, v)
+    again = torch.empty_like(out)
+    plan.run(q.to(DEV), again, table, ints(lengths))
+    assert torch.equal(out, again)
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_queries_that_are_not_finite(kind):
     """... have no result but NaN, and the rows beside them theirs."""
