@@ -632,21 +632,28 @@ __global__ void __launch_bounds__(256) cache_token_join(AttnArgs a, CacheArgs c,
     if (from == to) return;
     const size_t step = most_rows, first = (from + unit) * most_rows + (r - tile * most_rows);
     float top = -kInf, sum = 0.f, o[4] = {};
+    // (a wave's first part is asked for before the largest maximum is known)
+    float2 w = {};
+    float y[4] = {};
+    const auto fetch = [&](int s) {
+        w = a.part_ml[first + s * step];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            if (lane + 64 * k < a.D) y[k] = a.part_o[(first + s * step) * a.D + lane + 64 * k];
+    };
+    const int parts = to - from + 1;
+    if (wave < parts) fetch(wave);
 #pragma unroll 4
-    for (int s = lane; s <= to - from; s += 64) top = fmaxf(top, a.part_ml[first + s * step].x);
+    for (int s = lane; s < parts; s += 64) top = fmaxf(top, a.part_ml[first + s * step].x);
     for (int d = 32; d; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
     const float ref = top == -kInf ? 0.f : top;
 #pragma unroll 4
-    for (int s = wave; s <= to - from; s += 4) {
-        const float2 w = a.part_ml[first + s * step];
+    for (int s = wave; s < parts; s += 4) {
+        if (s != wave) fetch(s);
         const float x = w.y == 0.f ? 0.f : __builtin_amdgcn_exp2f(w.x - ref);      // (a part that saw no key)
         sum = fmaf(x, w.y, sum);
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            if (lane + 64 * k < a.D) {
-                const float y = a.part_o[(first + s * step) * a.D + lane + 64 * k];
-                o[k] += w.y == 0.f ? 0.f : x * y;
-            }
+        for (int k = 0; k < 4; ++k) o[k] += w.y == 0.f ? 0.f : x * y[k];
     }
 #pragma unroll
     for (int k = 0; k < 4; ++k) sums[wave][lane + 64 * k] = o[k];
