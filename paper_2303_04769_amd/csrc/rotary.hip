@@ -272,8 +272,13 @@ __global__ void __launch_bounds__(256) rotary_grad_join(const double *partial, f
     if (at >= all) return;
     const int f = at / each, e = at - f * each;
     double v = 0.0;
-#pragma unroll 4
-    for (int r = lane; r < rows; r += 64) v += partial[((size_t)f * rows + r) * each + e];
+    for (int r0 = lane; r0 < rows; r0 += 8 * 64) {            // (eight asked for at a time)
+        double x[8];
+#pragma unroll
+        for (int b = 0; b < 8; ++b) x[b] = r0 + 64 * b < rows ? partial[((size_t)f * rows + r0 + 64 * b) * each + e] : 0.0;
+#pragma unroll
+        for (int b = 0; b < 8; ++b) v += x[b];
+    }
     for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
     if (lane == 0) dfreq[at] = (float)v;
 }
