@@ -3,6 +3,7 @@
 // Bound by memory: activations in, codes out, or the other way. A workgroup has sixteen tokens that are neighbours in one page (or one token, where a call brings one a
 // stream), four channels of a token a thread, and goes through its share of the heads: queries that are only turned, keys, values. Sines are computed
 // once for all heads that share them. Values go through LDS, since a channel's tokens stand together in the cache: sixteen of them are a store of 16 to 64 bytes.
+// 8 x 8192 tokens of 8 heads of 64 read from 8-bit codes: 67 us, 5.0 TB/s; 4 x 4096 tokens turned and written: 36 us (a large copy: 4.9 TB/s).
 #include "cache.h"
 
 #include <type_traits>
@@ -235,7 +236,7 @@ __global__ void __launch_bounds__(1024) cache_write(StoreArgs a)
 }
 
 // Heads at a time: their loads are on their way together, and for values there is one wait of the workgroup instead of one for each (8 x 8192 tokens of 8 heads of 64, 8 bits:
-// one at a time 91 us, four 86).
+// one at a time 91 us, four 86, before results streamed past the caches).
 template <int KIND, bool VEC, int G, bool FAST>
 __global__ void __launch_bounds__(1024) cache_read(StoreArgs a)
 {
