@@ -428,6 +428,7 @@ constexpr float kSlack = 6.f;
 struct Reference {
     float at;
     bool seen;                    // a score was; until then `at` is what distances alone make of the nearest key, so that large ones cancel unrounded
+    Reference() = default;
     __device__ __forceinline__ Reference(const AttnArgs &a, const RowState &row, int begin, int end) : at(0.f), seen(false)
     {
         if (a.slopes) at = -row.slope * fabsf((float)(row.p - max(begin, min(row.p, end - 1))));

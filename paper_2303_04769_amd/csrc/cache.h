@@ -55,7 +55,7 @@ struct StoreArgs {
 };
 hipError_t launch_cache_write(const StoreArgs &a, bool vec, bool halves, hipStream_t s);                   // cache_store.hip
 hipError_t launch_cache_read(const StoreArgs &a, bool vec, hipStream_t s);
-struct TokenShape { int rows, keys, per_cu; };               // rows of a tile, keys of a round, workgroups that a compute unit runs at a time
+struct TokenShape { int rows, keys, per_cu; };               // rows of a unit, keys of a round, workgroups that a compute unit runs at a time
 TokenShape token_shape(int kind, int D, int rows);                                                          // cache_token.hip
 hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool joined, hipStream_t s);
 

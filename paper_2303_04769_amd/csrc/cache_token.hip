@@ -14,7 +14,7 @@
 #include "attn_tile.h"
 #include "cache.h"
 
-#include <initializer_list>
+#include <climits>
 
 namespace small {
 
@@ -137,8 +137,9 @@ __device__ __forceinline__ CacheArgs late_cache_args()
 }
 
 // Waves a SIMD that the registers are to leave room for, and waves of a workgroup: as many workgroups run at a time.
-constexpr int least_waves(int kind, int DT, int SP)
+constexpr int least_waves(int kind, int DT, int SP, int TR)
 {
+    if (TR == 2) return kind == SMALL_CACHE_F32 ? (DT <= 1 ? 4 : DT <= 3 ? 3 : 2) : DT <= 1 ? 3 : DT <= 4 ? 2 : 1;
     return kind == SMALL_CACHE_I8 ? (DT <= 4 && SP == 4 ? 3 : DT <= 5 || (DT <= 8 && SP > 1) ? 2 : 1) : DT <= 1 ? 5 : DT <= 3 ? 4 : DT == 4 ? 3 : DT <= 8 ? 2 : 1;
 }
 constexpr int group_waves(int DT) { return DT > 8 ? 2 : 4; }      // (their results fit 64 KB of LDS together)
@@ -231,11 +232,11 @@ constexpr int rounds_ints(int threads) { return threads + 6; }
 // SP: into how many columns a row's keys of a tile are shared out, where there are at most 16 / SP rows. Column m then has row m mod (16 / SP), and of the tile's results only
 // those of its share, m / (16 / SP): as if it were a row of its own, with a maximum, a sum and a result of its own, joined in the end. So the 16 columns
 // of single tokens' products are not mostly empty lanes in all that lies between the products.
-template <int KIND, int DT, int SP, bool ONE>
-__global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_waves_per_eu(least_waves(KIND, DT, SP)))) cache_token(AttnArgs args, CacheArgs cache_args)
+template <int KIND, int DT, int SP, bool ONE, int TR>
+__global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_waves_per_eu(least_waves(KIND, DT, SP, TR)))) cache_token(AttnArgs args, CacheArgs cache_args)
 {
     constexpr int B = cache_bytes(KIND), E = 16 / B, NB = E / 4, KT = 4 * E, NS = (16 * DT + KT - 1) / KT, DP = 16 * DT, H = E / 8 > 0 ? E / 8 : 1;
-    constexpr int NV = NB / SP, R = 16 / SP;                   // results of a lane that count, rows
+    constexpr int NV = NB / SP, R = 16 / SP, RU = R * TR;      // results of a lane that count, rows of a tile and of a unit
     constexpr int waves = group_waves(DT), KR = waves * KT;
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     __shared__ int rounds_lds[rounds_ints(64 * waves)];
@@ -259,14 +260,20 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
     const int key_head = unit / a.row_tiles, tile = unit - key_head * a.row_tiles;
     const bool whole = lo_round == 0 && hi_round == of_unit;
     round += hi_round - lo_round;
-    const int r0 = R * tile, rows = min(R, a.rows - r0), share = m / R;
-    const int r = r0 + min(m % R, rows - 1), hh = a.by_Sq.div(r), i = r - hh * a.Sq, head = key_head * a.group + hh;
+    const int r0 = RU * tile, rows = min(RU, a.rows - r0), share = m / R;
     ImageMask im(a, n);
     im.len = __builtin_amdgcn_readfirstlane(im.len);           // (the same for all lanes, which only scalar loads would tell the compiler: what follows from them is scalar)
     im.prefix = 0;
     im.first = a.first ? __builtin_amdgcn_readfirstlane(im.first) : im.len - a.Sq;
-    const RowState row(a, im, n, i, head);
-    // keys up to the last one that a row of the tile can see, of these rounds
+    RowState row_of[TR];                                       // of this lane's column in each tile
+    int place_of_row[TR];
+#pragma unroll
+    for (int t = 0; t < TR; ++t) {
+        const int r = r0 + min(R * t + m % R, rows - 1), hh = a.by_Sq.div(r);
+        place_of_row[t] = r - hh * a.Sq;
+        row_of[t] = RowState(a, im, n, place_of_row[t], key_head * a.group + hh);
+    }
+    // keys up to the last one that a row of the unit can see, of these rounds
     const int last = a.by_Sq.div(r0) == a.by_Sq.div(r0 + rows - 1) ? r0 + rows - 1 - a.by_Sq.div(r0) * a.Sq : a.Sq - 1;
     const int hi = max(0, min(im.len, im.position(last) + 1));
     const int begin = min(hi, lo_round * rounds.keys), end = min(hi, hi_round * rounds.keys);
@@ -353,38 +360,50 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
         fetch_v(j0);
     }
     // queries, times what makes their products scores (or, with a cap, what the tanh is taken of): floats, or their parts
-    floatx4 qf[KIND == SMALL_CACHE_F32 ? DT : 1];
-    Parts3 qp[KIND == SMALL_CACHE_F32 ? 1 : 2 * NS * H];
-    {
-        const float *token = token_at(a.q, a.qs, n, i);
+    floatx4 qf[TR][KIND == SMALL_CACHE_F32 ? DT : 1];
+    Parts3 qp[TR][KIND == SMALL_CACHE_F32 ? 1 : 2 * NS * H];
+#pragma unroll
+    for (int t = 0; t < TR; ++t) {
+        const float *token = token_at(a.q, a.qs, n, place_of_row[t]);
         const float in = a.cap > 0.f ? a.scale / a.cap : a.scale * kLog2e;
-        const auto quad = [&](int d) { return (a.vec ? load_quad<true>(a, a.qs, token, head * a.D, d) : load_quad<false>(a, a.qs, token, head * a.D, d)) * in; };
+        const auto quad = [&](int d) { return (a.vec ? load_quad<true>(a, a.qs, token, row_of[t].head * a.D, d) : load_quad<false>(a, a.qs, token, row_of[t].head * a.D, d)) * in; };
         if constexpr (KIND == SMALL_CACHE_F32) {
 #pragma unroll
-            for (int s = 0; s < DT; ++s) qf[s] = quad(16 * s + 4 * g);
+            for (int s = 0; s < DT; ++s) qf[t][s] = quad(16 * s + 4 * g);
         } else {
 #pragma unroll
             for (int s = 0; s < NS; ++s)
 #pragma unroll
-                for (int h = 0; h < 2 * H; ++h) qp[2 * H * s + h] = parts_of(quad(KT * s + E * g + 4 * h));
+                for (int h = 0; h < 2 * H; ++h) qp[t][2 * H * s + h] = parts_of(quad(KT * s + E * g + 4 * h));
         }
     }
-    const float far_lo = a.table ? bias_gather(a, head, 0) : 0.f, far_hi = a.table ? bias_gather(a, head, 2 * a.reach) : 0.f;
-    floatx4 o[DT] = {};
-    Reference top(a, row, begin, end);
-    float sum = 0.f;
+    float far_lo[TR], far_hi[TR], sum[TR] = {};
+    floatx4 o[TR][DT] = {};
+#pragma unroll
+    for (int t = 0; t < TR; ++t) {
+        far_lo[t] = a.table ? bias_gather(a, row_of[t].head, 0) : 0.f;
+        far_hi[t] = a.table ? bias_gather(a, row_of[t].head, 2 * a.reach) : 0.f;
+    }
+    Reference top[TR];
+#pragma unroll
+    for (int t = 0; t < TR; ++t) top[t] = Reference(a, row_of[t], begin, end);
     if (left > 1) ask_pages(j0 + stride);
     for (; left; --left, j0 += stride) {
         const int value0 = j0 + E * g, key0 = value0 + 4 * NV * share;        // of this lane's values, and of its scores: key0 + 4 b + e
         const bool no_page = v_page < 0;
         // a learned bias: all buckets are asked for, then all biases -- unless the tile's keys are all at one end of the reach, as most of a long cache is
-        bool near = false;
-        float far = 0.f, bias[NV][4];
-        if (a.table) {
+        bool near[TR];
+        float far[TR], bias[TR][NV][4];
+#pragma unroll
+        for (int t = 0; t < TR; ++t) {
+            const RowState &row = row_of[t];
+            near[t] = false;
+            far[t] = 0.f;
+            if (!a.table) continue;
             const bool all_lo = __all(j0 + KT - 1 - row.code <= -a.reach), all_hi = __all(j0 - row.code >= a.reach);
-            near = !all_lo && !all_hi;
-            far = all_lo ? far_lo : all_hi ? far_hi : 0.f;
-            if (near) {
+            near[t] = !all_lo && !all_hi;
+            far[t] = all_lo ? far_lo[t] : all_hi ? far_hi[t] : 0.f;
+            if (near[t]) {
                 int bucket[NV][4];
 #pragma unroll
                 for (int b = 0; b < NV; ++b)
@@ -393,75 +412,47 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
 #pragma unroll
                 for (int b = 0; b < NV; ++b)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) bias[b][e] = at_bytes(a.table, 4u * (unsigned)(head * a.buckets + max(0, min(bucket[b][e], a.buckets - 1))));
+                    for (int e = 0; e < 4; ++e) bias[t][b][e] = at_bytes(a.table, 4u * (unsigned)(row.head * a.buckets + max(0, min(bucket[b][e], a.buckets - 1))));
             }
         }
-        floatx4 all[NB] = {};
+        floatx4 all[TR][NB] = {};
 #pragma unroll
         for (int x = 0; x < NS; ++x)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 if constexpr (KIND == SMALL_CACHE_F32) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) all[b] = mfma(__uint_as_float(kx[b][x][e]), qf[x][e], all[b]);
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int t = 0; t < TR; ++t) all[t][b] = mfma(__uint_as_float(kx[b][x][e]), qf[t][x][e], all[t][b]);
                 } else {
 #pragma unroll
                     for (int h = 0; h < H; ++h) {
                         uintx4 k = kx[b][x];
                         if constexpr (KIND == SMALL_CACHE_I8) k = widened(kx[b][x][2 * h], kx[b][x][2 * h + 1]);
-                        const Parts3 &q0 = qp[2 * (H * x + h)], &q1 = qp[2 * (H * x + h) + 1];
 #pragma unroll
-                        for (int p = 2; p >= 0; --p) all[b] = mfma_bf16(k, words(q0.p[p], q1.p[p]), all[b]);
+                        for (int p = 2; p >= 0; --p)
+#pragma unroll
+                            for (int t = 0; t < TR; ++t) all[t][b] = mfma_bf16(k, words(qp[t][2 * (H * x + h)].p[p], qp[t][2 * (H * x + h) + 1].p[p]), all[t][b]);
                     }
                 }
             }
-        floatx4 s[NV];
+        floatx4 scores[TR][NV];
 #pragma unroll
-        for (int b = 0; b < NV; ++b) {
-            s[b] = all[b];
+        for (int t = 0; t < TR; ++t)
 #pragma unroll
-            for (int x = 1; x < SP; ++x) s[b] = share == x ? all[x * NV + b] : s[b];
-            if constexpr (KIND == SMALL_CACHE_I8) s[b] *= ksc[b];
-        }
+            for (int b = 0; b < NV; ++b) {
+                scores[t][b] = all[t][b];
+#pragma unroll
+                for (int x = 1; x < SP; ++x) scores[t][b] = share == x ? all[t][x * NV + b] : scores[t][b];
+                if constexpr (KIND == SMALL_CACHE_I8) scores[t][b] *= ksc[b];
+            }
         if (left > 1) {
             const int v_now = v_page;
             k_page = page_in(k_in);
             v_page = page_in(v_in);                            // (key scales stand at the values' keys)
             fetch_k(j0 + stride);
             v_page = v_now;
-        }
-        const float base = far - top.at;
-        if (a.cap > 0.f) {
-            tanh_all(s);
-            const float out = a.cap * kLog2e;
-#pragma unroll
-            for (int b = 0; b < NV; ++b) s[b] *= out;
-        }
-        if (a.slopes) {
-            const float from = (float)(row.p - key0);
-#pragma unroll
-            for (int b = 0; b < NV; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] += fmaf(-row.slope, fabsf(from - (float)(4 * b + e)), base);
-        } else {
-#pragma unroll
-            for (int b = 0; b < NV; ++b) s[b] += base;
-        }
-        if (near)
-#pragma unroll
-            for (int b = 0; b < NV; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[b][e] += bias_log2(bias[b][e]);
-        const int bound = min(row.bound, end);
-        if (!__all((j0 + KT <= bound) & !no_page)) {
-#pragma unroll
-            for (int b = 0; b < NV; ++b)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool seen = (key0 + 4 * b + e < bound) & !no_page;
-                    s[b][e] = seen ? s[b][e] : -kInf;
-                    if constexpr (KIND == SMALL_CACHE_I8) vsc[b][e] = seen ? vsc[b][e] : 0.f;              // (the scale of a hidden token may be anything)
-                }
         }
         if (KIND != SMALL_CACHE_I8 && (j0 + KT > end || __any(no_page))) {       // what stands behind the last key, or in no page of the stream's, becomes zeros
 #pragma unroll
@@ -472,42 +463,85 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
                     else vx[d][x] &= no_page ? 0u : value0 + 2 * x + 1 < end ? 0xffffffffu : value0 + 2 * x < end ? 0xffffu : 0u;
                 }
         }
-        raise_top(s, top, sum, o);
 #pragma unroll
-        for (int b = 0; b < NV; ++b)
+        for (int t = 0; t < TR; ++t) {
+            const RowState &row = row_of[t];
+            floatx4(&s)[NV] = scores[t];
+            floatx4 weight[NV];                                // of codes' values, zero where the row does not see them
+            if constexpr (KIND == SMALL_CACHE_I8) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
-                sum += s[b][e];
+                for (int b = 0; b < NV; ++b) weight[b] = vsc[b];
             }
-        if constexpr (KIND == SMALL_CACHE_F32) {
+            const float base = far[t] - top[t].at;
+            if (a.cap > 0.f) {
+                tanh_all(s);
+                const float out = a.cap * kLog2e;
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] = mfma(__uint_as_float(vx[d][e]), s[0][e], o[d]);
-        } else {
-            Parts3 w[NV];
-#pragma unroll
-            for (int b = 0; b < NV; ++b) {
-                if constexpr (KIND == SMALL_CACHE_I8) s[b] *= vsc[b];
-                w[b] = parts_of(s[b]);
+                for (int b = 0; b < NV; ++b) s[b] *= out;
             }
+            if (a.slopes) {
+                const float from = (float)(row.p - key0);
 #pragma unroll
-            for (int h = 0; h < H; ++h) {
-                uintx4 p[3];                                   // (zeros at the other shares' keys)
+                for (int b = 0; b < NV; ++b)
 #pragma unroll
-                for (int x = 0; x < 3; ++x)
+                    for (int e = 0; e < 4; ++e) s[b][e] += fmaf(-row.slope, fabsf(from - (float)(4 * b + e)), base);
+            } else {
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
-                        const int b = 2 * h + y / 2;
-                        p[x][y] = SP == 1 || share == b / NV ? w[b % NV].p[x][y & 1] : 0u;
+                for (int b = 0; b < NV; ++b) s[b] += base;
+            }
+            if (near[t])
+#pragma unroll
+                for (int b = 0; b < NV; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[b][e] += bias_log2(bias[t][b][e]);
+            const int bound = min(row.bound, end);
+            if (!__all((j0 + KT <= bound) & !no_page)) {
+#pragma unroll
+                for (int b = 0; b < NV; ++b)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool seen = (key0 + 4 * b + e < bound) & !no_page;
+                        s[b][e] = seen ? s[b][e] : -kInf;
+                        if constexpr (KIND == SMALL_CACHE_I8) weight[b][e] = seen ? weight[b][e] : 0.f;              // (the scale of a hidden token may be anything)
                     }
+            }
+            raise_top(s, top[t], sum[t], o[t]);
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    uintx4 v = vx[d];
-                    if constexpr (KIND == SMALL_CACHE_I8) v = widened(vx[d][2 * h], vx[d][2 * h + 1]);
+            for (int b = 0; b < NV; ++b)
 #pragma unroll
-                    for (int x = 2; x >= 0; --x) o[d] = mfma_bf16(v, p[x], o[d]);
+                for (int e = 0; e < 4; ++e) {
+                    s[b][e] = __builtin_amdgcn_exp2f(s[b][e]);
+                    sum[t] += s[b][e];
+                }
+            if constexpr (KIND == SMALL_CACHE_F32) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[t][d] = mfma(__uint_as_float(vx[d][e]), s[0][e], o[t][d]);
+            } else {
+                Parts3 w[NV];
+#pragma unroll
+                for (int b = 0; b < NV; ++b) {
+                    if constexpr (KIND == SMALL_CACHE_I8) s[b] *= weight[b];
+                    w[b] = parts_of(s[b]);
+                }
+#pragma unroll
+                for (int h = 0; h < H; ++h) {
+                    uintx4 p[3];                                   // (zeros at the other shares' keys)
+#pragma unroll
+                    for (int x = 0; x < 3; ++x)
+#pragma unroll
+                        for (int y = 0; y < 4; ++y) {
+                            const int b = 2 * h + y / 2;
+                            p[x][y] = SP == 1 || share == b / NV ? w[b % NV].p[x][y & 1] : 0u;
+                        }
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        uintx4 v = vx[d];
+                        if constexpr (KIND == SMALL_CACHE_I8) v = widened(vx[d][2 * h], vx[d][2 * h + 1]);
+#pragma unroll
+                        for (int x = 2; x >= 0; --x) o[t][d] = mfma_bf16(v, p[x], o[t][d]);
+                    }
                 }
             }
         }
@@ -517,15 +551,20 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
             if (left > 2) ask_pages(j0 + 2 * stride);
         }
     }
-    sum = column_sum(sum);
-    float most = top.maximum();
+    float most[TR];
+#pragma unroll
+    for (int t = 0; t < TR; ++t) {
+        sum[t] = column_sum(sum[t]);
+        most[t] = top[t].maximum();
+    }
     if constexpr (SP > 1) {                                    // a row's shares: columns 16 / SP apart, in the same sixteen lanes
-        float all = most;
+        static_assert(TR == 1, "rows that fill the columns have no shares");
+        float all = most[0];
         all = fmaxf(all, __int_as_float(dpp_of<0x128>(__float_as_int(all))));            // row_ror:8
         if constexpr (SP == 4) all = fmaxf(all, __int_as_float(dpp_of<0x124>(__float_as_int(all))));
-        const float w = sum == 0.f ? 0.f : __builtin_amdgcn_exp2f(most - all);            // (a share that saw no key)
+        const float w = sum[0] == 0.f ? 0.f : __builtin_amdgcn_exp2f(most[0] - all);            // (a share that saw no key)
         const auto over = [&](float x) {
-            x = sum == 0.f ? 0.f : x * w;
+            x = sum[0] == 0.f ? 0.f : x * w;
             x += __int_as_float(dpp_of<0x128>(__float_as_int(x)));
             if constexpr (SP == 4) x += __int_as_float(dpp_of<0x124>(__float_as_int(x)));
             return x;
@@ -533,92 +572,102 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) o[d][e] = over(o[d][e]);
-        sum = over(sum);
-        most = all;
+            for (int e = 0; e < 4; ++e) o[0][d][e] = over(o[0][d][e]);
+        sum[0] = over(sum[0]);
+        most[0] = all;
     }
 
-    // join the waves: [wave][row][DP] and [wave][row] (maximum, sum)
+    // join the waves: [wave][row][DP] and [wave][row] (maximum, sum), a tile of rows at a time
     const AttnArgs z = late_args();
     const CacheArgs zc = late_cache_args();
-    const size_t all_units = (size_t)n * rounds.units + unit, part = (w_id + all_units) * R;       // (workgroups and units both only grow: a place of its own for each pair)
+    const size_t all_units = (size_t)n * rounds.units + unit, unit_part = (w_id + all_units) * RU;       // (workgroups and units both only grow: a place of its own for each pair)
     if (zc.units && lo_round == 0 && tid == 0) zc.units[all_units] = int2{w_id, rounds.owner(round - (hi_round - lo_round) + of_unit - 1)};      // who has parts of it, for the join
     constexpr int LP = DP + 4;                                 // (rows of lanes that write at a time in different banks)
-    float *const lo_ = token_lds;
-    float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * rows * LP);
-    int *const flags = reinterpret_cast<int *>(ml + waves * rows);
-    if (m < rows) {
-        const int mine = wave * rows + m;
+#pragma clang loop unroll(disable)
+    for (int t = 0; t < TR; ++t) {
+        const int r0 = RU * tile + R * t, rows = min(R, z.rows - r0);
+        if (rows <= 0) break;
+        const size_t part = unit_part + R * t;
+        float *const lo_ = token_lds;
+        float2 *const ml = reinterpret_cast<float2 *>(token_lds + waves * rows * LP);
+        int *const flags = reinterpret_cast<int *>(ml + waves * rows);
+        const auto put = [&](const floatx4(&of)[DT], float maximum, float total) {
+            const int mine = wave * rows + m;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + mine * LP + 16 * d + 4 * g) = o[d];
-        if (g == 0) ml[mine] = float2{most, sum};
-    }
-    if (tid < 17) flags[tid] = 0;                             // of rows, and of any
-    lds_barrier();
-    constexpr int QD = DP / 4;
-    for (int e = tid; e < rows * QD; e += 64 * waves) {
-        const int rr = e / QD, d = (e - rr * QD) * 4;
-        float all = -kInf, total = 0.f;
+            for (int d = 0; d < DT; ++d) *reinterpret_cast<floatx4 *>(lo_ + mine * LP + 16 * d + 4 * g) = of[d];
+            if (g == 0) ml[mine] = float2{maximum, total};
+        };
+        if (m < rows) {
+            if (t == 0) put(o[0], most[0], sum[0]);
+            else put(o[TR - 1], most[TR - 1], sum[TR - 1]);
+        }
+        if (tid < 17) flags[tid] = 0;                             // of rows, and of any
+        lds_barrier();
+        constexpr int QD = DP / 4;
+        for (int e = tid; e < rows * QD; e += 64 * waves) {
+            const int rr = e / QD, d = (e - rr * QD) * 4;
+            float all = -kInf, total = 0.f;
 #pragma unroll 4
-        for (int w = 0; w < waves; ++w) all = fmaxf(all, ml[w * rows + rr].x);
-        const float ref = all == -kInf ? 0.f : all;
-        floatx4 y = {};
+            for (int w = 0; w < waves; ++w) all = fmaxf(all, ml[w * rows + rr].x);
+            const float ref = all == -kInf ? 0.f : all;
+            floatx4 y = {};
 #pragma unroll 4
-        for (int w = 0; w < waves; ++w) {
-            const float2 p = ml[w * rows + rr];
-            const floatx4 w4 = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * LP + d);
-            const float f = __builtin_amdgcn_exp2f(p.x - ref);
-            total += p.y == 0.f ? 0.f : f * p.y;
+            for (int w = 0; w < waves; ++w) {
+                const float2 p = ml[w * rows + rr];
+                const floatx4 w4 = *reinterpret_cast<const floatx4 *>(lo_ + (w * rows + rr) * LP + d);
+                const float f = __builtin_amdgcn_exp2f(p.x - ref);
+                total += p.y == 0.f ? 0.f : f * p.y;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * w4[x];       // (a wave that saw no key)
-        }
-        if (d < z.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = flags[16] = 1;
-        const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
-        if (!whole && z.D % 4 == 0) {
-            if (d < z.D) *reinterpret_cast<floatx4 *>(z.part_o + (part + rr) * z.D + d) = y;
-            if (d == 0) z.part_ml[part + rr] = float2{all, total};
-        } else if (!whole) {
+                for (int x = 0; x < 4; ++x) y[x] += p.y == 0.f ? 0.f : f * w4[x];       // (a wave that saw no key)
+            }
+            if (d < z.D && (y.x != y.x || y.y != y.y || y.z != y.z || y.w != y.w)) flags[rr] = flags[16] = 1;
+            const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
+            if (!whole && z.D % 4 == 0) {
+                if (d < z.D) *reinterpret_cast<floatx4 *>(z.part_o + (part + rr) * z.D + d) = y;
+                if (d == 0) z.part_ml[part + rr] = float2{all, total};
+            } else if (!whole) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
-                if (d + x < z.D) z.part_o[(part + rr) * z.D + d + x] = y[x];
-            if (d == 0) z.part_ml[part + rr] = float2{all, total};
-        } else {
-            const floatx4 all_of = total == 0.f ? floatx4{} : y * (1.f / total);
-            float *token = const_cast<float *>(token_at(z.o, z.os, n, i2));
-            if (z.vec) store_quad<true>(z, z.os, token, head2 * z.D, d, all_of);
-            else store_quad<false>(z, z.os, token, head2 * z.D, d, all_of);
-            if (z.lse && d == 0) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
+                for (int x = 0; x < 4; ++x)
+                    if (d + x < z.D) z.part_o[(part + rr) * z.D + d + x] = y[x];
+                if (d == 0) z.part_ml[part + rr] = float2{all, total};
+            } else {
+                const floatx4 all_of = total == 0.f ? floatx4{} : y * (1.f / total);
+                float *token = const_cast<float *>(token_at(z.o, z.os, n, i2));
+                if (z.vec) store_quad<true>(z, z.os, token, head2 * z.D, d, all_of);
+                else store_quad<false>(z, z.os, token, head2 * z.D, d, all_of);
+                if (z.lse && d == 0) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (all + __builtin_amdgcn_logf(total)) * kLn2;
+            }
         }
-    }
-    lds_barrier();
-    if (!__builtin_amdgcn_readfirstlane(flags[16])) {
-        lds_barrier();                                         // (what the join read is free)
-        continue;
-    }
-    __syncthreads();                                           // (stores of these rows have come to pass)
-    for (int rr = wave; rr < rows; rr += waves) {
-        if (!flags[rr]) continue;
-        const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
-        // (a query that is not finite itself has no other result, and may be padding)
-        const float *query = token_at(z.q, z.qs, n, i2);
-        bool fine = true;
-        for (int d = lane; d < z.D; d += 64) fine &= fabsf(query[channel_at(z, z.qs, head2 * z.D + d)]) < kInf;
-        if (!__all(fine)) continue;
-        const RowState again(z, im, n, i2, head2);
-        float y[4], most, total;
-        attend_cached_row<KIND>(z, zc, again, n, i2, key_head, begin, end, y, most, total);
-        const float inv = total == 0.f ? 0.f : 1.f / total;
-        for (int x = 0; x < 4; ++x) {
-            const int d = lane + 64 * x;
-            if (d >= z.D) continue;
-            if (!whole) z.part_o[(part + rr) * z.D + d] = y[x];
-            else const_cast<float *>(token_at(z.o, z.os, n, i2))[channel_at(z, z.os, head2 * z.D + d)] = total == 0.f ? 0.f : y[x] * inv;
+        lds_barrier();
+        if (!__builtin_amdgcn_readfirstlane(flags[16])) {
+            lds_barrier();                                         // (what the join read is free)
+            continue;
         }
-        if (lane) continue;
-        if (!whole) z.part_ml[part + rr] = float2{most, total};
-        else if (z.lse) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (most + __builtin_amdgcn_logf(total)) * kLn2;
+        __syncthreads();                                           // (stores of these rows have come to pass)
+        for (int rr = wave; rr < rows; rr += waves) {
+            if (!flags[rr]) continue;
+            const int h2 = z.by_Sq.div(r0 + rr), i2 = r0 + rr - h2 * z.Sq, head2 = key_head * z.group + h2;
+            // (a query that is not finite itself has no other result, and may be padding)
+            const float *query = token_at(z.q, z.qs, n, i2);
+            bool fine = true;
+            for (int d = lane; d < z.D; d += 64) fine &= fabsf(query[channel_at(z, z.qs, head2 * z.D + d)]) < kInf;
+            if (!__all(fine)) continue;
+            const RowState again(z, im, n, i2, head2);
+            float y[4], most, total;
+            attend_cached_row<KIND>(z, zc, again, n, i2, key_head, begin, end, y, most, total);
+            const float inv = total == 0.f ? 0.f : 1.f / total;
+            for (int x = 0; x < 4; ++x) {
+                const int d = lane + 64 * x;
+                if (d >= z.D) continue;
+                if (!whole) z.part_o[(part + rr) * z.D + d] = y[x];
+                else const_cast<float *>(token_at(z.o, z.os, n, i2))[channel_at(z, z.os, head2 * z.D + d)] = total == 0.f ? 0.f : y[x] * inv;
+            }
+            if (lane) continue;
+            if (!whole) z.part_ml[part + rr] = float2{most, total};
+            else if (z.lse) z.lse[((size_t)n * z.heads + head2) * z.Sq + i2] = total == 0.f ? -kInf : (most + __builtin_amdgcn_logf(total)) * kLn2;
+        }
+        __syncthreads();                                           // (what the join read is free)
     }
-    __syncthreads();                                           // (what the join read is free)
     }
 }
 
@@ -684,44 +733,55 @@ int token_tiles(int D)
     return 16;
 }
 
-template <int KIND, int SP, bool ONE>
+// Two tiles of rows in a unit: a tile of keys and values is loaded once for both. They halve the loads of calls with three tiles or more and leave room for fewer waves (8 streams
+// of 4096 tokens, 56 rows: floats of 64 channels 50 -> 40 us, bfloat16 33 -> 26 and of 128 channels 43 -> 35). With two tiles the waves lost cost as much but for small heads of
+// bfloat16 (32 streams, 20 rows: floats 36 -> 42, bfloat16 25.5 -> 24, of 128 channels 41 -> 47), and codes taken apart need the registers themselves (56 rows 25 -> 28.5).
+constexpr bool two_tiles(int kind, int DT, int rows)
+{
+    return kind == SMALL_CACHE_F32 ? DT <= 6 && rows > 32 : kind == SMALL_CACHE_BF16 && (DT <= 4 ? rows > 16 : DT <= 8 && rows > 32);
+}
+
+template <int KIND, int SP, bool ONE, int TR>
 hipError_t token_form(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
 {
     const int rows = a.rows < 16 / SP ? a.rows : 16 / SP;
     switch (token_tiles(a.D)) {
 #define TOKEN(dt) \
     case dt: \
-        hipLaunchKernelGGL((cache_token<KIND, dt, SP, ONE>), dim3((unsigned)c.workgroups), dim3(64 * group_waves(dt)), (size_t)group_waves(dt) * rows * (16 * dt + 6) * 4 + 80, s, a, c); \
+        hipLaunchKernelGGL((cache_token<KIND, dt, SP, ONE, (two_tiles(KIND, dt, INT_MAX) ? TR : 1)>), dim3((unsigned)c.workgroups), dim3(64 * group_waves(dt)), (size_t)group_waves(dt) * rows * (16 * dt + 6) * 4 + 80, s, a, c); \
         break;
         TOKEN(1) TOKEN(2) TOKEN(3) TOKEN(4) TOKEN(5) TOKEN(6) TOKEN(8) TOKEN(16)
 #undef TOKEN
     }
     return hipGetLastError();
 }
-template <int KIND, int SP>
+template <int KIND, int SP, int TR>
 hipError_t token_pages(const AttnArgs &a, const CacheArgs &c, hipStream_t s)
 {
     if constexpr (KIND != SMALL_CACHE_F32)
-        if ((1 << c.shift) < 64 / cache_bytes(KIND)) return token_form<KIND, SP, false>(a, c, s);
-    return token_form<KIND, SP, true>(a, c, s);
+        if ((1 << c.shift) < 64 / cache_bytes(KIND)) return token_form<KIND, SP, false, TR>(a, c, s);
+    return token_form<KIND, SP, true, TR>(a, c, s);
 }
 
 }  // namespace
 
 TokenShape token_shape(int kind, int D, int rows)
 {
-    const int shares = token_shares(kind, rows), dt = token_tiles(D), waves = group_waves(dt);
-    return TokenShape{16 / shares, waves * 64 / cache_bytes(kind), least_waves(kind, dt, shares) * 4 / waves};
+    const int shares = token_shares(kind, rows), dt = token_tiles(D), waves = group_waves(dt), tiles = two_tiles(kind, dt, rows) ? 2 : 1;
+    return TokenShape{16 / shares * tiles, waves * 64 / cache_bytes(kind), least_waves(kind, dt, shares, tiles) * 4 / waves};
 }
 
 hipError_t launch_cache_token(const AttnArgs &a, const CacheArgs &c, bool joined, hipStream_t s)
 {
-    const int shares = token_shares(c.kind, a.rows);
+    const int shares = token_shares(c.kind, a.rows), two = two_tiles(c.kind, token_tiles(a.D), a.rows);
     hipError_t e;
     switch (c.kind) {
-    case SMALL_CACHE_F32: e = token_pages<SMALL_CACHE_F32, 1>(a, c, s); break;
-    case SMALL_CACHE_BF16: e = shares == 2 ? token_pages<SMALL_CACHE_BF16, 2>(a, c, s) : token_pages<SMALL_CACHE_BF16, 1>(a, c, s); break;
-    default: e = shares == 4 ? token_pages<SMALL_CACHE_I8, 4>(a, c, s) : shares == 2 ? token_pages<SMALL_CACHE_I8, 2>(a, c, s) : token_pages<SMALL_CACHE_I8, 1>(a, c, s);
+    case SMALL_CACHE_F32: e = two ? token_pages<SMALL_CACHE_F32, 1, 2>(a, c, s) : token_pages<SMALL_CACHE_F32, 1, 1>(a, c, s); break;
+    case SMALL_CACHE_BF16:
+        e = two ? token_pages<SMALL_CACHE_BF16, 1, 2>(a, c, s) : shares == 2 ? token_pages<SMALL_CACHE_BF16, 2, 1>(a, c, s) : token_pages<SMALL_CACHE_BF16, 1, 1>(a, c, s);
+        break;
+    default:
+        e = shares == 4 ? token_pages<SMALL_CACHE_I8, 4, 1>(a, c, s) : shares == 2 ? token_pages<SMALL_CACHE_I8, 2, 1>(a, c, s) : token_pages<SMALL_CACHE_I8, 1, 1>(a, c, s);
     }
     if (e != hipSuccess || !joined) return e;
     const TokenShape shape = token_shape(c.kind, a.D, a.rows);

@@ -304,6 +304,46 @@ def test_attention(form, kind):
     assert torch.equal(out, again)
 
 
+MANY_ROWS = [
+    # N, Sq, heads, kv, D, Cb, page, per, lengths, first, bias, cap: 17 rows of a key head and more
+    (2, 17, 1, 1, 16, 16, 16, 9, [144, 11], None, "none", 0.0),
+    (2, 5, 8, 2, 64, 16, 32, 8, [250, 3], None, "slopes", 30.0),
+    (1, 33, 1, 1, 32, 32, 16, 6, [90], None, "buckets", 0.0),
+    (2, 11, 6, 2, 64, 384, 64, 5, [320, 7], None, "buckets", 0.0),
+    (2, 9, 8, 2, 80, 16, 16, 13, [208, 100], [150, 40], "slopes", 0.0),
+    (1, 16, 8, 2, 96, 96, 64, 9, [576], None, "none", 15.0),
+    (2, 40, 3, 3, 128, 128, 32, 8, [256, 50], None, "slopes", 0.0),
+    (1, 7, 8, 1, 120, 8, 16, 60, [951], None, "buckets", 20.0),
+    (1, 50, 1, 1, 256, 256, 16, 5, [75], None, "none", 0.0),
+    (3, 7, 16, 2, 40, 8, 64, 90, [5760, 0, 4001], None, "slopes", 0.0),
+]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("form", MANY_ROWS)
+def test_many_rows(form, kind):
+    test_attention(form, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows_around_an_infinite_value(kind, D):
+    """The third token from the end holds an infinite value: rows that do not see it, in both tiles of a unit, have the results of a cache without it."""
+    form = (2, 9, 8, 2, D, 16, 16, 8, [128, 61], None, "none", 0.0)
+    N, Sq, heads, kv, D, Cb, page, per, lengths, *_ = form
+    cache, table, q, k, v, more, reach, plan = attention_setup(form, kind)
+    out = torch.empty(q.shape, device=DEV)
+    plan.run(q.to(DEV), out, table, ints(lengths))
+    clean = tokens_of(out, heads)
+    one_k, one_v = rand(8, N, kv, 1, D), torch.full((N, kv, 1, D), math.inf)
+    cache.write(one_k.to(DEV), one_v.to(DEV), table, first=ints([x - 3 for x in lengths]))
+    plan.run(q.to(DEV), out, table, ints(lengths))
+    got = tokens_of(out, heads)
+    assert not torch.isfinite(got[:, Sq - 3:]).any()
+    # (in another order: sums of up to 128 weights below 1 and their products, each rounded to 24 bits, on both sides)
+    assert float((got - clean)[:, : Sq - 3].abs().max()) <= 2 * (D + 16 + 2 * 128) * 2.0 ** -24 * max(1.0, D ** 0.5) * float(v.abs().max())
+
+
 @pytest.mark.parametrize("kind", KINDS)
 def test_hidden_tokens_reach_no_row(kind):
     """A token that holds NaN and infinities, seen by the later of three new tokens only; pages of another stream's that hold them too."""
