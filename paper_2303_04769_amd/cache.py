@@ -220,7 +220,7 @@ class PagedCache:
 
     def write(self, k, v, pages, first=None, counts=None, rotary=None, freq=None, positions=None, q=None, q_out=None, stream=None):
         """Tokens i < counts[n] of k and v into the cache at positions first[n] + i of stream n. With a Rotary plan of these sizes (and its freq) keys are turned on the way,
-        and queries q into q_out (in place where it is None)."""
+        and queries q into q_out (in place where it is None). No two tokens of a call may have one place: it would hold parts of both."""
         if stream is None:
             rc = _fast().cache_write(self.record, k, v, pages, first, counts, None if rotary is None else rotary.record, freq, positions, q, q_out, None)
             if rc is not None:

@@ -272,8 +272,8 @@ int token_check(const small_cache &c, const small_attn &a)
     if (a.table && (a.reach < 0 || a.reach > kFar || a.buckets < 1 || (double)a.heads * a.buckets > 1 << 30)) return SMALL_ERR_SHAPE;
     return SMALL_OK;
 }
-// How the calls of these sizes share out their work (cache_token.hip): tiles of rows, workgroups, and places of parts: one for each pair of a workgroup and a
-// unit (a tile of rows of a key head of a stream) that it has a part of, of which there are fewer than workgroups and units together.
+// How the calls of these sizes share out their work (cache_token.hip): units' rows (one or two tiles), workgroups, and places of parts: one for each pair of a workgroup and a
+// unit (such rows of a key head of a stream) that it has a part of, of which there are fewer than workgroups and units together.
 struct TokenPlan {
     int rows, row_tiles, workgroups;
     bool joined;

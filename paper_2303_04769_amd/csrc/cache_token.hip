@@ -232,6 +232,7 @@ constexpr int rounds_ints(int threads) { return threads + 6; }
 // SP: into how many columns a row's keys of a tile are shared out, where there are at most 16 / SP rows. Column m then has row m mod (16 / SP), and of the tile's results only
 // those of its share, m / (16 / SP): as if it were a row of its own, with a maximum, a sum and a result of its own, joined in the end. So the 16 columns
 // of single tokens' products are not mostly empty lanes in all that lies between the products.
+// TR: tiles of rows of a unit (two_tiles).
 template <int KIND, int DT, int SP, bool ONE, int TR>
 __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_waves_per_eu(least_waves(KIND, DT, SP, TR)))) cache_token(AttnArgs args, CacheArgs cache_args)
 {

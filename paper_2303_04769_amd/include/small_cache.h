@@ -67,7 +67,8 @@ int small_rotary_grad(const small_rotation *r, const float *dq_out, const float 
  *
  * small_cache_write puts tokens i < counts[n] (NULL: all S; taken into 0 .. S) of k and v at first[n] + i (first NULL: i). With r (else NULL) keys are turned first, as small_rotary
  * turns them, bit for bit, and q, if it is not NULL, is turned into q_out: all its S tokens. r's N, S, kv_heads, D and Cb are the call's; its first is not read (the call's takes its place),
- * its k, k_out, dq, dk are not read. Streams may share pages that are read; one place that a call writes twice holds one of the two.
+ * its k, k_out, dq, dk are not read. Streams may share pages that are read. No place may be written
+ * twice by one call: it would hold parts of both tokens, codes of one with the scale of the other perhaps.
  * small_cache_read: the same tokens from the cache to k and v; tokens that are none and those from counts[n] on are left as they were.
  * k, v: [N][blocks][S][Cb] views as in small_attn.h. Limits: of the launch's threads -- a quarter of D, filled up to a power of two
  * and to 4 at least, for each of N * (S + 31) tokens; where S <= 4, at least 64 for each -- there are fewer than 2^32; per_stream * page <= 2^28. */
@@ -91,7 +92,7 @@ int small_cache_read(const small_cache *c, const small_span *s, float *k, float 
 /* ---- attention of new tokens over the cache: small_attention with the keys and values of each stream's first lengths[n] tokens, causal. Of *a are read
  * N, Sq, heads, D, Cb, q, out, scale, cap, reach, buckets, lengths (not NULL; at most per_stream * page count), first (NULL: lengths[n] - Sq, the last tokens),
  * slopes, table (the bias's) and bucket; width must be 1, prefix and docs NULL, kv_heads and D the cache's. A stream of length zero is an empty place: out = 0,
- * lse = -inf. Meant for one token, or a few, a stream: sixteen rows (tokens times the query heads of a key head) read the cache once. The streams' work is shared out by all of
+ * lse = -inf. Meant for one token, or a few, a stream: every sixteen rows (tokens times the query heads of a key head), or 32, read the cache once. The streams' work is shared out by all of
  * their lengths: where a row's sums are split, and so how they are rounded, depends on the other streams' too. heads * buckets <= 2^30, and of tiles of sixteen rows and at least
  * 32 keys there are fewer than 2^30.
  * What a row does not see, and what is behind a stream's length in its last page, does not reach it, however large, infinite or NaN.
