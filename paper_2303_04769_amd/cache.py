@@ -23,7 +23,7 @@ _KINDS = {"float32": (CACHE_F32, torch.float32), "bfloat16": (CACHE_BF16, torch.
 
 
 class small_rotation(C.Structure):
-    _fields_ = [(n, C.c_int) for n in ("N", "S", "heads", "kv_heads", "D", "Cb", "axes", "pairs", "halves", "freq_heads")] + [("extent", C.c_int * 4)] + \
+    _fields_ = [(n, C.c_int) for n in ("N", "S", "heads", "kv_heads", "D", "Cb", "axes", "pairs", "halves", "freq_heads")] + [("extent", C.c_int * 4), ("from_inputs", C.c_int)] + \
                [(n, small_tokens) for n in ("q", "k", "q_out", "k_out", "dq", "dk")] + [(n, C.c_void_p) for n in ("freq", "first", "positions")]
 
 
@@ -162,18 +162,19 @@ class Rotary:
         po, pko = self._pair(q if q_out is None else q_out, k if k_out is None else k_out, ("q_out", "k_out"))
         small_rotary(self.record, pq, pk, po, pko, stream)
 
-    def grad(self, dq_out, dk_out, freq, dq=None, dk=None, q=None, k=None, dfreq=None, first=None, positions=None, stream=None):
+    def grad(self, dq_out, dk_out, freq, dq=None, dk=None, q=None, k=None, dfreq=None, first=None, positions=None, stream=None, from_inputs=False):
         """Turns the gradients of run's outputs back into those of its inputs (in place where dq and dk are None). With dfreq, [freq_heads][axes][pairs], the frequencies'
-        gradient too, from q and k: run's outputs, or its inputs."""
+        gradient too, from q and k: run's outputs, or with from_inputs its inputs."""
         r = self.record
         if dfreq is not None and self._workspace is None:
             self._fill(freq, first, positions)
             self._workspace = torch.empty(small_rotary_workspace(r), dtype=torch.uint8, device=self.device)
         if stream is None:
-            rc = _fast().rotary_grad(r, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, None if dfreq is None else self._workspace, None)
+            rc = _fast().rotary_grad(r, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, None if dfreq is None else self._workspace, int(from_inputs), None)
             if rc is not None:
                 return B._check(rc, "small_rotary_grad")
         self._fill(freq, first, positions)
+        r.from_inputs = bool(from_inputs)
         if dfreq is not None:
             A._floats(dfreq, (r.freq_heads, r.axes, r.pairs))
         pq, pk = self._pair(q, k, ("q", "k"))

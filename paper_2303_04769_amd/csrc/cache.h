@@ -39,7 +39,7 @@ __device__ __forceinline__ Scale scale_of(unsigned top_bits)
 __device__ __forceinline__ int code_of_value(float x, float by) { return by == 0.f ? 0 : (int)__builtin_rintf(x * by); }
 
 hipError_t launch_rotary(const RotaryArgs &a, bool vec, bool halves, hipStream_t s);                       // rotary.hip
-hipError_t launch_rotary_grad(const RotaryArgs &a, bool vec, bool halves, float *dfreq, hipStream_t s);
+hipError_t launch_rotary_grad(const RotaryArgs &a, bool vec, bool halves, bool from_inputs, float *dfreq, hipStream_t s);
 
 struct StoreArgs {
     CacheArgs c;

@@ -203,7 +203,7 @@ int rotary(const small_rotation &r, const float *q, const float *k, float *q_out
     x.yq_step = step(saved[0], r.heads); x.yk_step = step(saved[1], r.kv_heads);
     if (back) x.sign = -1.f;
     place(x, p, dfreq != nullptr);
-    return from_hip(dfreq ? launch_rotary_grad(x, vec, r.halves != 0, dfreq, stream) : launch_rotary(x, vec, r.halves != 0, stream));
+    return from_hip(dfreq ? launch_rotary_grad(x, vec, r.halves != 0, r.from_inputs != 0, dfreq, stream) : launch_rotary(x, vec, r.halves != 0, stream));
 }
 
 // ---- the cache

@@ -356,8 +356,8 @@ ENTRY(rotary, 9, small_rotation rec = r.record<small_rotation>(0, rotation_type)
       auto *qo = r.view(args[6] == Py_None ? 1 : 6, rec.N, rec.S, rec.Cb, cq, &rec.q_out, true);
       auto *ko = r.view(args[7] == Py_None ? 2 : 7, rec.N, rec.S, rec.Cb, ck, &rec.k_out, true);
       return r.call([&](void *s) { return lib.small_rotary(&rec, q, k, qo, ko, s); });)
-// (record, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, workspace, stream)
-ENTRY(rotary_grad, 13, small_rotation rec = r.record<small_rotation>(0, rotation_type); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
+// (record, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, workspace, from_inputs, stream)
+ENTRY(rotary_grad, 14, small_rotation rec = r.record<small_rotation>(0, rotation_type); rec.from_inputs = r.i(12); const long cq = (long)rec.heads * rec.D, ck = (long)rec.kv_heads * rec.D;
       size_t size; void *ws = r.bytes(11, &size);
       r.places(3, rec); rec.first = r.of<int>(5, at::kInt, {rec.N});
       auto *dqo = r.view(1, rec.N, rec.S, rec.Cb, cq, &rec.q_out, true); auto *dko = r.view(2, rec.N, rec.S, rec.Cb, ck, &rec.k_out, true);

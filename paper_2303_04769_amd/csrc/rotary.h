@@ -21,7 +21,7 @@ struct RotaryArgs {
     // bits that all heads share, and a head's place is scalar: no vector operation is spent on addresses (14 x 14 pixels, 64 images, 8 heads of 32: 12.8 -> 11.2 us).
     int fast;
     long long q_step, k_step, qo_step, ko_step, yq_step, yk_step;
-    // gradient by the frequencies: y (what was turned) beside q and k
+    // gradient by the frequencies: y (the turned q and k, or those before the turn) beside them
     const float *yq, *yk;
     TokenStrides yqs, yks;
     double *partial;                         // [freq_heads][chunks * parts][axes][pairs]

@@ -5,7 +5,8 @@
 // tokens, so a wave's access is whole lines. Where tokens are few, heads are shared out over threads and sines computed again.
 // 14 x 14 pixels of 64 images, 8 heads of 32: 10.5 us, 4.9 TB/s; clips of 16 x 28 x 28 pixels: 23.2 us, 5.5 TB/s (a large copy: 4.9, one of 64 MB 8.0).
 //
-// With y = R(t) x, t = sum over axes of place * frequency: dx = R(-t) dy, and dt of a pair is dy1 y0 - dy0 y1, which needs no sine. Its sums times the places run in 64 bits
+// With y = R(t) x, t = sum over axes of place * frequency: dx = R(-t) dy, and dt of a pair is dy1 y0 - dy0 y1, which needs no sine -- or dx1 x0 - dx0 x1, where x is what there is:
+// a turn of both leaves their cross product as it is (dx as it was rounded, as y is where that is read). Its sums times the places run in 64 bits
 // over a chunk of tokens for each workgroup, whose results a second launch adds up in a fixed order (8 x 8 pixels of 256 images: 9.5 us and 3.9; 6 x 999 frames: 9 and 3).
 #include "rotary.h"
 
@@ -181,7 +182,8 @@ __global__ void __launch_bounds__(256) rotary_turn(RotaryArgs a)
 }
 
 // The turn back, with the sums over a chunk of tokens for the frequencies' gradient. A workgroup has one run of units of one set of frequencies; run is a power of two.
-template <bool VEC, bool HALVES, bool FAST>
+// INPUTS: from_inputs, a form of its own: chosen at run time it takes 16 to 29 registers more, and with them a wave a SIMD.
+template <bool VEC, bool HALVES, bool FAST, bool INPUTS>
 __global__ void __launch_bounds__(256) rotary_grad(RotaryArgs a)
 {
     using Unit = Pairs<VEC, HALVES>;
@@ -235,10 +237,14 @@ __global__ void __launch_bounds__(256) rotary_grad(RotaryArgs a)
                 for (int b = 0; b < G; ++b) {
                     if (j0 + b >= hi) break;
                     const int h = heads.head(j0 + b);
+                    const auto cross = [&] {
 #pragma unroll
-                    for (int p = 0; p < P; ++p)
-                        g[p] += __builtin_fma((double)x[b].x[2 * p + 1], (double)y[b].x[2 * p], -((double)x[b].x[2 * p] * (double)y[b].x[2 * p + 1]));
+                        for (int p = 0; p < P; ++p)
+                            g[p] += __builtin_fma((double)x[b].x[2 * p + 1], (double)y[b].x[2 * p], -((double)x[b].x[2 * p] * (double)y[b].x[2 * p + 1]));
+                    };
+                    if constexpr (!INPUTS) cross();
                     x[b].turn(t);
+                    if constexpr (INPUTS) cross();
                     if constexpr (FAST) x[b].store_at(to + h * (tensor ? a.ko_step : a.qo_step), to_at);
                     else x[b].store(a, ts, token_out, h * a.D, u);
                 }
@@ -287,14 +293,14 @@ __global__ void __launch_bounds__(256) rotary_grad_join(const double *partial, f
     if (lane == 0) dfreq[at] = (float)v;
 }
 
-#define BY_FORM(kernel, grid, vec, halves, s, a)                                                                            \
-    do {                                                                                                                    \
-        if (vec && halves && a.fast) hipLaunchKernelGGL((kernel<true, true, true>), dim3(grid), dim3(256), 0, s, a);        \
-        else if (vec && a.fast) hipLaunchKernelGGL((kernel<true, false, true>), dim3(grid), dim3(256), 0, s, a);            \
-        else if (vec && halves) hipLaunchKernelGGL((kernel<true, true, false>), dim3(grid), dim3(256), 0, s, a);            \
-        else if (vec) hipLaunchKernelGGL((kernel<true, false, false>), dim3(grid), dim3(256), 0, s, a);                     \
-        else if (halves) hipLaunchKernelGGL((kernel<false, true, false>), dim3(grid), dim3(256), 0, s, a);                  \
-        else hipLaunchKernelGGL((kernel<false, false, false>), dim3(grid), dim3(256), 0, s, a);                             \
+#define BY_FORM(kernel, grid, vec, halves, s, a, ...)                                                                                           \
+    do {                                                                                                                                        \
+        if (vec && halves && a.fast) hipLaunchKernelGGL((kernel<true, true, true __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a); \
+        else if (vec && a.fast) hipLaunchKernelGGL((kernel<true, false, true __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a);     \
+        else if (vec && halves) hipLaunchKernelGGL((kernel<true, true, false __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a);     \
+        else if (vec) hipLaunchKernelGGL((kernel<true, false, false __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a);              \
+        else if (halves) hipLaunchKernelGGL((kernel<false, true, false __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a);           \
+        else hipLaunchKernelGGL((kernel<false, false, false __VA_OPT__(, ) __VA_ARGS__>), dim3(grid), dim3(256), 0, s, a);                      \
     } while (0)
 
 }  // namespace
@@ -306,10 +312,11 @@ hipError_t launch_rotary(const RotaryArgs &a, bool vec, bool halves, hipStream_t
     return hipGetLastError();
 }
 
-hipError_t launch_rotary_grad(const RotaryArgs &a, bool vec, bool halves, float *dfreq, hipStream_t s)
+hipError_t launch_rotary_grad(const RotaryArgs &a, bool vec, bool halves, bool from_inputs, float *dfreq, hipStream_t s)
 {
     const unsigned grid = (unsigned)(a.freq_heads * a.parts * a.runs * a.chunks) + (a.copy_threads + 255u) / 256u;
-    BY_FORM(rotary_grad, grid, vec, halves, s, a);
+    if (from_inputs) BY_FORM(rotary_grad, grid, vec, halves, s, a, true);
+    else BY_FORM(rotary_grad, grid, vec, halves, s, a, false);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int each = a.axes * a.pairs, all = a.freq_heads * each;

@@ -32,7 +32,8 @@ extern "C" {
  *
  * small_rotary_grad: given the gradients dq_out, dk_out of q_out, k_out, the gradients dq, dk of q, k -- the turn back; in place likewise -- and, where dfreq is not NULL,
  *     dfreq[f][axis][k] = sum over images, tokens, the heads that turn by f of place[axis] * (dy1 y0 - dy0 y1)                  (summed in 64 bits)
- * for which it reads q and k: what small_rotary gave, or what it was given (the cross product is the same). They may be NULL without dfreq. Strides: r->q, r->k are those of
+ * for which it reads q and k: what small_rotary gave (y above, and dy are dq_out, dk_out), or with r->from_inputs what it was given (y and dy are q and dq, k and dk: turned back by one
+ * angle, both have the same cross product; neither has it with the other). They may be NULL without dfreq. Strides: r->q, r->k are those of
  * q and k, r->q_out, r->k_out of dq_out and dk_out, r->dq, r->dk of dq and dk. small_rotary_workspace (host only): bytes that the gradient call with dfreq needs,
  * 256-byte aligned; without dfreq none are needed.
  *
@@ -41,8 +42,9 @@ typedef struct {
     int N, S, heads, kv_heads, D, Cb;
     int axes, pairs, halves, freq_heads;
     int extent[4];
+    int from_inputs;                    /* this, dq and dk are read by the gradient call only */
     small_tokens q, k, q_out, k_out;
-    small_tokens dq, dk;                /* read by the gradient call only */
+    small_tokens dq, dk;
     const float *freq;
     const int *first, *positions;
 } small_rotation;

@@ -158,6 +158,40 @@ def test_frequency_gradient_by_differences(halves):
                 assert abs(slope - float(dfreq[f, a, p])) <= h * h / 6 * 8 * worst + 1e-5 * abs(slope)
 
 
+@pytest.mark.parametrize("form", FORMS)
+def test_frequency_gradient_from_inputs(form):
+    """From what was turned instead of what that gave, against automatic differentiation in 64 bits. A term is off by half a step of the turned back gradient's two channels, by 2^-50 of
+    the pairs' sizes and by the angle's rounding (check); sums of fewer than 2^13 terms in 64 bits, rounded once. Gradients in place, through ctypes: the same bits."""
+    N, S_, heads, kv, D, Cb, axes, pairs, halves, extent, F, _, _ = form
+    plan, q, k, freq, first, positions, place = setup(form)
+    dq, dk = rand(7, *q.shape).to(DEV), rand(8, *k.shape).to(DEV)
+    outs = [torch.full_like(t, math.nan) for t in (dq, dk)]
+    dfreq = torch.full_like(freq, math.nan)
+    plan.grad(dq, dk, freq, *outs, q=q, k=k, dfreq=dfreq, first=first, positions=positions, from_inputs=True)
+    leaf = freq.cpu().double().requires_grad_()
+    loss, size, far = 0.0, 0.0, 0.0
+    a, b = (slice(0, pairs), slice(pairs, 2 * pairs)) if halves else (slice(0, 2 * pairs, 2), slice(1, 2 * pairs, 2))
+    for d, x, h in ((dq, q, heads), (dk, k, kv)):
+        d, x = heads_of(d, h), heads_of(x, h)
+        y, angle = turned(x, place, leaf, pairs, halves)
+        far = max(far, float(angle.detach().abs().max()))
+        loss = loss + (y * d).sum()
+        both = ((d[..., a].abs() + d[..., b].abs()) * (x[..., a].abs() + x[..., b].abs())).reshape(N, F, h // F, S_, pairs)
+        size = size + torch.einsum("nfhsk,nsa->fak", both, place.abs())
+    total, = torch.autograd.grad(loss, leaf)
+    off = (dfreq.cpu().double() - total).abs() - 2.0 ** -24 * total.abs() - (2.0 ** -24 + 2.0 ** -39 + 2 * (2.0 ** -50 + 4 * 2.0 ** -53 * far)) * size
+    assert bool((off <= 0).all()), float(off.max())
+    again, other, copies = torch.empty_like(dfreq), torch.cuda.Stream(), (dq.clone(), dk.clone())
+    torch.cuda.synchronize()
+    plan.grad(*copies, freq, q=q, k=k, dfreq=again, first=first, positions=positions, from_inputs=True, stream=other)
+    other.synchronize()
+    assert torch.equal(again, dfreq)
+    # from outputs: the same but for the rounding of one or the other
+    plan.run(q, k, freq, first=first, positions=positions)
+    plan.grad(dq, dk, freq, *outs, q=q, k=k, dfreq=again, first=first, positions=positions)
+    assert bool(((again - dfreq).abs().cpu().double() <= 2.0 ** -23 * total.abs() + (2.0 ** -23 + 2.0 ** -38 + 4 * (2.0 ** -50 + 4 * 2.0 ** -53 * far)) * size).all())
+
+
 def _run(plan, q, k, freq):
     qo, ko = torch.empty_like(q), torch.empty_like(k)
     plan.run(q, k, freq, qo, ko)
