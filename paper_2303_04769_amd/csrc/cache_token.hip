@@ -474,7 +474,15 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
                 for (int b = 0; b < NV; ++b) weight[b] = vsc[b];
             }
             const float base = far[t] - top[t].at;
+            const int bound = min(row.bound, end);
+            const bool all_seen = __all((j0 + KT <= bound) & !no_page);
+            const auto seen = [&](int b, int e) { return (key0 + 4 * b + e < bound) & !no_page; };
             if (a.cap > 0.f) {
+                if (!all_seen)                                 // (the largest score chooses how the cap is computed, in other last bits: not one of a key that is not there)
+#pragma unroll
+                    for (int b = 0; b < NV; ++b)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) s[b][e] = seen(b, e) ? s[b][e] : 0.f;
                 tanh_all(s);
                 const float out = a.cap * kLog2e;
 #pragma unroll
@@ -495,15 +503,13 @@ __global__ void __launch_bounds__(64 * group_waves(DT)) __attribute__((amdgpu_wa
                 for (int b = 0; b < NV; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s[b][e] += bias_log2(bias[t][b][e]);
-            const int bound = min(row.bound, end);
-            if (!__all((j0 + KT <= bound) & !no_page)) {
+            if (!all_seen) {
 #pragma unroll
                 for (int b = 0; b < NV; ++b)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const bool seen = (key0 + 4 * b + e < bound) & !no_page;
-                        s[b][e] = seen ? s[b][e] : -kInf;
-                        if constexpr (KIND == SMALL_CACHE_I8) weight[b][e] = seen ? weight[b][e] : 0.f;              // (the scale of a hidden token may be anything)
+                        s[b][e] = seen(b, e) ? s[b][e] : -kInf;
+                        if constexpr (KIND == SMALL_CACHE_I8) weight[b][e] = seen(b, e) ? weight[b][e] : 0.f;        // (the scale of a hidden token may be anything)
                     }
             }
             raise_top(s, top[t], sum[t], o[t]);

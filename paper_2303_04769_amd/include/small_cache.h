@@ -97,7 +97,8 @@ int small_cache_read(const small_cache *c, const small_span *s, float *k, float 
  * lse = -inf. Meant for one token, or a few, a stream: every sixteen rows (tokens times the query heads of a key head), or 32, read the cache once. The streams' work is shared out by all of
  * their lengths: where a row's sums are split, and so how they are rounded, depends on the other streams' too. heads * buckets <= 2^30, and of tiles of sixteen rows and at least
  * 32 keys there are fewer than 2^30.
- * What a row does not see, and what is behind a stream's length in its last page, does not reach it, however large, infinite or NaN.
+ * What a row does not see, and what is behind a stream's length in its last page or in no page of its, does not reach it, however large, infinite or NaN. (What other rows of a call see
+ * of the same stream may decide which of two ways a value of a row is rounded, no more; memory that holds no token of a stream's does not decide even that.)
  * small_cache_attention_workspace (host only) looks at sizes alone. */
 int small_cache_attention_workspace(const small_cache *c, const small_attn *a, size_t *bytes);
 int small_cache_attention(const small_cache *c, const small_attn *a, const float *q, float *out, float *lse, void *workspace,

@@ -366,6 +366,38 @@ def test_hidden_tokens_reach_no_row(kind):
 
 
 @pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("Sq,heads,D,page,bias", [(1, 4, 32, 16, "none"), (1, 16, 64, 64, "slopes"), (5, 8, 32, 64, "none"), (9, 8, 64, 32, "buckets")])
+def test_capped_scores_beside_memory_of_no_token(Sq, heads, D, page, bias, kind):
+    """With a cap the same bits, whatever stands behind a stream's length in its last page and in the page that stands in for one that is none: nothing, or keys whose scores are far
+    larger than any that count, where another way to compute the cap would be chosen."""
+    N, kv, per = 3, 2, 9
+    lengths = [Sq + 3, 5 * page + 7, 9 * page - 2]
+    form = (N, Sq, heads, kv, D, D, page, per, lengths, None, bias, 30.0)
+    cache, table, q, k, v, more, reach, plan = attention_setup(form, kind)
+    table[1, 3] = -1
+    free = next(p for p in range(1, cache.pages) if not bool((table == p).any()))
+    for t in (cache.keys, cache.values, cache.key_scales, cache.value_scales):
+        if t is not None:
+            t[free] = t[0]
+    table[table == 0] = free                                   # (page 0 is nobody's: it is read where there is no page)
+    rows, outs = table.cpu(), []
+    for fill in (0, 100):
+        for n, held_ in enumerate(lengths):
+            at, place = int(rows[n, held_ // page]), held_ % page
+            cache.keys[at, :, place:, :D], cache.values[at, :, :, place:] = fill, fill
+            if kind == "int8":
+                cache.key_scales[at, :, place:], cache.value_scales[at, :, place:] = 1.0, 1.0
+        cache.keys[0, ..., :D], cache.values[0] = fill, fill
+        if kind == "int8":
+            cache.key_scales[0], cache.value_scales[0] = 1.0, 1.0
+        out, lse = torch.empty(q.shape, device=DEV), torch.empty(N, heads, Sq, device=DEV)
+        plan.run(q.to(DEV), out, table, ints(lengths), lse=lse, **more)
+        outs.append((out, lse))
+    assert torch.isfinite(outs[0][0]).all()
+    assert torch.equal(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+
+
+@pytest.mark.parametrize("kind", KINDS)
 def test_biases_that_hide(kind):
     """A learned bias of the type's lowest value hides its offsets, all of them a whole row."""
     form = (2, 1, 4, 2, 16, 16, 16, 8, [100, 128], None, "buckets", 0.0)
