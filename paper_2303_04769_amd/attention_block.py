@@ -208,7 +208,7 @@ class StreamBlock:
         self.free, self.held = list(range(pages))[::-1], [[] for _ in range(N)]
         self.lengths = [0] * N
         self.table = torch.full((N, per_stream), -1, dtype=torch.int32, device=dev)
-        self._first, self._length = (torch.zeros(N, dtype=torch.int32, device=dev) for _ in range(2))
+        self._length, self._after = (torch.zeros(N, dtype=torch.int32, device=dev) for _ in range(2))        # before and after the frames of a call
         self._plans = {}
 
     def _plan(self, S, Sk):
@@ -229,20 +229,16 @@ class StreamBlock:
         self._plans[S, Sk] = plan
         return plan
 
-    def _take(self, counts):
-        """Pages for so many more frames of each stream, all or none."""
+    def _new_pages(self, counts):
+        """Pages for so many more frames of each stream, all or none. They are still free."""
         need = [-(-(held + more) // self.page) - len(pages) for held, more, pages in zip(self.lengths, counts, self.held)]
         for n, (held, more) in enumerate(zip(self.lengths, counts)):
             if held + more > self.per_stream * self.page:
                 raise ValueError(f"stream {n}: {held} frames and {more} more do not fit {self.per_stream} pages of {self.page}")
         if sum(need) > len(self.free):
             raise ValueError(f"{sum(need)} pages are needed and {len(self.free)} free")
-        for n, more in enumerate(need):
-            if more:
-                new = [self.free.pop() for _ in range(more)]
-                at = len(self.held[n])
-                self.held[n] += new
-                self.table[n, at:at + more] = torch.tensor(new, dtype=torch.int32)
+        last_first = iter(self.free[::-1])
+        return [[next(last_first) for _ in range(more)] for more in need]
 
     def release(self, n):
         """Stream n ends: its pages are free, its place is empty for another."""
@@ -254,30 +250,45 @@ class StreamBlock:
 
     def forward(self, frames, counts=None):
         """The next frames [N][S][Cc], of which stream n has counts[n] (a list; None: S each): their outputs. What stands behind a stream's frames, in and out, is of no
-        meaning."""
+        meaning. A call that raises leaves all streams as they were."""
         S = frames.shape[1]
         _shaped(frames, (self.N, S, self.C))
         if counts is not None and (len(counts) != self.N or not all(0 <= c <= S for c in counts)):
             raise ValueError(f"expected {self.N} numbers of frames in 0 .. {S}, got {counts}")
         more = [S] * self.N if counts is None else [int(c) for c in counts]
-        self._take(more)
-        here = None if counts is None else torch.tensor(more, dtype=torch.int32).to(frames.device)
-        self._first.copy_(self._length)
-        self._length.add_(S if here is None else here)
-        self.lengths = [a + b for a, b in zip(self.lengths, more)]
+        pages, lengths = self._new_pages(more), [a + b for a, b in zip(self.lengths, more)]
         few = S * (self.heads // self.kv_heads) <= ROWS_ON_CACHE
-        norm, rotary, attention, h, qkv, ctx, read = self._plan(S, 0 if few else -(-max(self.lengths) // self.page) * self.page)
-        out = torch.empty_like(frames)
+        plan = self._plan(S, 0 if few else -(-max(lengths) // self.page) * self.page)
+        here = None if counts is None else torch.tensor(more, dtype=torch.int32).to(self._length.device)
+        torch.add(self._length, S if here is None else here, out=self._after)
+        try:
+            for n, new in enumerate(pages):
+                if new:
+                    at = len(self.held[n])
+                    self.table[n, at:at + len(new)] = torch.tensor(new, dtype=torch.int32)
+            out = self._layers(frames, here, few, *plan)
+        except BaseException:
+            for n, new in enumerate(pages):
+                if new:
+                    self.table[n, len(self.held[n]):] = -1
+            raise
+        self._length, self._after, self.lengths = self._after, self._length, lengths
+        self.held = [held + new for held, new in zip(self.held, pages)]
+        del self.free[len(self.free) - sum(map(len, pages)):]
+        return out
+
+    def _layers(self, frames, here, few, norm, rotary, attention, h, qkv, ctx, read):
+        S, out = frames.shape[1], torch.empty_like(frames)
         norm.run(frames, self.gamma, self.beta, h)
         _conv1x1(h, self.w_in, qkv, self.N * S, self.C, self.Cq + 2 * self.Ck, 1, 1, self.Cb, self.Cb)
         heads = lambda t, first, n: t.as_strided((self.N, n, S, self.D), (S * t.shape[1], self.D, t.shape[1], 1), first)  # noqa: E731
         q, k, v = heads(qkv, 0, self.heads), heads(qkv, self.Cq, self.kv_heads), heads(qkv, self.Cq + self.Ck, self.kv_heads)
-        self.cache.write(k, v, self.table, self._first, counts=here, rotary=rotary, freq=self.freq, q=q)
+        self.cache.write(k, v, self.table, self._length, counts=here, rotary=rotary, freq=self.freq, q=q)
         if few:
-            attention.run(q, heads(ctx, 0, self.heads), self.table, self._length, first=self._first)
+            attention.run(q, heads(ctx, 0, self.heads), self.table, self._after, first=self._length)
         else:
-            self.cache.read(*read, self.table, counts=self._length)
-            attention.run(q, *read, heads(ctx, 0, self.heads), lengths=self._length, first=self._first)
+            self.cache.read(*read, self.table, counts=self._after)
+            attention.run(q, *read, heads(ctx, 0, self.heads), lengths=self._after, first=self._length)
         _conv1x1(ctx, self.w_out, out, self.N * S, self.Cq, self.C, 1, 1, self.Cb, self.Cb)
         B.small_add(out, frames, out, out.numel())
         return out

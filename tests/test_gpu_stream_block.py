@@ -181,6 +181,24 @@ def test_no_pages_left():
     assert block.lengths == [33, 17]
 
 
+@pytest.mark.parametrize("S_", [5, 40])
+def test_refused_frames_leave_the_streams_as_they_were(S_):
+    """Frames of another type, on the host, or not contiguous: the streams go on as if the call had not been."""
+    gen = torch.Generator().manual_seed(4)
+    make, _ = stream_block(gen, 2, 32, 4, 4, 2, 16, "float32", 20, 16, 8)
+    block, other = make(), make()
+    frames = uniform(gen, 2, 60, 32).float().cuda()
+    first, next_ = frames[:, :S_].contiguous(), frames[:, S_:S_ + 20].contiguous()
+    assert torch.equal(block.forward(first), other.forward(first))
+    for bad in (next_.double(), next_.cpu(), frames[:, S_:S_ + 20], frames[:, S_:S_ + 20].half()):
+        before = (block.lengths[:], block.table.clone(), block.free[:], [h[:] for h in block.held])
+        with pytest.raises(TypeError):
+            block.forward(bad, [20, 3])
+        assert block.lengths == before[0] and torch.equal(block.table, before[1]) and block.free == before[2] and block.held == before[3]
+    a, b = block.forward(next_, [20, 3]), other.forward(next_, [20, 3])
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1, :3], b[1, :3])
+
+
 def test_the_example_runs(capsys):
     AB.main(steps=2)
     assert "8-bit pages" in capsys.readouterr().out
