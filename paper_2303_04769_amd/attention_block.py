@@ -212,7 +212,7 @@ class StreamBlock:
         self._plans = {}
 
     def _plan(self, S, Sk):
-        """What calls of S new frames need; Sk: tokens that are read back, 0 where the cache is attended to. The last few are kept."""
+        """What calls of S new frames need; Sk: tokens that are read back (a page of them at least), 0 where the cache is attended to. The last few are kept."""
         plan = self._plans.pop((S, Sk), None)
         if plan is None:
             dev, tokens = self.w_in.device, self.N * S
@@ -258,7 +258,7 @@ class StreamBlock:
         more = [S] * self.N if counts is None else [int(c) for c in counts]
         pages, lengths = self._new_pages(more), [a + b for a, b in zip(self.lengths, more)]
         few = S * (self.heads // self.kv_heads) <= ROWS_ON_CACHE
-        plan = self._plan(S, 0 if few else -(-max(lengths) // self.page) * self.page)
+        plan = self._plan(S, 0 if few else max(1, -(-max(lengths) // self.page)) * self.page)
         here = None if counts is None else torch.tensor(more, dtype=torch.int32).to(self._length.device)
         torch.add(self._length, S if here is None else here, out=self._after)
         try:

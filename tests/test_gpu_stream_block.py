@@ -199,6 +199,37 @@ def test_refused_frames_leave_the_streams_as_they_were(S_):
     assert torch.equal(a[0], b[0]) and torch.equal(a[1, :3], b[1, :3])
 
 
+@pytest.mark.parametrize("S_", [4, 40])
+def test_a_batch_of_nothing(S_):
+    """No stream has a frame or brings one; then one does."""
+    gen = torch.Generator().manual_seed(6)
+    make, run = stream_block(gen, 2, 32, 4, 4, 2, 16, "float32", 12, 16, 6)
+    block = make()
+    frames = uniform(gen, 2, S_, 32)
+    assert block.forward(frames.float().cuda(), [0, 0]).shape == frames.shape and block.lengths == [0, 0] and len(block.free) == 12
+    out = block.forward(frames.float().cuda(), [0, S_]).cpu().double()
+    close(out[1], run(frames[1]), "out")
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "int8"])
+@pytest.mark.parametrize("width,counts", [(4, [2, 0, 4]), (40, [40, 7, 33])])
+def test_what_stands_behind_the_frames_of_a_batch(width, counts, kind):
+    """NaN and infinities in the padding: the same bits for the frames that there are."""
+    found = []
+    for fill in (7.0, float("nan"), float("inf")):
+        gen = torch.Generator().manual_seed(1)
+        make, _ = stream_block(gen, 3, 48, 4, 4, 2, 16, kind, 24, 16, 8, F=2)
+        block = make()
+        for _ in range(2):
+            frames = uniform(gen, 3, width, 48).float()
+            for n, c in enumerate(counts):
+                frames[n, c:] = fill
+            out = block.forward(frames.cuda(), counts).cpu()
+            found.append(torch.cat([out[n, :c] for n, c in enumerate(counts)]))
+    assert torch.isfinite(found[0]).all() and torch.isfinite(found[1]).all()
+    assert all(torch.equal(a, b) for a, b in zip(found[2:], found[:2] * 2))
+
+
 def test_the_example_runs(capsys):
     AB.main(steps=2)
     assert "8-bit pages" in capsys.readouterr().out

@@ -91,3 +91,14 @@ def test_frames_are_counted_from_call_to_call(layers):
     b.release(2)
     b.forward(torch.zeros(N, 5, CC))
     assert b.lengths == [at[0] + 5, at[1] + 5, 5] and layers.last("write")[1][3].tolist() == [at[0], at[1], 0]
+
+
+def test_wide_call_on_empty_streams(layers):
+    """An idle batch, more rows than are attended on the cache, in streams without a frame so far: a plan of the wide form, of a page at least."""
+    b = block()
+    b.forward(torch.zeros(N, 40, CC), [0, 0, 0])
+    assert layers.last("Attention")[1][2] >= 1 and layers.last("read")[2]["counts"].tolist() == [0, 0, 0]
+    name, args, kw = layers.last("attend")
+    assert kw["lengths"].tolist() == [0, 0, 0] and b.lengths == [0, 0, 0] and not sum(b.held, []) and len(b.free) == 12
+    b.forward(torch.zeros(N, 40, CC), [40, 0, 1])
+    assert b.lengths == [40, 0, 1]
