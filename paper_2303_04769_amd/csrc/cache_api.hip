@@ -46,6 +46,9 @@ bool quads(int D, int Cb, std::initializer_list<const small_tokens *> strides, s
     return D % 4 == 0 && Cb % 4 == 0 && bits % 4 == 0 && at % 16 == 0;
 }
 
+// Shares of so many heads: as many as are wanted, no more than there are heads, and so that a share's number times the heads, which the kernels divide, fits an int.
+int shares_of(int heads, double wanted) { return (int)fmin(fmin(heads, wanted), INT_MAX / heads); }
+
 // ---- rotary positions
 
 int rotation_check(const small_rotation &r, bool grad)
@@ -82,14 +85,14 @@ TurnPlan plan_turn(const small_rotation &r, bool vec, bool q, bool k, bool grad)
     if (!grad) {
         // two waves a SIMD at least, if there are heads enough to share out
         const double threads = tokens * p.units * r.freq_heads, want = 131072.0;
-        if (threads < want) p.parts = (int)fmin(items, ceil(want / threads));
+        if (threads < want) p.parts = shares_of(items, ceil(want / threads));
         return p;
     }
     p.run = power_of_two_of(p.run);
     if (p.run > 64) p.run = 64;
     const int at_once = 256 / p.run, wanted = 1024;
     const long rounds = ((long)r.N * r.S + at_once - 1) / at_once, sets = (long)r.freq_heads * (p.units / p.run);
-    if (rounds * sets < wanted) p.parts = (int)fmin(items, (double)((wanted + rounds * sets - 1) / (rounds * sets)));
+    if (rounds * sets < wanted) p.parts = shares_of(items, (double)((wanted + rounds * sets - 1) / (rounds * sets)));
     long chunks = wanted / (sets * p.parts);
     if (chunks < 1) chunks = 1;
     if (chunks > rounds) chunks = rounds;
@@ -253,7 +256,7 @@ int plan_store(StoreArgs &x, const small_cache &c, const small_span &s, int head
     x.items = heads + 2 * c.kv_heads;
     // four workgroups a compute unit, if there are heads enough to share out
     const double base = (double)c.N * x.tiles;
-    x.parts = base < 1024 ? (int)fmin(x.items, ceil(1024 / base)) : 1;
+    x.parts = base < 1024 ? shares_of(x.items, ceil(1024 / base)) : 1;
     x.by_parts = make_fastdiv(x.parts); x.by_tiles = make_fastdiv(x.tiles);
     x.r.by_Cb = make_fastdiv(s.Cb);
     const double threads = ((x.tile << x.lanes_log2) + 63) / 64 * 64;

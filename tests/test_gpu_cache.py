@@ -562,6 +562,18 @@ def test_captured_beside_eager_calls_and_another_stream():
         assert torch.equal(outs[0], outs[1]) and torch.equal(caches[0].keys, caches[1].keys) and torch.equal(caches[0].values, caches[1].values)
 
 
+@pytest.mark.parametrize("T", [1, 17])
+def test_very_many_heads(T):
+    """More heads than fit 31 bits with the workgroups that share them."""
+    kv = 1100000
+    cache = S.PagedCache(1, 32, kv, 1, kind="float32")
+    k, v = rand(0, 1, kv // 16, T, 16).to(DEV), rand(1, 1, kv // 16, T, 16).to(DEV)
+    cache.write(k, v, ints([[0]]), ints([3]))
+    back = [torch.full_like(k, math.nan) for _ in range(2)]
+    cache.read(*back, ints([[0]]), ints([3]))
+    assert torch.equal(back[0], k) and torch.equal(back[1], v)
+
+
 def test_a_cache_past_two_gigabytes():
     """Offsets of pages and channels past 32 bits: the last pages of a pool of 2.3 GB."""
     kv, D, page = 4, 256, 256

@@ -213,6 +213,24 @@ def test_parts_of_one_projection():
     assert torch.equal(qkv[:, nq + nk:], before[:, nq + nk:])
 
 
+@pytest.mark.parametrize("heads,kv,halves", [(65536, 65536, False), (1 << 21, 1, True)])
+def test_very_many_heads_of_one_token(heads, kv, halves):
+    """More heads than their square fits 31 bits, shared out over workgroups."""
+    q, k = rand(0, 1, heads, 1, 2).to(DEV), rand(1, 1, kv, 1, 2).to(DEV)
+    freq, first = rand(2, 1, 1, 1).to(DEV), torch.tensor([12345], dtype=torch.int32, device=DEV)
+    plan = S.Rotary(1, 1, heads, kv, 2, halves=halves, Cb=2)
+    qo, ko, dfreq = torch.full_like(q, math.nan), torch.full_like(k, math.nan), torch.empty_like(freq)
+    plan.run(q, k, freq, qo, ko, first=first)
+    place = places(1, 1, 1, (), first, None)
+    check(heads_of(qo, heads), heads_of(q, heads), place, freq.cpu(), 1, halves)
+    check(heads_of(ko, kv), heads_of(k, kv), place, freq.cpu(), 1, halves)
+    dq, dk = (torch.full_like(t, math.nan) for t in (q, k))
+    plan.grad(q, k, freq, dq, dk, q=qo, k=ko, dfreq=dfreq, first=first)
+    check(heads_of(dq, heads), heads_of(q, heads), place, freq.cpu(), 1, halves, -1.0)
+    terms = torch.cat([12345.0 * (d[..., 1] * y[..., 0] - d[..., 0] * y[..., 1]).flatten() for d, y in ((q.double(), qo.double()), (k.double(), ko.double()))])
+    assert abs(float(dfreq) - float(terms.sum())) <= 2.0 ** -24 * abs(float(terms.sum())) + 2.0 ** -31 * float(terms.abs().sum())      # (2^22 terms at most, in 64 bits)
+
+
 def test_unaligned_views_have_the_same_bits():
     N, S_, heads, D = 2, 21, 3, 16
     base = rand(0, N * heads * S_ * D + 1).to(DEV)
