@@ -28,13 +28,17 @@ bool meets_any(const Range &w, std::initializer_list<Range> reads)
 bool same(const small_tokens &a, const small_tokens &b) { return a.image == b.image && a.block == b.block && a.token == b.token; }
 
 const size_t kMostStride = (size_t)1 << 40;
+int strides_check(std::initializer_list<const small_tokens *> strides)
+{
+    for (const small_tokens *s : strides)
+        if (s->image > kMostStride || s->block > kMostStride || s->token > kMostStride) return SMALL_ERR_SHAPE;
+    return SMALL_OK;
+}
 int sizes_check(int N, int S, int heads, int kv_heads, int D, int Cb, std::initializer_list<const small_tokens *> strides)
 {
     if (N <= 0 || S <= 0 || heads <= 0 || kv_heads <= 0 || D <= 0 || Cb <= 0 || heads % kv_heads || D > 256 || S > kFar || Cb > 1 << 20) return SMALL_ERR_SHAPE;
     if ((double)heads * D > 1 << 24 || (double)N * S > INT_MAX) return SMALL_ERR_SHAPE;
-    for (const small_tokens *s : strides)
-        if (s->image > kMostStride || s->block > kMostStride || s->token > kMostStride) return SMALL_ERR_SHAPE;
-    return SMALL_OK;
+    return strides_check(strides);
 }
 // Four channels of a head stand together and aligned in all of these.
 bool quads(int D, int Cb, std::initializer_list<const small_tokens *> strides, std::initializer_list<const void *> tensors)
@@ -51,11 +55,10 @@ int shares_of(int heads, double wanted) { return (int)fmin(fmin(heads, wanted), 
 
 // ---- rotary positions
 
-int rotation_check(const small_rotation &r, bool grad)
+// (but for the strides, which are those of the tensors that a call has)
+int rotation_check(const small_rotation &r)
 {
-    if (const int rc = sizes_check(r.N, r.S, r.heads, r.kv_heads, r.D, r.Cb, {&r.q, &r.k, &r.q_out, &r.k_out})) return rc;
-    if (grad)
-        if (const int rc = sizes_check(r.N, r.S, r.heads, r.kv_heads, r.D, r.Cb, {&r.dq, &r.dk})) return rc;
+    if (const int rc = sizes_check(r.N, r.S, r.heads, r.kv_heads, r.D, r.Cb, {})) return rc;
     if (r.axes < 1 || r.axes > 4 || r.pairs < 1 || 2 * r.pairs > r.D || (r.freq_heads != 1 && r.freq_heads != r.kv_heads)) return SMALL_ERR_SHAPE;
     if (!r.freq) return SMALL_ERR_NULL;
     if (!r.positions)
@@ -160,7 +163,10 @@ int rotary(const small_rotation &r, const float *q, const float *k, float *q_out
            const small_tokens &qos, const small_tokens &kos, const float *yq, const float *yk, float *dfreq, bool back, void *workspace, size_t workspace_bytes, hipStream_t stream)
 {
     if ((!q && !k) || !q != !q_out || !k != !k_out) return SMALL_ERR_NULL;
-    if (const int rc = rotation_check(r, back)) return rc;
+    if (const int rc = rotation_check(r)) return rc;
+    if (const int rc = strides_check({q ? &qs : &ks, q ? &qos : &kos, k ? &ks : &qs, k ? &kos : &qos})) return rc;
+    if (dfreq)
+        if (const int rc = strides_check({q ? &r.q : &r.k, k ? &r.k : &r.q})) return rc;
     if (dfreq && ((q && !yq) || (k && !yk))) return SMALL_ERR_NULL;
     const Laid none{nullptr, {}, 1, 0, 1, 0};
     const Laid in[] = {q ? laid(r.N, r.S, r.heads, r.D, r.Cb, q, qs) : none, k ? laid(r.N, r.S, r.kv_heads, r.D, r.Cb, k, ks) : none};
@@ -315,7 +321,7 @@ extern "C" {
 int small_rotary_workspace(const small_rotation *r, size_t *bytes)
 {
     if (!r || !bytes) return SMALL_ERR_NULL;
-    if (const int rc = rotation_check(*r, true)) return rc;
+    if (const int rc = rotation_check(*r)) return rc;
     *bytes = grad_bytes(*r);
     return SMALL_OK;
 }
@@ -340,8 +346,13 @@ int small_cache_write(const small_cache *c, const small_span *s, const float *k,
     if (const int rc = cache_check(*c)) return rc;
     if (const int rc = cache_memory(*c)) return rc;
     if (const int rc = sizes_check(c->N, s->S, c->kv_heads, c->kv_heads, c->D, s->Cb, {&s->k, &s->v})) return rc;
+    small_rotation turn{};
     if (r) {
-        if (const int rc = rotation_check(*r, false)) return rc;
+        turn = *r;
+        turn.first = nullptr;                                  // (the span's takes its place)
+        if (const int rc = rotation_check(turn)) return rc;
+        if (q)
+            if (const int rc = strides_check({&r->q, &r->q_out})) return rc;
         if (r->N != c->N || r->S != s->S || r->kv_heads != c->kv_heads || r->D != c->D || r->Cb != s->Cb) return SMALL_ERR_SHAPE;
     }
     const Laid in[] = {laid(c->N, s->S, c->kv_heads, c->D, s->Cb, k, s->k), laid(c->N, s->S, c->kv_heads, c->D, s->Cb, v, s->v)};
@@ -354,7 +365,7 @@ int small_cache_write(const small_cache *c, const small_span *s, const float *k,
             if (t.meets(held.r[w])) return SMALL_ERR_ALIAS;
         for (int o = 0; o < w; ++o)
             if (held.r[o].meets(held.r[w])) return SMALL_ERR_ALIAS;
-        if (r && meets_rotation(*r, held.r[w])) return SMALL_ERR_ALIAS;
+        if (r && meets_rotation(turn, held.r[w])) return SMALL_ERR_ALIAS;
     }
     if (q) {
         const Laid queries = laid(c->N, s->S, r->heads, c->D, s->Cb, q, r->q), out = laid(c->N, s->S, r->heads, c->D, s->Cb, q_out, r->q_out);
@@ -366,10 +377,10 @@ int small_cache_write(const small_cache *c, const small_span *s, const float *k,
             if (!out.apart(t)) return SMALL_ERR_ALIAS;
         for (const Range &t : held.r)
             if (!out.apart(t) || !queries.apart(t)) return SMALL_ERR_ALIAS;
-        if (meets_rotation(*r, out.range())) return SMALL_ERR_ALIAS;
+        if (meets_rotation(turn, out.range())) return SMALL_ERR_ALIAS;
     }
     StoreArgs x{};
-    if (r) x.r = rotary_args(*r);
+    if (r) x.r = rotary_args(turn);
     if (const int rc = plan_store(x, *c, *s, q ? r->heads : 0, false)) return rc;
     x.k = k; x.v = v;
     x.ks = strides(s->k); x.vs = strides(s->v);

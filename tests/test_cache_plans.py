@@ -170,3 +170,33 @@ def test_any_sizes(plans):
         assert rc in (0, 2) and said == "", (kind, N, S_, heads, kv, D, Cb, rc, said)
         ran += rc == 0
     assert ran > 1000
+
+
+WILD = S.small_tokens(1 << 50, 1 << 50, 1 << 50)
+
+
+def test_what_a_write_does_not_read_is_not_looked_at(plans):
+    """Of a write's rotation: first, k, k_out, dq and dk, and without queries q and q_out. Nor the strides of queries or keys that a turn does not have."""
+    c = S.small_cache(kind=0, pages=2, page=16, kv_heads=2, D=8, keys=at(1), values=at(2), N=1, per_stream=2, table=at(5))
+    s = S.small_span(S=5, Cb=8, k=tokens(16, 5, 8), v=tokens(16, 5, 8))
+    r = S.small_rotation(N=1, S=5, heads=4, kv_heads=2, D=8, Cb=8, axes=1, pairs=4, freq_heads=1)
+    r.freq, r.first = at(9), at(1)                             # (first: in the cache's keys)
+    r.k = r.k_out = r.dq = r.dk = WILD
+    r.q = r.q_out = tokens(32, 5, 8)
+    assert call(plans, "small_cache_write", C.byref(c), C.byref(s), at(7), at(8), C.byref(r), at(10), at(11), None) == (0, "")
+    r.first = at(11)                                           # (in the queries' result)
+    assert call(plans, "small_cache_write", C.byref(c), C.byref(s), at(7), at(8), C.byref(r), at(10), at(11), None) == (0, "")
+    r.q = r.q_out = WILD
+    assert call(plans, "small_cache_write", C.byref(c), C.byref(s), at(7), at(8), C.byref(r), None, None, None) == (0, "")
+    assert call(plans, "small_cache_write", C.byref(c), C.byref(s), at(7), at(8), C.byref(r), at(10), at(11), None)[0] == 2
+    r.first = None
+    for q, k in ((at(10), None), (None, at(10))):
+        r.q = r.q_out = tokens(32, 5, 8) if q else WILD
+        r.k = r.k_out = tokens(16, 5, 8) if k else WILD
+        assert call(plans, "small_rotary", C.byref(r), q, k, q and at(11), k and at(11), None) == (0, "")
+        r.dq, r.dk = r.q, r.k
+        assert call(plans, "small_rotary_grad", C.byref(r), q, k, None, None, q and at(11), k and at(11), None, None, 0, None) == (0, "")
+    r.dq = WILD
+    assert call(plans, "small_rotary_grad", C.byref(r), None, at(10), None, None, None, at(11), None, None, 0, None) == (0, "")
+    n = C.c_size_t(0)
+    assert plans.small_rotary_workspace(C.byref(r), C.byref(n)) == 0        # sizes alone
