@@ -135,16 +135,19 @@ class Rotary:
                                      freq_heads=freq_heads, extent=(C.c_int * 4)(0, *extent))
         self._extents, self._workspace = len(extent) == axes - 1, None
 
-    def _fill(self, freq, first, positions):
-        r = self.record
+    def _filled(self, freq, first, positions):
+        """A call's own record: two threads may turn by one plan."""
+        r = small_rotation.from_buffer_copy(self.record)
         if positions is None and not self._extents:
             raise ValueError(f"places on {r.axes} axes need extents or positions")
         r.freq = A._floats(freq, (r.freq_heads, r.axes, r.pairs))
         r.first, r.positions = A._ints(first, (r.N,)), A._ints(positions, (r.N, r.S, r.axes))
+        return r
 
-    def _pair(self, q, k, names):
+    @staticmethod
+    def _pair(r, q, k, names):
         """Pointers of a tensor of queries and one of keys, either of which may be None, with their strides in the record."""
-        r, found = self.record, []
+        found = []
         for t, heads, name in ((q, r.heads, names[0]), (k, r.kv_heads, names[1])):
             p, s = (None, small_tokens()) if t is None else _blocks(t, r.N, r.S, r.Cb, heads * r.D)
             setattr(r, name, s)
@@ -157,29 +160,27 @@ class Rotary:
             rc = _fast().rotary(self.record, q, k, freq, positions, first, q_out, k_out, None)
             if rc is not None:
                 return B._check(rc, "small_rotary")
-        self._fill(freq, first, positions)
-        pq, pk = self._pair(q, k, ("q", "k"))
-        po, pko = self._pair(q if q_out is None else q_out, k if k_out is None else k_out, ("q_out", "k_out"))
-        small_rotary(self.record, pq, pk, po, pko, stream)
+        r = self._filled(freq, first, positions)
+        pq, pk = self._pair(r, q, k, ("q", "k"))
+        po, pko = self._pair(r, q if q_out is None else q_out, k if k_out is None else k_out, ("q_out", "k_out"))
+        small_rotary(r, pq, pk, po, pko, stream)
 
     def grad(self, dq_out, dk_out, freq, dq=None, dk=None, q=None, k=None, dfreq=None, first=None, positions=None, stream=None, from_inputs=False):
         """Turns the gradients of run's outputs back into those of its inputs (in place where dq and dk are None). With dfreq, [freq_heads][axes][pairs], the frequencies'
         gradient too, from q and k: run's outputs, or with from_inputs its inputs."""
-        r = self.record
         if dfreq is not None and self._workspace is None:
-            self._fill(freq, first, positions)
-            self._workspace = torch.empty(small_rotary_workspace(r), dtype=torch.uint8, device=self.device)
+            self._workspace = torch.empty(small_rotary_workspace(self._filled(freq, first, positions)), dtype=torch.uint8, device=self.device)
         if stream is None:
-            rc = _fast().rotary_grad(r, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, None if dfreq is None else self._workspace, int(from_inputs), None)
+            rc = _fast().rotary_grad(self.record, dq_out, dk_out, freq, positions, first, dq, dk, q, k, dfreq, None if dfreq is None else self._workspace, int(from_inputs), None)
             if rc is not None:
                 return B._check(rc, "small_rotary_grad")
-        self._fill(freq, first, positions)
+        r = self._filled(freq, first, positions)
         r.from_inputs = bool(from_inputs)
         if dfreq is not None:
             A._floats(dfreq, (r.freq_heads, r.axes, r.pairs))
-        pq, pk = self._pair(q, k, ("q", "k"))
-        pdo, pdko = self._pair(dq_out, dk_out, ("q_out", "k_out"))
-        pd, pdk = self._pair(dq_out if dq is None else dq, dk_out if dk is None else dk, ("dq", "dk"))
+        pq, pk = self._pair(r, q, k, ("q", "k"))
+        pdo, pdko = self._pair(r, dq_out, dk_out, ("q_out", "k_out"))
+        pd, pdk = self._pair(r, dq_out if dq is None else dq, dk_out if dk is None else dk, ("dq", "dk"))
         small_rotary_grad(r, pdo, pdko, pq, pk, pd, pdk, dfreq, None if dfreq is None else self._workspace, stream)
 
 
@@ -207,17 +208,20 @@ class PagedCache:
                                   key_scales=self.key_scales.data_ptr() if kind == "int8" else None,
                                   value_scales=self.value_scales.data_ptr() if kind == "int8" else None)
 
-    def _table(self, pages, N):
+    def _with(self, pages, N):
+        """The cache's record with a call's table: threads that serve different streams share the cache."""
         if pages.dim() != 2 or pages.shape[0] != N:
             raise TypeError(f"expected a table of pages of {N} streams, got {list(pages.shape)}")
-        self.record.N, self.record.per_stream, self.record.table = N, pages.shape[1], B._ptr32i(pages)
+        c = small_cache.from_buffer_copy(self.record)
+        c.N, c.per_stream, c.table = N, pages.shape[1], B._ptr32i(pages)
+        return c
 
     def _span(self, k, v, pages, first, counts):
         N, S, Cb = k.shape[0], k.shape[2], k.shape[3]
-        self._table(pages, N)
+        c = self._with(pages, N)
         pk, sk = _blocks(k, N, S, Cb, self.kv_heads * self.D)
         pv, sv = _blocks(v, N, S, Cb, self.kv_heads * self.D)
-        return small_span(S=S, Cb=Cb, k=sk, v=sv, first=A._ints(first, (N,)), counts=A._ints(counts, (N,))), pk, pv
+        return c, small_span(S=S, Cb=Cb, k=sk, v=sv, first=A._ints(first, (N,)), counts=A._ints(counts, (N,))), pk, pv
 
     def write(self, k, v, pages, first=None, counts=None, rotary=None, freq=None, positions=None, q=None, q_out=None, stream=None):
         """Tokens i < counts[n] of k and v into the cache at positions first[n] + i of stream n. With a Rotary plan of these sizes (and its freq) keys are turned on the way,
@@ -226,15 +230,15 @@ class PagedCache:
             rc = _fast().cache_write(self.record, k, v, pages, first, counts, None if rotary is None else rotary.record, freq, positions, q, q_out, None)
             if rc is not None:
                 return B._check(rc, "small_cache_write")
-        span, pk, pv = self._span(k, v, pages, first, counts)
+        c, span, pk, pv = self._span(k, v, pages, first, counts)
         if rotary is None:
             if q is not None:
                 raise TypeError("queries are turned by a Rotary plan: none was given")
-            return small_cache_write(self.record, span, pk, pv, stream=stream)
-        rotary._fill(freq, None, positions)
-        pq, _ = rotary._pair(q, None, ("q", "k"))
-        po, _ = rotary._pair(q if q_out is None else q_out, None, ("q_out", "k_out"))
-        small_cache_write(self.record, span, pk, pv, rotary.record, pq, po, stream)
+            return small_cache_write(c, span, pk, pv, stream=stream)
+        r = rotary._filled(freq, None, positions)
+        pq, _ = rotary._pair(r, q, None, ("q", "k"))
+        po, _ = rotary._pair(r, q if q_out is None else q_out, None, ("q_out", "k_out"))
+        small_cache_write(c, span, pk, pv, r, pq, po, stream)
 
     def read(self, k, v, pages, first=None, counts=None, stream=None):
         """The same tokens from the cache into k and v; what is no token of a stream's is left as it was."""
@@ -242,8 +246,8 @@ class PagedCache:
             rc = _fast().cache_read(self.record, k, v, pages, first, counts, None)
             if rc is not None:
                 return B._check(rc, "small_cache_read")
-        span, pk, pv = self._span(k, v, pages, first, counts)
-        small_cache_read(self.record, span, pk, pv, stream)
+        c, span, pk, pv = self._span(k, v, pages, first, counts)
+        small_cache_read(c, span, pk, pv, stream)
 
 
 class CacheAttention:
@@ -270,7 +274,7 @@ class CacheAttention:
                 return B._check(rc, "small_cache_attention")
         if pages.shape[1] != self.per_stream:
             raise TypeError(f"expected a table of {self.per_stream} pages a stream, got {list(pages.shape)}")
-        self.cache._table(pages, r.N)
+        c, r = self.cache._with(pages, r.N), small_attn.from_buffer_copy(r)
         r.lengths, r.first = A._ints(lengths, (r.N,)), A._ints(first, (r.N,))
         r.slopes = A._floats(slopes, (r.heads,))
         r.table, r.bucket = A._floats(table, (r.heads, r.buckets)), A._ints(bucket, (2 * r.reach + 1,))
@@ -278,7 +282,7 @@ class CacheAttention:
         po, r.out = _blocks(out, r.N, r.Sq, r.Cb, r.heads * r.D)
         if lse is not None:
             A._floats(lse, (r.N, r.heads, r.Sq))
-        small_cache_attention(self.cache.record, r, pq, po, lse, self.workspace, stream)
+        small_cache_attention(c, r, pq, po, lse, self.workspace, stream)
 
 
 def axis_frequencies(pairs, base=10000.0, axes=1):

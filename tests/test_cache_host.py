@@ -160,3 +160,65 @@ def test_tensors_are_checked_before_the_library():
         S.PagedCache(4, 16, 1, 8, tensors=[torch.zeros(1)] * 4)
     with pytest.raises(KeyError):
         S.PagedCache(4, 16, 1, 8, kind="float16")
+
+
+@pytest.fixture
+def on_ctypes(monkeypatch):
+    """Calls through ctypes with tensors on the host, and the library's functions replaced: what(record, ...) runs in the place of each."""
+    import torch
+    from paper_2303_04769_amd import attn, binding
+    what = {}
+    monkeypatch.setattr(attn, "_tokens", lambda t, N, S_, Cb: (t.data_ptr(), S.small_tokens(*t.stride()[:3])))
+    for name in ("_ptr", "_ptr32i"):
+        monkeypatch.setattr(binding, name, lambda t: None if t is None else t.data_ptr())
+    for name in ("small_rotary", "small_rotary_grad", "small_cache_write", "small_cache_read", "small_cache_attention"):
+        monkeypatch.setattr(K, name, lambda *args, name=name, **kw: what[name](*args, **kw))
+    return what
+
+
+def bits(record):
+    return bytes(C.string_at(C.addressof(record), C.sizeof(record)))
+
+
+def test_calls_at_the_same_time_have_records_of_their_own(on_ctypes):
+    """Two threads that serve different streams on one cache, and turn with one plan: while one is in the library the other fills its arguments. Neither sees the other's."""
+    import torch
+    pool = object.__new__(S.PagedCache)
+    pool.kind, pool.pages, pool.page, pool.kv_heads, pool.D = 0, 8, 16, 1, 4
+    pool.record = S.small_cache(kind=0, pages=8, page=16, kv_heads=1, D=4, keys=0x1000, values=0x2000)
+    turn = S.Rotary(1, 3, 2, 1, 4, Cb=4, device="cpu")
+    turn._workspace = torch.zeros(256, dtype=torch.uint8)
+    plans = []
+    for N, per in ((1, 2), (1, 3)):
+        plan = object.__new__(S.CacheAttention)
+        plan.cache, plan.per_stream, plan.workspace = pool, per, None
+        plan.record = S.small_attn(N=N, Sq=3, Sk=per * 16, heads=2, kv_heads=1, D=4, Cb=4, width=1)
+        plans.append(plan)
+    q, k, freq = torch.zeros(1, 2, 3, 4), torch.zeros(1, 1, 3, 4), [torch.zeros(1, 1, 2) for _ in range(2)]
+    tables, lengths = [torch.zeros(1, n, dtype=torch.int32) for n in (2, 3)], torch.zeros(1, dtype=torch.int32)
+    calls = {
+        "small_cache_write": lambda x: pool.write(k, k, tables[x], rotary=turn, freq=freq[x], q=q, stream="one"),
+        "small_cache_read": lambda x: pool.read(k, k, tables[x], stream="one"),
+        "small_cache_attention": lambda x: plans[x].run(q, q, tables[x], lengths, stream="one"),
+        "small_rotary": lambda x: turn.run(q, k, freq[x], stream="one"),
+        "small_rotary_grad": lambda x: turn.grad(q, k, freq[x], q=q, k=k, dfreq=torch.zeros(1, 1, 2), from_inputs=bool(x), stream="one"),
+    }
+    for name, call in calls.items():
+        seen = []
+
+        def inside(*args, **kw):
+            records = [a for a in args if isinstance(a, (S.small_cache, S.small_rotation))]
+            before = [bits(r) for r in records]
+            for r in records:
+                if isinstance(r, S.small_cache):
+                    assert (r.per_stream, r.table) == (tables[len(seen)].shape[1], tables[len(seen)].data_ptr()), name
+                else:
+                    assert r.freq == freq[len(seen)].data_ptr(), name
+            seen.append(records)
+            if len(seen) == 1:
+                call(1)                                        # (the other thread, meanwhile)
+            assert [bits(r) for r in records] == before, name
+        on_ctypes.clear()
+        on_ctypes[name] = inside
+        call(0)
+        assert len(seen) == 2

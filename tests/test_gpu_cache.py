@@ -574,6 +574,27 @@ def test_very_many_heads(T):
     assert torch.equal(back[0], k) and torch.equal(back[1], v)
 
 
+@pytest.mark.parametrize("kind", KINDS)
+def test_calls_with_a_stream(kind):
+    """A stream that is given, which goes through ctypes: the same bits as on the current stream."""
+    N, heads, kv, D, page, per, T = 2, 4, 2, 32, 16, 6, 20
+    q, k, v = rand(0, N, heads, T, D).to(DEV), rand(1, N, kv, T, D).to(DEV), rand(2, N, kv, T, D).to(DEV)
+    freq, first, lengths, table, side = rand(3, 1, 1, 16).to(DEV), ints([0, 37]), ints([T, 37 + T]), table_for(N, per, N * per), torch.cuda.Stream()
+    found = []
+    for stream in (None, side):
+        cache, turns = S.PagedCache(N * per, page, kv, D, kind=kind), S.Rotary(N, T, heads, kv, D, Cb=D)
+        turned, out, back = torch.empty_like(q), torch.empty_like(q), [torch.zeros_like(k) for _ in range(2)]
+        plan, lse = S.CacheAttention(cache, N, T, heads, per, Cb=D), torch.empty(N, heads, T, device=DEV)
+        torch.cuda.synchronize()
+        cache.write(k, v, table, first, rotary=turns, freq=freq, q=q, q_out=turned, stream=stream)
+        cache.read(*back, table, first, stream=stream)
+        plan.run(turned, out, table, lengths, lse=lse, first=first, stream=stream)
+        torch.cuda.synchronize()
+        found.append([turned, out, lse, *back])
+        assert cache.record.N == 0 and not cache.record.table and not turns.record.freq
+    assert all(torch.equal(a, b) for a, b in zip(*found))
+
+
 def test_a_cache_past_two_gigabytes():
     """Offsets of pages and channels past 32 bits: the last pages of a pool of 2.3 GB."""
     kv, D, page = 4, 256, 256
