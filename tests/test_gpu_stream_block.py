@@ -146,6 +146,84 @@ def test_streams_that_come_and_go(kind):
         close(out, want, k, TOL if kind == "float32" else 0.1 / (1 + float(want.abs().max())))
 
 
+def held64(x, kind):
+    """What a cache gives back for [..][D]: the rounding of its kind, of the fp32 value."""
+    x = x.float()
+    if kind == "int8":
+        top = x.abs().amax(-1, keepdim=True)
+        return (torch.round(x * (torch.full_like(top, 127.0) / top)) * (top / torch.full_like(top, 127.0))).double()
+    return (x.bfloat16() if kind == "bfloat16" else x).double()
+
+
+@pytest.mark.parametrize("kind", ["float32", "bfloat16", "int8"])
+def test_streams_against_what_the_cache_holds(kind):
+    """The cache holds what the definition's keys and values are rounded to, but for some that fp32 layers (off by TOL at most, by 2^-16 of the largest in nearly all) put on the other side
+    of a border: a step. Outputs are those of the definition in 64 bits on what is held, for all kinds within the error of fp32 layers. What a wrong turn, key head or mask would move is
+    many times that: looked at in the definition itself."""
+    gen = torch.Generator().manual_seed(11)
+    N, Cc, G, heads, kv_heads, D, page, per = 2, 48, 4, 4, 2, 16, 16, 12
+    w_in, w_out = uniform(gen, (heads + 2 * kv_heads) * D, Cc, of=4 * Cc ** -0.5), uniform(gen, Cc, heads * D, of=(heads * D) ** -0.5)
+    gamma, beta, freq = 1 + uniform(gen, Cc, of=0.3).float().double(), uniform(gen, Cc, of=0.3), uniform(gen, 2, 1, D // 2)
+    streams = [uniform(gen, 150, Cc) for _ in range(3)]
+
+    def keys_of(x, turn=True):
+        """(q, k, v) of one stream's frames"""
+        S_, place = x.shape[0], torch.arange(x.shape[0], dtype=torch.float64)[:, None]
+        qkv = norm64(x.view(S_, 1, Cc), gamma, beta, G).view(1, S_, Cc) @ w_in.t()
+        q, k, v = (t.reshape(1, S_, -1, D) for t in qkv.split((heads * D, kv_heads * D, kv_heads * D), 2))
+        return (turn64(q, place, freq, True), turn64(k, place, freq, True), v) if turn else (q, k, v)
+
+    def outputs(x, q, k, v, last=0):
+        i = torch.arange(x.shape[0])
+        return x + (attention64(q, k, v, None, 6.0, i[None] <= (i - last).clamp(min=0)[:, None]) @ w_out.t())[0]
+
+    block = AB.StreamBlock(*(t.float().cuda() for t in (w_in, w_out, gamma, beta, freq)), N, 20, page, per, Cc, G, heads, kv_heads, D, kind=kind, cap=6.0)
+    at, who, got, kept = [0, 0], [0, 1], {0: [], 1: [], 2: []}, {}
+
+    def bring(counts, width):
+        frames = torch.zeros(N, width, Cc, dtype=torch.float64)
+        for n, c in enumerate(counts):
+            frames[n, :c] = streams[who[n]][at[n]:at[n] + c]
+        out = block.forward(frames.float().cuda(), counts).cpu().double()
+        for n, c in enumerate(counts):
+            got[who[n]].append(out[n, :c])
+            at[n] += c
+
+    def keep(n):
+        """Keys and values that the cache holds of the stream in place n."""
+        pages = torch.tensor(block.held[n])
+        k, v = block.cache.keys.cpu()[pages].double()[..., :D], block.cache.values.cpu()[pages].double().transpose(2, 3)       # [pages][kv][page][D]
+        if kind == "int8":
+            k, v = (t * s.cpu()[pages].double()[..., None] for t, s in ((k, block.cache.key_scales), (v, block.cache.value_scales)))
+        kept[who[n]] = [t.transpose(1, 2).reshape(1, -1, kv_heads, D)[:, :at[n]] for t in (k, v)]
+    bring([40, 9], 40)
+    for _ in range(4):
+        bring([1, 1], 1)
+    bring([7, 0], 7)
+    keep(1)
+    block.release(1)
+    who[1], at[1] = 2, 0
+    bring([60, 50], 60)
+    bring([3, 3], 3)
+    keep(0)
+    keep(1)
+    for s, pieces in got.items():
+        out = torch.cat(pieces)
+        x = streams[s][:len(out)]
+        q, *rest = keys_of(x)
+        for held, exact in zip(kept[s], rest):
+            want, most = held64(exact, kind), exact.abs().amax(-1, keepdim=True)
+            step = {"float32": 0.0 * most, "bfloat16": 2.0 ** -7 * exact.abs(), "int8": most / 127}[kind]
+            off = (held - want).abs()
+            assert bool((off <= step + TOL).all()) and float((off <= 2.0 ** -16 * float(exact.abs().max())).double().mean()) > 0.99
+        want = outputs(x, q, *kept[s])
+        tol = TOL * (1 + float(want.abs().max()))
+        assert float((out - want).abs().max()) <= tol, (s, float((out - want).abs().max()), tol)
+        k, v = kept[s]
+        for wrong in (outputs(x, *keys_of(x, turn=False)), outputs(x, q, k.flip(2), v), outputs(x, q, k, v, last=1), outputs(x, q, 0 * k, v)):
+            assert float((wrong - want)[len(x) // 4:].abs().max()) > 8 * tol
+
+
 @pytest.mark.parametrize("kind", ["float32", "int8"])
 def test_frames_one_by_one_and_at_once(kind):
     """The same keys and values whichever way they come in: outputs differ by fp32 sums in another order alone."""
