@@ -183,12 +183,15 @@ class FrameBlock:
         return out
 
 
+# Rows of a key head (new frames times the query heads that share it) up to which frames attend to the cache itself. Up to there that is ahead of reading it back for the sequence kernels
+# for every kind and head width measured, the further the wider the heads (64 rows on 8 streams of 4096: floats of 32 channels 25 us and 31, of 96 37 and 59, of 256 76 and 130; bfloat16
+# of 96 26 and 57; codes 24 and 55). They draw level further on: floats at 256 rows (51 and 50, 92 and 93, 245 and 246), fewer bits beyond (codes of 96 53 and 87).
 ROWS_ON_CACHE = 64
 
 
 class StreamBlock:
     """The block over up to N streams, channels last, with rotary positions (freq: [1 or kv_heads][1][pairs]) and a paged cache of `pages` pages of `page` tokens for all of them,
-    `per_stream` of them at most for one; kind: what the cache holds (cache.PagedCache). Each call brings the next frames of some or all streams; a stream that ends gives its
+    `per_stream` of them at most for one; kind: what the cache holds (cache.PagedCache), 8-bit codes unless another is named. Each call brings the next frames of some or all streams; a stream that ends gives its
     pages back. Few new frames attend to the cache itself, many to what is read back from it: the same keys and values, whichever way a stream's frames come in."""
 
     def __init__(self, w_in, w_out, gamma, beta, freq, N, pages, page, per_stream, Cc, G, heads, kv_heads, D, kind="int8", cap=0.0, halves=True, Cb=16):

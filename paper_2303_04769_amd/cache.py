@@ -124,7 +124,7 @@ class Rotary:
     the sizes of all axes but the first, from which a token's number gives its place -- (W,) for images, (H, W) for clips; calls may give places instead.
     freq: [freq_heads][axes][pairs], radians a step (axis_frequencies); freq_heads 1 or kv_heads.
 
-    The gradient's workspace belongs to the plan: its calls must not overlap in time on different streams."""
+    The gradient's workspace belongs to the plan, which makes it at the first call with dfreq: such calls must not overlap in time on different streams."""
 
     def __init__(self, N, S, heads, kv_heads, D, axes=1, pairs=None, halves=False, extent=(), freq_heads=1, Cb=16, device="cuda:0"):
         extent = tuple(extent)
@@ -186,7 +186,7 @@ class Rotary:
 
 class PagedCache:
     """`pages` pages of `page` tokens (16, 32, 64, 128 or 256) for the keys and values of kv_heads heads of D channels, as "float32", "bfloat16" or "int8" (codes and a
-    scale for each token of a head). Its memory is four tensors, keys, values, key_scales, value_scales (the last two None but for int8); tensors: these, instead of new
+    scale for each token of a head), the last unless another is named. Its memory is four tensors, keys, values, key_scales, value_scales (the last two None but for int8); tensors: these, instead of new
     ones. Which pages a stream has is the program's affair: every call takes a table, int32 [N][pages of a stream at most]."""
 
     def __init__(self, pages, page, kv_heads, D, kind="int8", device="cuda:0", tensors=None):

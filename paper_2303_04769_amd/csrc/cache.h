@@ -51,7 +51,7 @@ struct StoreArgs {
     long long q_step, qo_step, k_step, v_step;
     int turns, N, S, lanes_log2, tile, tiles, items, parts;      // tile: tokens of a workgroup, 16 or 1
     const int *first, *counts;
-    FastDiv by_parts, by_tiles, by_per_q, by_per_k;              // by_per: heads of one set of frequencies
+    FastDiv by_parts, by_tiles, by_per_q;                        // by_per_q: query heads of one set of frequencies
 };
 hipError_t launch_cache_write(const StoreArgs &a, bool vec, bool halves, hipStream_t s);                   // cache_store.hip
 hipError_t launch_cache_read(const StoreArgs &a, bool vec, hipStream_t s);

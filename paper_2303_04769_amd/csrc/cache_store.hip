@@ -4,6 +4,7 @@
 // stream), four channels of a token a thread, and goes through its share of the heads: queries that are only turned, keys, values. Sines are computed
 // once for all heads that share them. Values go through LDS, since a channel's tokens stand together in the cache: sixteen of them are a store of 16 to 64 bytes.
 // 8 x 8192 tokens of 8 heads of 64 read from 8-bit codes: 67 us, 5.0 TB/s; 4 x 4096 tokens turned and written: 36 us (a large copy: 4.9 TB/s).
+// Written as they are, 8 x 8192 tokens: floats 127 us, 4.2 TB/s, bfloat16 103, 3.9, codes 83, 4.1; read: floats 102, 5.3, bfloat16 91, 4.4.
 #include "cache.h"
 
 #include <type_traits>

@@ -9,8 +9,8 @@
 // Codes are whole numbers below 128 and so bfloat16 numbers; queries and weights go in three bfloat16 parts of eight bits, which hold all of a float's 24 at its own
 // range, so the products are those of floats: no power of two that a token's neighbours set, whatever the scales. A key's scale multiplies its score, a value's its weight.
 //
-// 64 streams of 2048 to 16384 tokens, 16 heads on 4 key heads of 64, 8 bits: 67 us for 316 MB, 4.7 TB/s (a large copy: 4.9), and 5 for the join. Where the cache is smaller, a
-// workgroup's chain of dependent loads is what it takes: lengths, page numbers, keys and values, the waves' join (one round for each: 7 us).
+// 64 streams of 2048 to 16384 tokens, 16 heads on 4 key heads of 64, 8 bits: 68 us for 316 MB, 4.6 TB/s (a large copy: 4.9), and 5 for the join. Where the cache is smaller, a
+// workgroup's chain of dependent loads is what it takes: lengths, page numbers, keys and values, the waves' join (one round for each: 8 us).
 #include "attn_tile.h"
 #include "cache.h"
 

@@ -3,11 +3,11 @@
 // Bound by memory: every channel is read and written once. A thread computes the sines of a token's two or four neighbouring pairs (some 45 operations in 64 bits for
 // each) and turns these in all heads that share them, four heads' loads on their way at a time; lanes go along a channel block first and then along
 // tokens, so a wave's access is whole lines. Where tokens are few, heads are shared out over threads and sines computed again.
-// 14 x 14 pixels of 64 images, 8 heads of 32: 10.5 us, 4.9 TB/s; clips of 16 x 28 x 28 pixels: 23.2 us, 5.5 TB/s (a large copy: 4.9, one of 64 MB 8.0).
+// 14 x 14 pixels of 64 images, 8 heads of 32: 10.8 us, 4.8 TB/s; clips of 16 x 28 x 28 pixels: 24 us, 5.4 TB/s (a large copy: 4.9, one of 64 MB 8.0).
 //
 // With y = R(t) x, t = sum over axes of place * frequency: dx = R(-t) dy, and dt of a pair is dy1 y0 - dy0 y1, which needs no sine -- or dx1 x0 - dx0 x1, where x is what there is:
 // a turn of both leaves their cross product as it is (dx as it was rounded, as y is where that is read). Its sums times the places run in 64 bits
-// over a chunk of tokens for each workgroup, whose results a second launch adds up in a fixed order (8 x 8 pixels of 256 images: 9.5 us and 3.9; 6 x 999 frames: 9 and 3).
+// over a chunk of tokens for each workgroup, whose results a second launch adds up in a fixed order (8 x 8 pixels of 256 images: 12 us and 4; 6 x 999 frames: 10.5 and 2.5).
 #include "rotary.h"
 
 namespace small {
